@@ -51,7 +51,8 @@ typedef enum {
 
 /* Bits of the word a kernel ORs into `device_status` (device int32, may be NULL). */
 #define PSA_DEVSTAT_WAIT_EXPIRED 1 /* a bounded barrier wait gave up; outputs are invalid    */
-#define PSA_DEVSTAT_BAD_TARGET   2 /* dpo_logp: a scored target id was outside [0, vocab)    */
+#define PSA_DEVSTAT_BAD_TARGET   2 /* dpo_logp: a scored target id was outside [0, vocab);
+                                      psa_embed, psa_embed_bwd: a token id was             */
 #define PSA_DEVSTAT_BAD_SEGMENT  4 /* dpo_logp: a segment id was >= n_segments               */
 #define PSA_DEVSTAT_OUT_OF_BOUNDS 8 /* debug library only (libpsa_debug.so): a thread's own global
                                        index fell outside its tensor; the access was skipped     */
@@ -489,6 +490,111 @@ psa_status_t dpo_logp_bwd(const void* logits, int32_t logits_dtype, int64_t n_ro
                           const int32_t* fork_rows, const int32_t* fork_targets,
                           const int32_t* fork_segments, int32_t n_forks, int32_t n_segments,
                           const float* coef, void* dlogits, int32_t* device_status, void* stream);
+
+/*
+ * psa_norm -- normalisation of every token's row of hidden values, with the residual add in front of it (the step
+ * between the sublayers of a decoder layer; the paper has no counterpart).  Per row, in fp32:
+ *     s = x + residual, rounded to x's type (s = x where residual is NULL)
+ *     m = mean(s)  (0 if rms),   r = 1 / sqrt(mean((s - m)^2) + eps),   out = (s - m) * r * weight + bias
+ *   x, residual  device [n_tokens, hidden] of `dtype`; residual may be NULL
+ *   weight, bias device [hidden] of `weight_dtype`; bias may be NULL, and is NULL if rms
+ *   dtype, weight_dtype   PSA_DTYPE_BF16 with either type of weights, or PSA_DTYPE_F32 with fp32 weights
+ *   hidden       1 to 16384 (any: rows that are no multiple of 16 bytes are read element by element)
+ *   rms          0: layer norm, else the root-mean-square form
+ *   out          device [n_tokens, hidden] of `dtype` (out); may be x or residual
+ *   total        device [n_tokens, hidden] of `dtype` (out): s; given where residual is, may be x or residual
+ *   stats        device fp32 [2, n_tokens] (out): m of every row, then r of every row, for psa_norm_bwd
+ * A row with a NaN or an infinity gives NaN in that row alone.  n_tokens = 0 is a no-op.
+ * Errors: INVALID_ARG, UNSUPPORTED (hidden, n_tokens >= 2^31), ALIGNMENT (16 bytes), CUDA.
+ */
+psa_status_t psa_norm(const void* x, const void* residual, const void* weight, const void* bias,
+                      int32_t dtype, int32_t weight_dtype, int64_t n_tokens, int32_t hidden, float eps,
+                      int32_t rms, void* out, void* total, float* stats, void* stream);
+
+/*
+ * psa_norm_bwd -- gradient of psa_norm.  With u = (s - m) * r and g = d_out * weight:
+ *     dx = r * (g - u * mean(g * u) - mean(g)) + d_total      (no mean(g) if rms)
+ *     dweight = sum over tokens of d_out * u,   dbias = sum over tokens of d_out
+ *   d_out     device [n_tokens, hidden] of `dtype`
+ *   x         device: what was normalised, i.e. `total` where there was a residual
+ *   stats     device fp32 [2, n_tokens] as written by psa_norm
+ *   d_total   device or NULL: the gradient that reaches s by the residual stream
+ *   dx        device (out): the gradient of x and of residual; may be d_out, d_total or x
+ *   dweight, dbias   device [hidden] of `weight_dtype` (out); dbias may be NULL, and is NULL if rms
+ *   workspace device scratch of psa_norm_bwd_workspace_bytes() bytes, 16-byte aligned
+ * The sums over tokens are taken in an order that depends on the sizes alone.  n_tokens = 0 writes zeros to dweight, dbias.
+ * Errors: as psa_norm.
+ */
+size_t psa_norm_bwd_workspace_bytes(int64_t n_tokens, int32_t hidden);
+psa_status_t psa_norm_bwd(const void* d_out, const void* x, const void* weight, const float* stats,
+                          const void* d_total, int32_t dtype, int32_t weight_dtype, int64_t n_tokens,
+                          int32_t hidden, int32_t rms, void* dx, void* dweight, void* dbias,
+                          void* workspace, void* stream);
+
+/*
+ * psa_embed -- token embedding: out[t] = scale * table[token_ids[t]]  (the paper has no counterpart).
+ *   token_ids   device int32 [n_tokens]
+ *   table       device [vocab, hidden] of `dtype` (PSA_DTYPE_F32 or PSA_DTYPE_BF16)
+ *   out         device [n_tokens, hidden] of `dtype` (out)
+ *   device_status  device int32 or NULL: an id outside [0, vocab) ORs PSA_DEVSTAT_BAD_TARGET in and its row is zeros
+ * n_tokens up to 2^24, vocab up to 2^24, hidden up to 2^20.
+ * Errors: INVALID_ARG, UNSUPPORTED, ALIGNMENT (table, out: 16 bytes), CUDA.
+ */
+psa_status_t psa_embed(const int32_t* token_ids, const void* table, int32_t dtype, int64_t n_tokens,
+                       int64_t vocab, int32_t hidden, float scale, void* out, int32_t* device_status,
+                       void* stream);
+
+/*
+ * psa_embed_bwd -- gradient of psa_embed's table: dtable[v] = scale * sum over t with token_ids[t] = v of d_out[t],
+ * in fp32 and always in the tokens' order.
+ *   d_out       device [n_tokens, hidden] of `dtype`
+ *   dtable      device [vocab, hidden] of `grad_dtype` (PSA_DTYPE_F32, or bf16 where d_out is bf16)
+ *   accumulate  0: dtable is overwritten, with zeros in the rows of ids that do not occur;
+ *               else the gradient is added to what dtable holds, and other rows are neither read nor written
+ *   workspace   device scratch of psa_embed_bwd_workspace_bytes() bytes, 16-byte aligned
+ *   device_status  as for psa_embed; a bad id adds nothing
+ * Errors and limits: as psa_embed.
+ */
+size_t psa_embed_bwd_workspace_bytes(int64_t n_tokens, int64_t vocab, int32_t hidden);
+psa_status_t psa_embed_bwd(const void* d_out, const int32_t* token_ids, int32_t dtype, int32_t grad_dtype,
+                           int64_t n_tokens, int64_t vocab, int32_t hidden, float scale,
+                           int32_t accumulate, void* dtable, void* workspace, int32_t* device_status,
+                           void* stream);
+
+/*
+ * psa_ffn -- the gated feed-forward block of a decoder layer (the MLP layer of Section 4.2's micro-benchmarks):
+ *     G = X Wg,  U = X Wu,  H = silu(G) * U,  out = H Wd,      silu(g) = g / (1 + exp(-g))
+ * with fp32 sums; H, and G and U as they are kept for the backward, are rounded to bf16.
+ *   x            device bf16 [n_tokens, hidden]
+ *   w_gate, w_up device bf16 [hidden, ffn]      w_down  device bf16 [ffn, hidden]
+ *   hidden, ffn  multiples of 8, at most 2^20
+ *   out          device bf16 [n_tokens, hidden] (out)
+ *   gate, up     device bf16 [n_tokens, ffn] (out): G and U for psa_ffn_bwd; both NULL where there is no backward
+ *   workspace    device scratch of psa_ffn_workspace_bytes(.., backward = 0) bytes, 256-byte aligned
+ *   device_status  device int32 or NULL; PSA_DEVSTAT_WAIT_EXPIRED is ORed in as by psa_fwd
+ * Outputs must not overlap inputs or one another.  n_tokens = 0 is a no-op.
+ * Errors: INVALID_ARG, UNSUPPORTED (sizes), ALIGNMENT (16 bytes), CUDA.
+ */
+size_t psa_ffn_workspace_bytes(int64_t n_tokens, int32_t hidden, int32_t ffn, int32_t backward);
+psa_status_t psa_ffn(const void* x, const void* w_gate, const void* w_up, const void* w_down,
+                     int64_t n_tokens, int32_t hidden, int32_t ffn, void* out, void* gate, void* up,
+                     void* workspace, int32_t* device_status, void* stream);
+
+/*
+ * psa_ffn_bwd -- gradient of psa_ffn:
+ *     dH = dY Wd^T,  dU = dH * silu(G),  dG = dH * U * s * (1 + G * (1 - s))  with s = 1 / (1 + exp(-G)),
+ *     dx = dG Wg^T + dU Wu^T,  dw_gate = X^T dG,  dw_up = X^T dU,  dw_down = H^T dY
+ * with fp32 sums; dG, dU and H (formed again from G and U) are rounded to bf16 between the products.
+ *   d_out        device bf16 [n_tokens, hidden]      gate, up  as written by psa_ffn
+ *   dx, dw_gate, dw_up, dw_down   device bf16 (out), shaped as x and the weights
+ *   workspace    device scratch of psa_ffn_workspace_bytes(.., backward = 1) bytes, 256-byte aligned
+ * No atomics: the same inputs give the same bits.  n_tokens = 0 writes zeros to the weights' gradients.
+ * Errors and the rest: as psa_ffn.
+ */
+psa_status_t psa_ffn_bwd(const void* d_out, const void* x, const void* w_gate, const void* w_up,
+                         const void* w_down, const void* gate, const void* up, int64_t n_tokens,
+                         int32_t hidden, int32_t ffn, void* dx, void* dw_gate, void* dw_up, void* dw_down,
+                         void* workspace, int32_t* device_status, void* stream);
 
 /*
  * psa_profile_events -- measurement aid, no counterpart in the paper.  Registers a

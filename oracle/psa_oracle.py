@@ -561,3 +561,60 @@ def attention_layer_bwd(x, wq, wk, wv, wo, pos, mask, n_q_heads, n_kv_heads, d_o
     dk2 = rope(dk, neg, theta).reshape(T, -1)
     dv2 = dv.reshape(T, -1)
     return dict(dx=dq2 @ wq.T + dk2 @ wk.T + dv2 @ wv.T, dwq=x.T @ dq2, dwk=x.T @ dk2, dwv=x.T @ dv2, dwo=dwo)
+
+
+# ---------------------------------------------------------------------------- the decoder layer around the attention
+
+def norm_fwd(x, weight, bias=None, eps=1e-5, rms=False):
+    """Layer norm (or its root-mean-square form) of every row: (out, mean, 1 / deviation)."""
+    mean = np.zeros(len(x)) if rms else x.mean(axis=1)
+    rstd = 1.0 / np.sqrt(((x - mean[:, None]) ** 2).mean(axis=1) + eps)
+    out = (x - mean[:, None]) * rstd[:, None] * weight
+    return (out if bias is None else out + bias), mean, rstd
+
+
+def norm_bwd(d_out, x, weight, eps=1e-5, rms=False):
+    """(dx, dweight, dbias) for the loss sum(out * d_out), through the chain of the definition: out = c * r * w,
+    r = (var + eps)^-1/2, var = mean(c^2), c = x - mean(x)."""
+    n = x.shape[1]
+    c = x if rms else x - x.mean(axis=1, keepdims=True)
+    var = (c ** 2).mean(axis=1, keepdims=True) + eps
+    r = var ** -0.5
+    dr = (d_out * weight * c).sum(axis=1, keepdims=True)
+    dc = d_out * weight * r + (dr * -0.5 * var ** -1.5) * 2.0 * c / n
+    dx = dc if rms else dc - dc.mean(axis=1, keepdims=True)
+    return dx, (d_out * c * r).sum(axis=0), d_out.sum(axis=0)
+
+
+def embed_fwd(token_ids, table, scale=1.0):
+    """scale * table[token_ids], zeros for ids outside the table."""
+    out = np.zeros((len(token_ids), table.shape[1]))
+    for t, v in enumerate(token_ids):
+        if 0 <= v < len(table):
+            out[t] = scale * table[v]
+    return out
+
+
+def embed_bwd(d_out, token_ids, vocab, scale=1.0):
+    """Gradient of embed_fwd's table."""
+    grad = np.zeros((vocab, d_out.shape[1]))
+    for t, v in enumerate(token_ids):
+        if 0 <= v < vocab:
+            grad[v] += scale * d_out[t]
+    return grad
+
+
+def ffn_fwd(x, w_gate, w_up, w_down):
+    """The gated feed-forward block: (out, gate, up, h)."""
+    gate, up = x @ w_gate, x @ w_up
+    h = gate / (1.0 + np.exp(-gate)) * up
+    return h @ w_down, gate, up, h
+
+
+def ffn_bwd(d_out, x, w_gate, w_up, w_down):
+    """(dx, dw_gate, dw_up, dw_down) for the loss sum(out * d_out)."""
+    _, gate, up, h = ffn_fwd(x, w_gate, w_up, w_down)
+    s = 1.0 / (1.0 + np.exp(-gate))
+    dh = d_out @ w_down.T
+    d_gate, d_up = dh * up * (s + gate * s * (1.0 - s)), dh * gate * s
+    return d_gate @ w_gate.T + d_up @ w_up.T, x.T @ d_gate, x.T @ d_up, h.T @ d_out

@@ -35,7 +35,8 @@ EXPORTED_SYMBOLS = (
     "psa_bwd_static_scratch", "dpo_loss", "dpo_logp_bwd", "psa_pack_ffd", "psa_position_ids", "psa_rope",
     "psa_step_host_arena_bytes", "psa_step_host", "simpo_loss", "orpo_loss", "psa_bwd_f32",
     "psa_check_device_status", "psa_selftest_wait_expiry", "psa_logp_labels", "psa_pack_ffd_emit",
-    "psa_selftest_bounds", "dpo_logp_f64sum", "psa_plan_launch",
+    "psa_selftest_bounds", "dpo_logp_f64sum", "psa_plan_launch", "psa_norm", "psa_norm_bwd", "psa_norm_bwd_workspace_bytes",
+    "psa_embed", "psa_embed_bwd", "psa_embed_bwd_workspace_bytes", "psa_ffn", "psa_ffn_bwd", "psa_ffn_workspace_bytes",
 )
 
 
@@ -96,10 +97,19 @@ def load_library():
     lib.dpo_logp_bwd.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.dpo_logp.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp]
     lib.dpo_logp_f64sum.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+    lib.psa_norm.argtypes = [vp, vp, vp, vp, i32, i32, i64, i32, f32, i32, vp, vp, vp, vp]
+    lib.psa_norm_bwd.argtypes = [vp, vp, vp, vp, vp, i32, i32, i64, i32, i32, vp, vp, vp, vp, vp]
+    lib.psa_norm_bwd_workspace_bytes.argtypes = [i64, i32]
+    lib.psa_embed.argtypes = [vp, vp, i32, i64, i64, i32, f32, vp, vp, vp]
+    lib.psa_embed_bwd.argtypes = [vp, vp, i32, i32, i64, i64, i32, f32, i32, vp, vp, vp, vp]
+    lib.psa_embed_bwd_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.psa_ffn.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.psa_ffn_bwd.argtypes = [vp] * 7 + [i64, i32, i32] + [vp] * 7
+    lib.psa_ffn_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    lib.psa_step_host_arena_bytes.argtypes = [vp]
     for name in EXPORTED_SYMBOLS:
-        if name == "psa_step_host_arena_bytes":
-            lib.psa_step_host_arena_bytes.restype = C.c_size_t
-            lib.psa_step_host_arena_bytes.argtypes = [C.c_void_p]
+        if name.endswith("_bytes"):
+            getattr(lib, name).restype = C.c_size_t
         elif name != "psa_status_string":
             getattr(lib, name).restype = C.c_int
     _lib = lib
@@ -708,3 +718,234 @@ def psa_rope(x, position_ids, rope_theta=10000.0, out=None, stream=None):
     _check("psa_rope", load_library().psa_rope(_ptr(x), _ptr(out), _ptr(position_ids), x.shape[0], x.shape[1],
                                               x.shape[2], float(rope_theta), _stream(stream)))
     return out
+
+
+def _want_given(given):
+    """Raises ValueError unless every tensor of `given`, a list of (name, tensor, shape, dtype), fits, and all of them lie
+    on the current CUDA device: the kernels take sizes from the first ones alone, and launch there."""
+    import torch
+    for placement in (False, True):
+        for name, t, shape, dtype in given:
+            _want(t, name, shape, dtype, True, placement)
+    devices = {t.device for _, t, _, _ in given if t.device.type == "cuda"}
+    if devices and devices != {torch.device("cuda", torch.cuda.current_device())}:
+        raise ValueError("tensors on %s: all have to be on the current device" % ", ".join(sorted(map(str, devices))))
+
+
+def _want_apart(outputs, inputs):
+    """Raises ValueError where an output, a (name, tensor), shares memory with an input or with another output."""
+    span = lambda t: (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())  # noqa: E731
+    for i, (name, t) in enumerate(outputs):
+        lo, hi = span(t)
+        for other, u in outputs[i + 1:] + inputs:
+            a, b = span(u)
+            if lo < b and a < hi:
+                raise ValueError("%s and %s share memory" % (name, other))
+
+
+def _dtype_code(t, name):
+    """PSA_DTYPE_F32 or PSA_DTYPE_BF16 of a tensor."""
+    import torch
+    if t.dtype == torch.float32:
+        return PSA_DTYPE_F32
+    if t.dtype == torch.bfloat16:
+        return PSA_DTYPE_BF16
+    raise ValueError("%s: dtype %s, fp32 or bf16 is needed" % (name, t.dtype))
+
+
+def _want_norm(x, weight, name):
+    """(n_tokens, hidden, type of x, type of weight) of a normalisation."""
+    if x.dim() != 2:
+        raise ValueError("%s: a [tokens, hidden] tensor is needed" % name)
+    dtype, wtype = _dtype_code(x, name), _dtype_code(weight, "weight")
+    if dtype == PSA_DTYPE_F32 and wtype != PSA_DTYPE_F32:
+        raise ValueError("weight: fp32 rows need fp32 weights")
+    return x.shape[0], x.shape[1], dtype, wtype
+
+
+def psa_norm(x, weight, bias=None, eps=1e-5, rms=False, residual=None, out=None, total=None, stats=None, stream=None):
+    """Layer norm, or with rms=True the root-mean-square form, of every row of x [T, hidden] (bf16 or fp32) with weight and
+    bias [hidden] (x's type, or fp32).  With `residual` [T, hidden] the rows of x + residual are normalised.  Returns
+    (out, stats), or (out, stats, total) with total = x + residual; stats, fp32 [2, T], and what was normalised are what
+    psa_norm_bwd needs.  out and total may be x or residual."""
+    import torch
+    T, D, dtype, wtype = _want_norm(x, weight, "x")
+    given = [("x", x, (T, D), x.dtype), ("weight", weight, (D,), weight.dtype)]
+    if bias is not None:
+        if rms:
+            raise ValueError("bias: the root-mean-square form has none")
+        given.append(("bias", bias, (D,), weight.dtype))
+    if residual is not None:
+        given.append(("residual", residual, (T, D), x.dtype))
+    elif total is not None:
+        raise ValueError("total: there is none without residual")
+    _want_given(given)
+    out = torch.empty_like(x) if out is None else out
+    stats = torch.empty((2, T), dtype=torch.float32, device=x.device) if stats is None else stats
+    outputs = [("out", out, (T, D), x.dtype), ("stats", stats, (2, T), torch.float32)]
+    if residual is not None:
+        total = torch.empty_like(x) if total is None else total
+        outputs.append(("total", total, (T, D), x.dtype))
+    _want_given(outputs)
+    _want_in_place([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given], {"out": ("x", "residual"),
+                                                                                      "total": ("x", "residual")})
+    _check("psa_norm", load_library().psa_norm(_ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), dtype, wtype, T, D, float(eps),
+                                               1 if rms else 0, _ptr(out), _ptr(total), _ptr(stats), _stream(stream)))
+    return (out, stats) if residual is None else (out, stats, total)
+
+
+def _want_in_place(outputs, inputs, allowed):
+    """_want_apart, but an output named in `allowed` may be one of the inputs listed there, the whole of it."""
+    for name, t in outputs:
+        whole = [(n, u) for n, u in inputs if n in allowed.get(name, ()) and u.data_ptr() == t.data_ptr()]
+        _want_apart([(name, t)], [i for i in inputs if all(i[1] is not w[1] for w in whole)])
+    _want_apart(outputs, [])
+
+
+def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=False, dx=None, dweight=None, dbias=None,
+                 workspace=None, stream=None):
+    """Gradient of psa_norm: x is what was normalised (`total` where there was a residual), d_total, if given, the gradient
+    that reaches it by the residual stream.  Returns (dx, dweight, dbias), dbias None unless with_bias; dx is the gradient of
+    x and of residual, and may be d_out, d_total or x."""
+    import torch
+    T, D, dtype, wtype = _want_norm(x, weight, "x")
+    given = [("d_out", d_out, (T, D), x.dtype), ("x", x, (T, D), x.dtype), ("weight", weight, (D,), weight.dtype),
+             ("stats", stats, (2, T), torch.float32)]
+    if d_total is not None:
+        given.append(("d_total", d_total, (T, D), x.dtype))
+    if rms and (with_bias or dbias is not None):
+        raise ValueError("dbias: the root-mean-square form has no bias")
+    _want_given(given)
+    dx = torch.empty_like(x) if dx is None else dx
+    dweight = torch.empty_like(weight) if dweight is None else dweight
+    outputs = [("dx", dx, (T, D), x.dtype), ("dweight", dweight, (D,), weight.dtype)]
+    if with_bias or dbias is not None:
+        dbias = torch.empty_like(weight) if dbias is None else dbias
+        outputs.append(("dbias", dbias, (D,), weight.dtype))
+    _want_given(outputs)
+    _want_in_place([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given], {"dx": ("d_out", "d_total", "x")})
+    lib = load_library()
+    need = lib.psa_norm_bwd_workspace_bytes(T, D)
+    if workspace is None:
+        workspace = _temporary(max(need, 256), torch.uint8, x.device, stream)
+    _want_room(workspace, "workspace", need)
+    _check("psa_norm_bwd", lib.psa_norm_bwd(_ptr(d_out), _ptr(x), _ptr(weight), _ptr(stats), _ptr(d_total), dtype, wtype, T, D,
+                                            1 if rms else 0, _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                                            _stream(stream)))
+    return dx, dweight, dbias
+
+
+def psa_embed(token_ids, table, scale=1.0, out=None, status=None, stream=None):
+    """scale * table[token_ids]: token_ids int32 [T], table [vocab, hidden] bf16 or fp32 -> [T, hidden].  An id outside the
+    vocabulary gives a row of zeros and sets PSA_DEVSTAT_BAD_TARGET in `status`."""
+    import torch
+    if table.dim() != 2 or token_ids.dim() != 1:
+        raise ValueError("token_ids: [tokens], table: [vocab, hidden]")
+    dtype = _dtype_code(table, "table")
+    T, (V, D) = token_ids.shape[0], table.shape
+    _want_given([("token_ids", token_ids, (T,), torch.int32), ("table", table, (V, D), table.dtype)])
+    _want_status(status)
+    out = torch.empty((T, D), dtype=table.dtype, device=table.device) if out is None else out
+    _want_given([("out", out, (T, D), table.dtype)])
+    _want_apart([("out", out)], [("token_ids", token_ids), ("table", table)])
+    _check("psa_embed", load_library().psa_embed(_ptr(token_ids), _ptr(table), dtype, T, V, D, float(scale), _ptr(out),
+                                                 _ptr(status), _stream(stream)))
+    return out
+
+
+def psa_embed_bwd(d_out, token_ids, vocab, scale=1.0, dtable=None, dtype=None, accumulate=False, workspace=None, status=None,
+                  stream=None):
+    """Gradient [vocab, hidden] of psa_embed's table for d_out [T, hidden] (bf16 or fp32), in d_out's type, or in fp32 with
+    dtype=torch.float32 or an fp32 `dtable`.  With accumulate=True it is added to `dtable`, where only the rows of ids that
+    occur are touched.  Sums are fp32 and in the tokens' order."""
+    import torch
+    if d_out.dim() != 2 or token_ids.dim() != 1:
+        raise ValueError("d_out: [tokens, hidden], token_ids: [tokens]")
+    if accumulate and dtable is None:
+        raise ValueError("accumulate: a dtable to add to is needed")
+    T, D, V = d_out.shape[0], d_out.shape[1], int(vocab)
+    code = _dtype_code(d_out, "d_out")
+    _want_given([("d_out", d_out, (T, D), d_out.dtype), ("token_ids", token_ids, (T,), torch.int32)])
+    _want_status(status)
+    if dtable is None:
+        dtable = torch.empty((V, D), dtype=dtype or d_out.dtype, device=d_out.device)
+    grad = _dtype_code(dtable, "dtable")
+    if (dtype is not None and dtable.dtype != dtype) or (code == PSA_DTYPE_F32 and grad != PSA_DTYPE_F32):
+        raise ValueError("dtable: dtype %s does not fit" % dtable.dtype)
+    _want_given([("dtable", dtable, (V, D), dtable.dtype)])
+    _want_apart([("dtable", dtable)], [("d_out", d_out), ("token_ids", token_ids)])
+    lib = load_library()
+    need = lib.psa_embed_bwd_workspace_bytes(T, V, D)
+    if workspace is None:
+        workspace = _temporary(max(need, 256), torch.uint8, d_out.device, stream)
+    _want_room(workspace, "workspace", need)
+    _check("psa_embed_bwd", lib.psa_embed_bwd(_ptr(d_out), _ptr(token_ids), code, grad, T, V, D, float(scale),
+                                              1 if accumulate else 0, _ptr(dtable), _ptr(workspace), _ptr(status),
+                                              _stream(stream)))
+    return dtable
+
+
+def _want_ffn(x, w_gate, w_up, w_down):
+    """(T, hidden, ffn) and the checked operands of a feed-forward block."""
+    import torch
+    if x.dim() != 2 or w_gate.dim() != 2:
+        raise ValueError("x: [tokens, hidden], w_gate: [hidden, ffn]")
+    (T, D), F = x.shape, w_gate.shape[1]
+    given = [("x", x, (T, D), torch.bfloat16), ("w_gate", w_gate, (D, F), torch.bfloat16),
+             ("w_up", w_up, (D, F), torch.bfloat16), ("w_down", w_down, (F, D), torch.bfloat16)]
+    return T, D, F, given
+
+
+def psa_ffn(x, w_gate, w_up, w_down, save=True, out=None, gate=None, up=None, workspace=None, status=None, stream=None):
+    """The gated feed-forward block (silu(x w_gate) * (x w_up)) w_down, bf16: x [T, hidden], w_gate and w_up [hidden, ffn],
+    w_down [ffn, hidden], hidden and ffn multiples of 8.  Returns (out, saved); saved = (gate, up) [T, ffn] each is what
+    psa_ffn_bwd needs, None with save=False."""
+    import torch
+    T, D, F, given = _want_ffn(x, w_gate, w_up, w_down)
+    _want_given(given)
+    _want_status(status)
+    out = torch.empty_like(x) if out is None else out
+    outputs = [("out", out, (T, D), torch.bfloat16)]
+    if save:
+        new = lambda: torch.empty((T, F), dtype=torch.bfloat16, device=x.device)  # noqa: E731
+        gate, up = new() if gate is None else gate, new() if up is None else up
+        outputs += [("gate", gate, (T, F), torch.bfloat16), ("up", up, (T, F), torch.bfloat16)]
+    elif gate is not None or up is not None:
+        raise ValueError("gate, up: not written with save=False")
+    _want_given(outputs)
+    _want_apart([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given])
+    lib = load_library()
+    need = lib.psa_ffn_workspace_bytes(T, D, F, 0)
+    if workspace is None:
+        workspace = _temporary(max(need, 256), torch.uint8, x.device, stream)
+    _want_room(workspace, "workspace", need)
+    _check("psa_ffn", lib.psa_ffn(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), T, D, F, _ptr(out), _ptr(gate), _ptr(up),
+                                  _ptr(workspace), _ptr(status), _stream(stream)))
+    return out, ((gate, up) if save else None)
+
+
+def psa_ffn_bwd(d_out, x, w_gate, w_up, w_down, saved, dx=None, dw_gate=None, dw_up=None, dw_down=None, workspace=None,
+                status=None, stream=None):
+    """Gradient of psa_ffn for d_out [T, hidden]; `saved` as psa_ffn returned it.  Returns (dx, dw_gate, dw_up, dw_down),
+    bf16."""
+    import torch
+    T, D, F, given = _want_ffn(x, w_gate, w_up, w_down)
+    gate, up = saved
+    given += [("d_out", d_out, (T, D), torch.bfloat16), ("gate", gate, (T, F), torch.bfloat16), ("up", up, (T, F), torch.bfloat16)]
+    _want_given(given)
+    _want_status(status)
+    dx, dw_gate, dw_up, dw_down = (torch.empty_like(like) if t is None else t
+                                   for t, like in ((dx, x), (dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down)))
+    outputs = [("dx", dx, (T, D), torch.bfloat16), ("dw_gate", dw_gate, (D, F), torch.bfloat16),
+               ("dw_up", dw_up, (D, F), torch.bfloat16), ("dw_down", dw_down, (F, D), torch.bfloat16)]
+    _want_given(outputs)
+    _want_apart([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given])
+    lib = load_library()
+    need = lib.psa_ffn_workspace_bytes(T, D, F, 1)
+    if workspace is None:
+        workspace = _temporary(max(need, 256), torch.uint8, x.device, stream)
+    _want_room(workspace, "workspace", need)
+    _check("psa_ffn_bwd", lib.psa_ffn_bwd(_ptr(d_out), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(gate), _ptr(up),
+                                          T, D, F, _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(workspace),
+                                          _ptr(status), _stream(stream)))
+    return dx, dw_gate, dw_up, dw_down

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpsa.so")
 LIB_DEBUG = os.path.join(HERE, "libpsa_debug.so")   # the same sources with -DPSA_DEBUG_BOUNDS (checked global indices)
 SOURCES = ["psa_plan.cpp", "psa_host_helpers.cpp", "psa_api.cu", "psa_fwd.cu", "psa_bwd.cu", "psa_bwd_static.cu", "psa_selftest.cu",
-           "dpo_logp.cu", "dpo_loss.cu", "psa_rope.cu"]
+           "dpo_logp.cu", "dpo_loss.cu", "psa_rope.cu", "psa_norm.cu", "psa_embed.cu", "psa_ffn.cu"]
 
 
 def _stale(lib=LIB) -> bool:
