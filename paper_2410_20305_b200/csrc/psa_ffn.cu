@@ -53,6 +53,15 @@ struct GemmParams {
 
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
 
+// dH, G, U of an element -> dG and dU (over G and U) and H.
+__device__ __forceinline__ void gate_bwd(float dh, float& g, float& u, float& h) {
+  const float s = sigmoid(g), act = g * s;
+  h = act * u;
+  const float dg = dh * u * (s * (1.0f + g * (1.0f - s)));
+  u = dh * act;
+  g = dg;
+}
+
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
@@ -202,18 +211,13 @@ ffn_small_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[j + i]);
           if (EPI == kEpiGateBwd) {
-            float g[8], u[8], dg[8], du[8], h[8];
+            float g[8], u[8], h[8];
             unpack8(*reinterpret_cast<const uint4*>(prm.gate + at), g);
             unpack8(*reinterpret_cast<const uint4*>(prm.up + at), u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float sg = sigmoid(g[i]), act = g[i] * sg;
-              h[i] = act * u[i];
-              du[i] = x[i] * act;
-              dg[i] = x[i] * u[i] * (sg * (1.0f + g[i] * (1.0f - sg)));
-            }
-            *reinterpret_cast<uint4*>(prm.out[0] + at) = pack8(dg);
-            *reinterpret_cast<uint4*>(prm.out[1] + at) = pack8(du);
+            for (int i = 0; i < 8; ++i) gate_bwd(x[i], g[i], u[i], h[i]);
+            *reinterpret_cast<uint4*>(prm.out[0] + at) = pack8(g);
+            *reinterpret_cast<uint4*>(prm.out[1] + at) = pack8(u);
             *reinterpret_cast<uint4*>(prm.h + at) = pack8(h);
           } else if (prm.splits > 1) {
             float4* dst = reinterpret_cast<float4*>(prm.partial + (int64_t(blockIdx.z) * prm.n_outputs + sel) * prm.M * prm.N + at);
@@ -231,6 +235,305 @@ ffn_small_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__
   if (warp == 5) {
     tc_fence_after();
     tmem_dealloc(tmem, kBN);
+  }
+}
+
+// ---------------------------------------------------------------- two CTAs per tile of 256 x 256
+// A persistent kernel: 74 clusters of two CTAs take every 74th tile.  A tile's product is one UMMA stream of the pair
+// (M = 256, N = 256): each CTA loads its 128 rows of A and 128 of the tile's 256 columns of B, so a stage brings 32 KB to each
+// SM for the work of which a CTA alone would need 48.  The accumulator takes half of TMEM: while the end of one tile
+// drains it, the next tile's UMMAs fill the other half.
+// Warps: 0 TMA, 1 UMMA (in the CTA of rank 0), 2 TMEM, 4-7 the end of a tile, each for 32 rows of its CTA.
+// A result leaves by TMA stores of 32 rows x 64 columns, from four buffers that each warp owns: no barrier but the warp's own,
+// and the tensor map clips what lies behind the last row or column.
+constexpr int kBigBM = 256, kBigBN = 256, kBigStages = 5, kBigThreads = 256, kBigBufs = 4;
+constexpr uint32_t kBigHalf = 128 * kBK * 2;                       // one operand's half of a stage
+constexpr uint32_t kBigStageBytes = 2 * kBigHalf;
+constexpr uint32_t kBufBytes = 32 * 64 * 2;
+constexpr uint32_t kBigBufsAt = kBigStages * kBigStageBytes;
+constexpr uint32_t kBigBarsAt = kBigBufsAt + 4 * kBigBufs * kBufBytes;
+constexpr uint32_t kBigSmem = kBigBarsAt + 256 + 1024;
+static_assert(kBigSmem <= 227 * 1024, "shared memory of one CTA");
+
+struct BigMaps {
+  CUtensorMap a[2], b[2], out[3], in[2];    // out: C of both outputs, or G / dG, U / dU, H;  in: G, U
+};
+
+template <bool A_MN, bool B_MN, int EPI>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBigThreads, 1)
+ffn_big_kernel(const __grid_constant__ BigMaps maps, const GemmParams prm) {
+  constexpr int kTileN = EPI == kEpiGate ? kBigBN / 2 : kBigBN;
+  constexpr uint32_t kSub = kChunk * kBK * 2;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen_base = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t bars = base + kBigBarsAt;
+  auto full = [&](int s) { return bars + 8u * s; };                    // of rank 0: both CTAs' loads
+  auto empty = [&](int s) { return bars + 8u * (kBigStages + s); };
+  auto acc_full = [&](int i) { return bars + 8u * (2 * kBigStages + i); };
+  auto acc_empty = [&](int i) { return bars + 8u * (2 * kBigStages + 2 + i); };   // of rank 0: both CTAs' warps
+  auto in_full = [&](int w) { return bars + 8u * (2 * kBigStages + 4 + w); };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + kBigBarsAt + 192);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_base + kBigBarsAt + 200);
+  const WaitCtx wctx{abort_flag, prm.status, kWaitLimitClocks};
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const int cluster = int(blockIdx.x) >> 1, n_clusters = int(gridDim.x) >> 1;
+
+  const int m_tiles = (prm.M + kBigBM - 1) / kBigBM, n_all = prm.n_tiles * prm.n_outputs, n_work = m_tiles * n_all;
+  const int total = prm.k_tiles * prm.k_pairs;
+  // Tiles run down kGroup rows of tiles before they move one column on: the 74 tiles in flight share kGroup strips of A
+  // and about 74 / kGroup of B, which stay in L2.
+  constexpr int kGroup = 8;
+  struct Place { int m0, n0, sel; };
+  auto place = [&](int tile) {
+    const int per_group = kGroup * n_all, group = tile / per_group, first = group * kGroup;
+    const int rows = min(kGroup, m_tiles - first), in = tile - group * per_group;
+    const int n = in / rows;
+    return Place{(first + in % rows) * kBigBM, (n % prm.n_tiles) * kTileN, n / prm.n_tiles};
+  };
+
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int s = 0; s < kBigStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(acc_full(i), 1); mbar_init(acc_empty(i), 8); }
+    for (int w = 0; w < 4; ++w) mbar_init(in_full(w), 1);
+    fence_mbar_init();
+    for (int i = 0; i < 2; ++i) { tma_prefetch_desc(&maps.a[i]); tma_prefetch_desc(&maps.b[i]); }
+  }
+  if (warp == 2) tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();     // the other CTA's barriers are there
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int n = 0;
+      for (int tile = cluster; tile < n_work && !*abort_flag; tile += n_clusters) {
+        const Place at = place(tile);
+        const int m0 = at.m0 + 128 * int(rank);
+        for (int it = 0; it < total; ++it, ++n) {
+          const int s = n % kBigStages;
+          if (n >= kBigStages) mbar_wait(empty(s), (n / kBigStages - 1) & 1, wctx);
+          if (*abort_flag) break;
+          const bool second = it >= prm.k_tiles;
+          const int k0 = (second ? it - prm.k_tiles : it) * kBK;
+          const uint32_t sa = base + s * kBigStageBytes, sb = sa + kBigHalf, bar = cluster_map(full(s), 0);
+          const CUtensorMap* am = &maps.a[second];
+          if (rank == 0) mbar_expect_tx(full(s), 2 * kBigStageBytes);
+          if (A_MN) {
+            tma_load_3d_pair(sa, am, m0, 0, k0, bar);
+            tma_load_3d_pair(sa + kSub, am, m0 + kChunk, 0, k0, bar);
+          } else {
+            tma_load_3d_pair(sa, am, k0, 0, m0, bar);
+          }
+          // Gate: rank 0 loads the tile's features of Wg, rank 1 the same features of Wu.
+          const CUtensorMap* bm = &maps.b[EPI == kEpiGate ? int(rank) : (second || at.sel)];
+          const int n0 = EPI == kEpiGate ? at.n0 : at.n0 + 128 * int(rank);
+          if (B_MN) {
+            tma_load_3d_pair(sb, bm, n0, 0, k0, bar);
+            tma_load_3d_pair(sb + kSub, bm, n0 + kChunk, 0, k0, bar);
+          } else {
+            tma_load_3d_pair(sb, bm, k0, 0, n0, bar);
+          }
+        }
+      }
+      if (*abort_flag) {   // shared memory must outlive the copies in flight (the cluster's last barrier holds the other CTA)
+        const long long t0 = clock64();
+        if (rank == 0)
+          for (int i = n > kBigStages ? n - kBigStages : 0; i < n; ++i)
+            while (!mbar_try_wait(full(i % kBigStages), (i / kBigStages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
+        while (clock64() - t0 < 1000000) {}
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const uint32_t issuer = elect_one();
+      constexpr uint32_t idesc = umma_idesc_bf16(kBigBM, kBigBN, A_MN, B_MN);
+      int n = 0, i = 0;
+      for (int tile = cluster; tile < n_work && !*abort_flag; tile += n_clusters, ++i) {
+        const uint32_t acc = tmem + uint32_t(i & 1) * 256;
+        mbar_wait_cluster(acc_empty(i & 1), ((i >> 1) & 1) ^ 1, wctx);
+        tc_fence_after();
+        for (int it = 0; it < total; ++it, ++n) {
+          const int s = n % kBigStages;
+          mbar_wait_cluster(full(s), (n / kBigStages) & 1, wctx);
+          if (*abort_flag) break;
+          tc_fence_after();
+          const uint32_t sa = base + s * kBigStageBytes;
+          const uint32_t a = smem_desc_lo(sa, A_MN ? kSub : 16), b = smem_desc_lo(sa + kBigHalf, B_MN ? kSub : 16);
+#pragma unroll
+          for (int kk = 0; kk < kBK / 16; ++kk)
+            umma_ss_pair_w(acc, a + kk * ((A_MN ? 2048 : 32) >> 4), b + kk * ((B_MN ? 2048 : 32) >> 4), idesc, it > 0 || kk > 0, issuer);
+          umma_commit_pair_w(empty(s), issuer);
+        }
+        umma_commit_pair_w(acc_full(i & 1), issuer);
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    const int w = warp - 4;
+    const uint32_t bufs = base + kBigBufsAt + uint32_t(w) * kBigBufs * kBufBytes;
+    auto buf = [&](uint32_t use) { return bufs + (use % kBigBufs) * kBufBytes; };
+    // 16 bytes (8 columns) of this thread's row in a buffer, in the 128-byte-swizzled layout of the tensor maps
+    auto cell = [&](uint32_t b, int eight) { return b + uint32_t(lane) * 128 + ((uint32_t(eight) ^ uint32_t(lane & 7)) << 4); };
+    uint32_t use = 0;      // buffers used so far; each is one group of stores
+    int i = 0, n_in = 0;   // n_in: loads of G and U requested so far
+    for (int tile = cluster; tile < n_work && !*abort_flag; tile += n_clusters, ++i) {
+      const Place at = place(tile);
+      const int row0 = at.m0 + 128 * int(rank) + 32 * w;
+      const uint32_t lanes = tmem + uint32_t(i & 1) * 256 + (uint32_t(w * 32) << 16);
+      auto store = [&](const CUtensorMap* m, uint32_t b, int col) {    // by one lane, after the warp's writes
+        if (row0 < prm.M && col < prm.N) tma_store_3d(m, b, col, 0, row0);
+        tma_commit_group();
+      };
+      if (EPI != kEpiGateBwd) {
+        mbar_wait(acc_full(i & 1), (i >> 1) & 1, wctx);
+        tc_fence_after();
+        if (*abort_flag) break;
+      }
+      if (EPI == kEpiOut) {
+#pragma unroll 1
+        for (int c = 0; c < kBigBN / 64; ++c, ++use) {
+          uint32_t v[64];
+          tmem_ld64_wait(lanes + c * 64, v);
+          if (c == kBigBN / 64 - 1) {      // the accumulator is read
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(cluster_map(acc_empty(i & 1), 0));
+          }
+          if (lane == 0) tma_wait_group_read<kBigBufs - 1>();
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float* x = reinterpret_cast<const float*>(v) + 8 * j;
+            const uint4 p = pack8(x);
+            st_shared_v4(cell(buf(use), j), p.x, p.y, p.z, p.w);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) store(&maps.out[at.sel], buf(use), at.n0 + c * 64);
+        }
+      } else if (EPI == kEpiGate) {
+        const bool keep = prm.out[0] != nullptr;
+        const int n_bufs = keep ? 3 : 1;
+#pragma unroll 1
+        for (int c = 0; c < kTileN / 64; ++c, use += n_bufs) {
+          if (lane == 0) {
+            if (keep) tma_wait_group_read<kBigBufs - 3>(); else tma_wait_group_read<kBigBufs - 1>();
+          }
+          __syncwarp();
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            uint32_t g[32], u[32];
+            tmem_ld32_wait(lanes + c * 64 + half * 32, g);
+            tmem_ld32_wait(lanes + kTileN + c * 64 + half * 32, u);
+            if (c == kTileN / 64 - 1 && half) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive_cluster(cluster_map(acc_empty(i & 1), 0));
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float *gf = reinterpret_cast<const float*>(g) + 8 * j, *uf = reinterpret_cast<const float*>(u) + 8 * j;
+              float h[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) h[k] = gf[k] * sigmoid(gf[k]) * uf[k];
+              const int at8 = half * 4 + j;
+              uint4 p = pack8(h);
+              st_shared_v4(cell(buf(use), at8), p.x, p.y, p.z, p.w);
+              if (keep) {
+                p = pack8(gf);
+                st_shared_v4(cell(buf(use + 1), at8), p.x, p.y, p.z, p.w);
+                p = pack8(uf);
+                st_shared_v4(cell(buf(use + 2), at8), p.x, p.y, p.z, p.w);
+              }
+            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            store(&maps.out[2], buf(use), at.n0 + c * 64);
+            if (keep) {
+              store(&maps.out[0], buf(use + 1), at.n0 + c * 64);
+              store(&maps.out[1], buf(use + 2), at.n0 + c * 64);
+            }
+          }
+        }
+      } else {
+        // G and U of the tile arrive in two buffers, and leave from them as dG and dU.
+#pragma unroll 1
+        for (int c = 0; c < kBigBN / 64; ++c, use += 3) {
+          if (lane == 0) {
+            tma_wait_group_read<kBigBufs - 3>();
+            mbar_expect_tx(in_full(w), 2 * kBufBytes);
+            tma_load_3d(buf(use), &maps.in[0], at.n0 + c * 64, 0, row0, in_full(w));
+            tma_load_3d(buf(use + 1), &maps.in[1], at.n0 + c * 64, 0, row0, in_full(w));
+          }
+          if (c == 0) {
+            mbar_wait(acc_full(i & 1), (i >> 1) & 1, wctx);
+            tc_fence_after();
+          }
+          mbar_wait(in_full(w), n_in & 1, wctx);
+          ++n_in;
+          __syncwarp();
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            uint32_t v[32];
+            tmem_ld32_wait(lanes + c * 64 + half * 32, v);
+            if (c == kBigBN / 64 - 1 && half) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive_cluster(cluster_map(acc_empty(i & 1), 0));
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float* x = reinterpret_cast<const float*>(v) + 8 * j;
+              const int at8 = half * 4 + j;
+              float g[8], u[8], h[8];
+              unpack8(ld_shared_v4(cell(buf(use), at8)), g);
+              unpack8(ld_shared_v4(cell(buf(use + 1), at8)), u);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) gate_bwd(x[k], g[k], u[k], h[k]);
+              uint4 p = pack8(g);
+              st_shared_v4(cell(buf(use), at8), p.x, p.y, p.z, p.w);
+              p = pack8(u);
+              st_shared_v4(cell(buf(use + 1), at8), p.x, p.y, p.z, p.w);
+              p = pack8(h);
+              st_shared_v4(cell(buf(use + 2), at8), p.x, p.y, p.z, p.w);
+            }
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (*abort_flag) break;
+          if (lane == 0) {
+            store(&maps.out[0], buf(use), at.n0 + c * 64);
+            store(&maps.out[1], buf(use + 1), at.n0 + c * 64);
+            store(&maps.out[2], buf(use + 2), at.n0 + c * 64);
+          }
+        }
+      }
+    }
+    if (lane == 0) {
+      if (EPI == kEpiGateBwd && *abort_flag && n_in > 0) {   // loads of G and U in flight
+        const long long t0 = clock64();
+        while (!mbar_try_wait(in_full(w), (n_in - 1) & 1) && clock64() - t0 < kWaitLimitClocks) {}
+      }
+      tma_wait_group_read<0>();   // shared memory must outlive the stores' reads
+    }
+    __syncwarp();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive();
+  cluster_wait();     // no CTA leaves while the pair's UMMAs or arrivals may still reach it
+  if (warp == 2) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, 512);
   }
 }
 
@@ -263,6 +566,8 @@ struct Product {
   int k_pairs = 1, n_outputs = 1;
 };
 
+bool takes_big(int64_t M, int64_t N, int n_outputs);
+
 int split_count(int64_t M, int64_t N, int64_t K, int k_pairs, int n_outputs) {
   const int64_t tiles = ((M + kSmallBM - 1) / kSmallBM) * ((N + kSmallBN - 1) / kSmallBN) * n_outputs;
   if (tiles == 0) return 1;
@@ -271,12 +576,49 @@ int split_count(int64_t M, int64_t N, int64_t K, int k_pairs, int n_outputs) {
 }
 
 int64_t partial_bytes(int64_t M, int64_t N, int64_t K, int k_pairs, int n_outputs) {
+  if (takes_big(M, N, n_outputs)) return 0;
   const int s = split_count(M, N, K, k_pairs, n_outputs);
   return s > 1 ? 4 * M * N * n_outputs * s : 0;
 }
 
+bool takes_big(int64_t M, int64_t N, int n_outputs) {
+  return ((M + kBigBM - 1) / kBigBM) * ((N + kBigBN - 1) / kBigBN) * n_outputs >= kSmCount / 2;
+}
+
+template <bool A_MN, bool B_MN, int EPI>
+psa_status_t launch_big(const Product& p, GemmParams prm, cudaStream_t stream) {
+  constexpr int kTileN = EPI == kEpiGate ? kBigBN / 2 : kBigBN;
+  BigMaps maps;
+  bool ok = true;
+  for (int i = 0; i < 2; ++i) {
+    const void *pa = p.a[i] ? p.a[i] : p.a[0], *pb = p.b[i] ? p.b[i] : p.b[0];
+    ok = ok && (A_MN ? matrix_map(&maps.a[i], pa, p.K, p.M, kBK) : matrix_map(&maps.a[i], pa, p.M, p.K, 128));
+    ok = ok && (B_MN ? matrix_map(&maps.b[i], pb, p.K, p.N, kBK) : matrix_map(&maps.b[i], pb, p.N, p.K, 128));
+    const void *out = prm.out[i] ? prm.out[i] : prm.out[0], *in = i ? prm.up : prm.gate;
+    ok = ok && matrix_map(&maps.out[i], out ? out : prm.h, p.M, p.N, 32);
+    maps.in[i] = maps.a[i];
+    if (EPI == kEpiGateBwd) ok = ok && matrix_map(&maps.in[i], in, p.M, p.N, 32);
+  }
+  ok = ok && matrix_map(&maps.out[2], prm.h ? prm.h : prm.out[0], p.M, p.N, 32);
+  if (!ok) return PSA_ERR_CUDA;
+  prm.M = int32_t(p.M);
+  prm.N = int32_t(p.N);
+  prm.k_tiles = int32_t((p.K + kBK - 1) / kBK);
+  prm.k_pairs = p.k_pairs;
+  prm.n_tiles = int32_t((p.N + kTileN - 1) / kTileN);
+  prm.n_outputs = p.n_outputs;
+  prm.splits = 1;
+  auto kernel = ffn_big_kernel<A_MN, B_MN, EPI>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem) != cudaSuccess) return PSA_ERR_CUDA;
+  const int64_t tiles = (p.M + kBigBM - 1) / kBigBM * prm.n_tiles * p.n_outputs;
+  const unsigned grid = unsigned(2 * std::min<int64_t>(tiles, kSmCount / 2));
+  kernel<<<grid, kBigThreads, kBigSmem, stream>>>(maps, prm);
+  return check_last_cuda_error("psa_ffn launch");
+}
+
 template <bool A_MN, bool B_MN, int EPI>
 psa_status_t launch_product(const Product& p, GemmParams prm, cudaStream_t stream) {
+  if (takes_big(p.M, EPI == kEpiGate ? 2 * p.N : p.N, p.n_outputs)) return launch_big<A_MN, B_MN, EPI>(p, prm, stream);
   constexpr int kTileN = EPI == kEpiGate ? kSmallBN / 2 : kSmallBN;
   CUtensorMap a[2], b[2];
   for (int i = 0; i < 2; ++i) {
