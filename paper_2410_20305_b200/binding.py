@@ -9,8 +9,9 @@ Calls go through ctypes, or, as a training step makes them, through a compiled
 route that takes 4 to 9 us less of the host: psa_plan, psa_fwd and the losses
 without stream=, psa_bwd and psa_bwd_f32 without stream= and with workspace=,
 dpo_logp without stream=, out= and scratch=, dpo_logp_bwd without stream= and
-with dlogits=, psa_rope without stream= and with out=.  Results and refusals
-are the same.
+with dlogits=, psa_rope without stream= and with out=, the normalisation, the
+embedding and the feed-forward block without stream= and outputs of their own.
+Results and refusals are the same.
 """
 from __future__ import annotations
 
@@ -123,7 +124,9 @@ def load_library():
 _native = None
 _native_tried = False
 _NATIVE_ENTRIES = ("psa_fwd", "psa_bwd", "psa_bwd_f32", "dpo_logp_f64sum", "dpo_logp_bwd", "dpo_loss", "simpo_loss",
-                   "orpo_loss", "psa_rope", "psa_plan", "psa_plan_stats", "psa_plan_destroy")
+                   "orpo_loss", "psa_rope", "psa_plan", "psa_plan_stats", "psa_plan_destroy", "psa_norm", "psa_norm_bwd",
+                   "psa_norm_bwd_workspace_bytes", "psa_embed", "psa_embed_bwd", "psa_embed_bwd_workspace_bytes", "psa_ffn",
+                   "psa_ffn_bwd", "psa_ffn_workspace_bytes")
 
 
 def _load_native():
@@ -743,6 +746,17 @@ def _want_apart(outputs, inputs):
                 raise ValueError("%s and %s share memory" % (name, other))
 
 
+def _scratch(workspace, need, like, stream):
+    """The caller's workspace, refused unless it has `need` bytes where `like` is, or a temporary one."""
+    import torch
+    if workspace is None:
+        return _temporary(max(need, 256), torch.uint8, like.device, stream)
+    _want_room(workspace, "workspace", need)
+    if workspace.device != like.device:
+        raise ValueError("workspace: on %s, the call's tensors are on %s" % (workspace.device, like.device))
+    return workspace
+
+
 def _dtype_code(t, name):
     """PSA_DTYPE_F32 or PSA_DTYPE_BF16 of a tensor."""
     import torch
@@ -768,6 +782,13 @@ def psa_norm(x, weight, bias=None, eps=1e-5, rms=False, residual=None, out=None,
     bias [hidden] (x's type, or fp32).  With `residual` [T, hidden] the rows of x + residual are normalised.  Returns
     (out, stats), or (out, stats, total) with total = x + residual; stats, fp32 [2, T], and what was normalised are what
     psa_norm_bwd needs.  out and total may be x or residual."""
+    fast = _fast(stream) if out is None and total is None and stats is None else None
+    if fast:
+        got = fast.norm(x, weight, bias, float(eps), rms, residual)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            _check("psa_norm", got)
     import torch
     T, D, dtype, wtype = _want_norm(x, weight, "x")
     given = [("x", x, (T, D), x.dtype), ("weight", weight, (D,), weight.dtype)]
@@ -807,6 +828,13 @@ def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=Fal
     """Gradient of psa_norm: x is what was normalised (`total` where there was a residual), d_total, if given, the gradient
     that reaches it by the residual stream.  Returns (dx, dweight, dbias), dbias None unless with_bias; dx is the gradient of
     x and of residual, and may be d_out, d_total or x."""
+    fast = _fast(stream) if dx is None and dweight is None and dbias is None else None
+    if fast:
+        got = fast.norm_bwd(d_out, x, weight, stats, rms, d_total, with_bias, workspace)
+        if type(got) is tuple:
+            return got if with_bias else got + (None,)
+        if got is not None:
+            _check("psa_norm_bwd", got)
     import torch
     T, D, dtype, wtype = _want_norm(x, weight, "x")
     given = [("d_out", d_out, (T, D), x.dtype), ("x", x, (T, D), x.dtype), ("weight", weight, (D,), weight.dtype),
@@ -826,9 +854,7 @@ def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=Fal
     _want_in_place([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given], {"dx": ("d_out", "d_total", "x")})
     lib = load_library()
     need = lib.psa_norm_bwd_workspace_bytes(T, D)
-    if workspace is None:
-        workspace = _temporary(max(need, 256), torch.uint8, x.device, stream)
-    _want_room(workspace, "workspace", need)
+    workspace = _scratch(workspace, need, x, stream)
     _check("psa_norm_bwd", lib.psa_norm_bwd(_ptr(d_out), _ptr(x), _ptr(weight), _ptr(stats), _ptr(d_total), dtype, wtype, T, D,
                                             1 if rms else 0, _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(workspace),
                                             _stream(stream)))
@@ -838,6 +864,13 @@ def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=Fal
 def psa_embed(token_ids, table, scale=1.0, out=None, status=None, stream=None):
     """scale * table[token_ids]: token_ids int32 [T], table [vocab, hidden] bf16 or fp32 -> [T, hidden].  An id outside the
     vocabulary gives a row of zeros and sets PSA_DEVSTAT_BAD_TARGET in `status`."""
+    fast = _fast(stream) if out is None else None
+    if fast:
+        got = fast.embed(token_ids, table, float(scale), status)
+        if type(got) is int:
+            _check("psa_embed", got)
+        elif got is not None:
+            return got
     import torch
     if table.dim() != 2 or token_ids.dim() != 1:
         raise ValueError("token_ids: [tokens], table: [vocab, hidden]")
@@ -859,6 +892,13 @@ def psa_embed_bwd(d_out, token_ids, vocab, scale=1.0, dtable=None, dtype=None, a
     dtype=torch.float32 or an fp32 `dtable`.  With accumulate=True it is added to `dtable`, where only the rows of ids that
     occur are touched.  Sums are fp32 and in the tokens' order."""
     import torch
+    fast = _fast(stream) if dtable is None and not accumulate and dtype in (None, torch.float32) else None
+    if fast:
+        got = fast.embed_bwd(d_out, token_ids, vocab, float(scale), dtype is not None, workspace, status)
+        if type(got) is int:
+            _check("psa_embed_bwd", got)
+        elif got is not None:
+            return got
     if d_out.dim() != 2 or token_ids.dim() != 1:
         raise ValueError("d_out: [tokens, hidden], token_ids: [tokens]")
     if accumulate and dtable is None:
@@ -876,9 +916,7 @@ def psa_embed_bwd(d_out, token_ids, vocab, scale=1.0, dtable=None, dtype=None, a
     _want_apart([("dtable", dtable)], [("d_out", d_out), ("token_ids", token_ids)])
     lib = load_library()
     need = lib.psa_embed_bwd_workspace_bytes(T, V, D)
-    if workspace is None:
-        workspace = _temporary(max(need, 256), torch.uint8, d_out.device, stream)
-    _want_room(workspace, "workspace", need)
+    workspace = _scratch(workspace, need, d_out, stream)
     _check("psa_embed_bwd", lib.psa_embed_bwd(_ptr(d_out), _ptr(token_ids), code, grad, T, V, D, float(scale),
                                               1 if accumulate else 0, _ptr(dtable), _ptr(workspace), _ptr(status),
                                               _stream(stream)))
@@ -900,6 +938,13 @@ def psa_ffn(x, w_gate, w_up, w_down, save=True, out=None, gate=None, up=None, wo
     """The gated feed-forward block (silu(x w_gate) * (x w_up)) w_down, bf16: x [T, hidden], w_gate and w_up [hidden, ffn],
     w_down [ffn, hidden], hidden and ffn multiples of 8.  Returns (out, saved); saved = (gate, up) [T, ffn] each is what
     psa_ffn_bwd needs, None with save=False."""
+    fast = _fast(stream) if out is None and gate is None and up is None else None
+    if fast:
+        got = fast.ffn(x, w_gate, w_up, w_down, save, workspace, status)
+        if type(got) is int:
+            _check("psa_ffn", got)
+        elif got is not None:
+            return (got[0], got[1:]) if save else (got, None)
     import torch
     T, D, F, given = _want_ffn(x, w_gate, w_up, w_down)
     _want_given(given)
@@ -916,9 +961,7 @@ def psa_ffn(x, w_gate, w_up, w_down, save=True, out=None, gate=None, up=None, wo
     _want_apart([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given])
     lib = load_library()
     need = lib.psa_ffn_workspace_bytes(T, D, F, 0)
-    if workspace is None:
-        workspace = _temporary(max(need, 256), torch.uint8, x.device, stream)
-    _want_room(workspace, "workspace", need)
+    workspace = _scratch(workspace, need, x, stream)
     _check("psa_ffn", lib.psa_ffn(_ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), T, D, F, _ptr(out), _ptr(gate), _ptr(up),
                                   _ptr(workspace), _ptr(status), _stream(stream)))
     return out, ((gate, up) if save else None)
@@ -928,6 +971,13 @@ def psa_ffn_bwd(d_out, x, w_gate, w_up, w_down, saved, dx=None, dw_gate=None, dw
                 status=None, stream=None):
     """Gradient of psa_ffn for d_out [T, hidden]; `saved` as psa_ffn returned it.  Returns (dx, dw_gate, dw_up, dw_down),
     bf16."""
+    fast = _fast(stream) if dx is None and dw_gate is None and dw_up is None and dw_down is None else None
+    if fast:
+        got = fast.ffn_bwd(d_out, x, w_gate, w_up, w_down, saved[0], saved[1], workspace, status)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            _check("psa_ffn_bwd", got)
     import torch
     T, D, F, given = _want_ffn(x, w_gate, w_up, w_down)
     gate, up = saved
@@ -942,9 +992,7 @@ def psa_ffn_bwd(d_out, x, w_gate, w_up, w_down, saved, dx=None, dw_gate=None, dw
     _want_apart([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given])
     lib = load_library()
     need = lib.psa_ffn_workspace_bytes(T, D, F, 1)
-    if workspace is None:
-        workspace = _temporary(max(need, 256), torch.uint8, x.device, stream)
-    _want_room(workspace, "workspace", need)
+    workspace = _scratch(workspace, need, x, stream)
     _check("psa_ffn_bwd", lib.psa_ffn_bwd(_ptr(d_out), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(gate), _ptr(up),
                                           T, D, F, _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(workspace),
                                           _ptr(status), _stream(stream)))

@@ -25,6 +25,15 @@ struct Entry {   // in the order of binding.py's _NATIVE_ENTRIES
   decltype(&::psa_plan) plan;
   decltype(&::psa_plan_stats) stats;
   decltype(&::psa_plan_destroy) destroy;
+  decltype(&::psa_norm) norm;
+  decltype(&::psa_norm_bwd) norm_bwd;
+  decltype(&::psa_norm_bwd_workspace_bytes) norm_bwd_bytes;
+  decltype(&::psa_embed) embed;
+  decltype(&::psa_embed_bwd) embed_bwd;
+  decltype(&::psa_embed_bwd_workspace_bytes) embed_bwd_bytes;
+  decltype(&::psa_ffn) ffn;
+  decltype(&::psa_ffn_bwd) ffn_bwd;
+  decltype(&::psa_ffn_workspace_bytes) ffn_bytes;
 } g_lib;
 bool g_ready = false;
 
@@ -349,9 +358,251 @@ PyObject* destroy(PyObject*, PyObject* handle) {
   Py_RETURN_NONE;
 }
 
+// ---- the calls below take tensors of the current device and make their outputs; a workspace may be given
+bool here(const at::Tensor& t) { return t.device().index() == c10::cuda::current_device(); }
+const at::Tensor* take_here(PyObject* o, at::ScalarType type, at::IntArrayRef shape) {
+  const at::Tensor* t = plain(o);
+  return t && t->scalar_type() == type && t->sizes() == shape && t->is_contiguous() && here(*t) ? t : nullptr;
+}
+// As take_here, where None stands for a null pointer.
+bool take_optional(PyObject* o, at::ScalarType type, at::IntArrayRef shape, void** p) {
+  *p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = take_here(o, type, shape);
+  if (t) *p = t->data_ptr();
+  return t != nullptr;
+}
+bool take_bool(PyObject* o, bool* v) {
+  *v = o == Py_True;
+  return PyBool_Check(o);
+}
+bool take_dtype(const at::Tensor& t, int32_t* code) {
+  *code = t.scalar_type() == at::kFloat ? PSA_DTYPE_F32 : PSA_DTYPE_BF16;
+  return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16;
+}
+at::Tensor make(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like) {
+  return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+}
+// A workspace of `bytes`: the caller's, or one of the current stream, which torch gives to a later tensor of that stream.
+bool take_workspace(PyObject* o, size_t bytes, const at::Tensor& like, at::Tensor* ws) {
+  if (o == Py_None) {
+    *ws = make({int64_t(bytes < 256 ? 256 : bytes)}, at::kByte, like);
+    return true;
+  }
+  const at::Tensor* t = plain(o);
+  const int64_t n = int64_t(bytes);
+  if (!t || !here(*t) || int64_t(t->nbytes()) < n ||
+      int64_t(t->storage().nbytes()) - t->storage_offset() * int64_t(t->itemsize()) < n)
+    return false;
+  *ws = *t;
+  return true;
+}
+template <typename... T>
+PyObject* tuple_of(const T&... t) {
+  return Py_BuildValue(sizeof...(T) == 2 ? "(NN)" : sizeof...(T) == 3 ? "(NNN)" : "(NNNN)", THPVariable_Wrap(t)...);
+}
+
+// Rows [T, hidden] and their weight, as a normalisation takes them.
+struct NormArgs {
+  const at::Tensor *x, *weight;
+  int64_t T, hidden;
+  int32_t dtype, wtype;
+};
+bool take_norm(PyObject* x, PyObject* weight, NormArgs* a) {
+  a->x = plain(x);
+  a->weight = plain(weight);
+  if (!a->x || !a->weight || a->x->dim() != 2 || !a->x->is_contiguous() || !here(*a->x) || !take_dtype(*a->x, &a->dtype) ||
+      !take_dtype(*a->weight, &a->wtype))
+    return false;
+  a->T = a->x->size(0);
+  a->hidden = a->x->size(1);
+  return a->hidden <= INT32_MAX && take_here(weight, a->weight->scalar_type(), {a->hidden});
+}
+
+// norm(x, weight, bias, eps, rms, residual) -> (out, stats) or (out, stats, total), a status code (not 0), or None
+PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    NormArgs m;
+    float eps;
+    bool rms;
+    void *bias, *res;
+    if (n != 6 || !modes_off() || !take_norm(a[0], a[1], &m) || !take_float(a[3], &eps) || !take_bool(a[4], &rms) ||
+        !take_optional(a[2], m.weight->scalar_type(), {m.hidden}, &bias) ||
+        !take_optional(a[5], m.x->scalar_type(), {m.T, m.hidden}, &res) || (rms && a[2] != Py_None) ||
+        (m.dtype == PSA_DTYPE_F32 && m.wtype != PSA_DTYPE_F32))
+      return none();
+    const bool add = a[5] != Py_None;
+    at::Tensor out = make({m.T, m.hidden}, m.x->scalar_type(), *m.x), stats = make({2, m.T}, at::kFloat, *m.x), total;
+    if (add) total = make({m.T, m.hidden}, m.x->scalar_type(), *m.x);
+    void *const x = m.x->data_ptr(), *const w = m.weight->data_ptr(), *const to = out.data_ptr(), *const on = stream();
+    void* const sum = add ? total.data_ptr() : nullptr;
+    float* const st = stats.data_ptr<float>();
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.norm(x, res, w, bias, m.dtype, m.wtype, m.T, int32_t(m.hidden), eps, rms, to, sum, st, on);
+    });
+    if (rc != PSA_OK) return PyLong_FromLong(rc);
+    return add ? tuple_of(out, stats, total) : tuple_of(out, stats);
+  });
+}
+
+// norm_bwd(d_out, x, weight, stats, rms, d_total, with_bias, workspace) -> (dx, dweight) or (dx, dweight, dbias), a status
+// code (not 0), or None
+PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    NormArgs m;
+    bool rms, with_bias;
+    void *d_out, *stats, *d_total;
+    at::Tensor ws;
+    if (n != 8 || !modes_off() || !take_norm(a[1], a[2], &m) || !take_bool(a[4], &rms) || !take_bool(a[6], &with_bias) ||
+        a[0] == Py_None || !take_optional(a[0], m.x->scalar_type(), {m.T, m.hidden}, &d_out) || a[3] == Py_None ||
+        !take_optional(a[3], at::kFloat, {2, m.T}, &stats) ||
+        !take_optional(a[5], m.x->scalar_type(), {m.T, m.hidden}, &d_total) || (rms && with_bias) ||
+        (m.dtype == PSA_DTYPE_F32 && m.wtype != PSA_DTYPE_F32) ||
+        !take_workspace(a[7], g_lib.norm_bwd_bytes(m.T, int32_t(m.hidden)), *m.x, &ws))
+      return none();
+    at::Tensor dx = make({m.T, m.hidden}, m.x->scalar_type(), *m.x), dw = make({m.hidden}, m.weight->scalar_type(), *m.x), db;
+    if (with_bias) db = make({m.hidden}, m.weight->scalar_type(), *m.x);
+    void *const x = m.x->data_ptr(), *const w = m.weight->data_ptr(), *const to = dx.data_ptr(), *const tw = dw.data_ptr();
+    void *const tb = with_bias ? db.data_ptr() : nullptr, *const scratch = ws.data_ptr(), *const on = stream();
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.norm_bwd(d_out, x, w, static_cast<float*>(stats), d_total, m.dtype, m.wtype, m.T, int32_t(m.hidden), rms, to,
+                            tw, tb, scratch, on);
+    });
+    if (rc != PSA_OK) return PyLong_FromLong(rc);
+    return with_bias ? tuple_of(dx, dw, db) : tuple_of(dx, dw);
+  });
+}
+
+// embed(token_ids, table, scale, status) -> out, a status code (not 0), or None
+PyObject* embed(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    float scale;
+    void* st;
+    int32_t dtype;
+    if (n != 4 || !modes_off() || !take_float(a[2], &scale) || !take_status(a[3], &st)) return none();
+    const at::Tensor *ids = plain(a[0]), *table = plain(a[1]);
+    if (!ids || !table || ids->dim() != 1 || ids->scalar_type() != at::kInt || !ids->is_contiguous() || !here(*ids) ||
+        table->dim() != 2 || !table->is_contiguous() || !here(*table) || !take_dtype(*table, &dtype) ||
+        table->size(1) > INT32_MAX)
+      return none();
+    const int64_t T = ids->size(0), V = table->size(0), D = table->size(1);
+    at::Tensor out = make({T, D}, table->scalar_type(), *table);
+    void *const from = table->data_ptr(), *const to = out.data_ptr(), *const on = stream();
+    const int32_t* const id = static_cast<const int32_t*>(ids->data_ptr());
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.embed(id, from, dtype, T, V, int32_t(D), scale, to, static_cast<int32_t*>(st), on);
+    });
+    return rc == PSA_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+  });
+}
+
+// embed_bwd(d_out, token_ids, vocab, scale, f32, workspace, status) -> dtable (fp32, or d_out's type), a status code
+// (not 0), or None
+PyObject* embed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    float scale;
+    int64_t V;
+    bool f32;
+    void* st;
+    int32_t dtype;
+    at::Tensor ws;
+    if (n != 7 || !modes_off() || !take_int(a[2], &V) || !take_float(a[3], &scale) || !take_bool(a[4], &f32) ||
+        !take_status(a[6], &st))
+      return none();
+    const at::Tensor *d = plain(a[0]), *ids = plain(a[1]);
+    if (!d || d->dim() != 2 || !d->is_contiguous() || !here(*d) || !take_dtype(*d, &dtype) || d->size(1) > INT32_MAX || V <= 0 ||
+        V > INT32_MAX || !ids || ids->dim() != 1 || ids->size(0) != d->size(0) || ids->scalar_type() != at::kInt ||
+        !ids->is_contiguous() || !here(*ids))
+      return none();
+    const int64_t T = d->size(0), D = d->size(1);
+    const size_t bytes = g_lib.embed_bwd_bytes(T, V, int32_t(D));
+    if (bytes == 0 || !take_workspace(a[5], bytes, *d, &ws)) return none();
+    f32 = f32 || dtype == PSA_DTYPE_F32;
+    at::Tensor out = make({V, D}, f32 ? at::kFloat : at::kBFloat16, *d);
+    void *const from = d->data_ptr(), *const to = out.data_ptr(), *const scratch = ws.data_ptr(), *const on = stream();
+    const int32_t* const id = static_cast<const int32_t*>(ids->data_ptr());
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.embed_bwd(from, id, dtype, f32 ? PSA_DTYPE_F32 : PSA_DTYPE_BF16, T, V, int32_t(D), scale, 0, to, scratch,
+                             static_cast<int32_t*>(st), on);
+    });
+    return rc == PSA_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+  });
+}
+
+// x [T, hidden] and the three weights of a feed-forward block.
+struct FfnArgs {
+  const at::Tensor* x;
+  int64_t T, D, F;
+  void *px, *wg, *wu, *wd;
+};
+bool take_ffn(PyObject* x, PyObject* const* w, FfnArgs* f) {
+  const auto b = at::kBFloat16;
+  f->x = plain(x);
+  const at::Tensor* g = plain(w[0]);
+  if (!f->x || !g || f->x->dim() != 2 || g->dim() != 2) return false;
+  f->T = f->x->size(0);
+  f->D = f->x->size(1);
+  f->F = g->size(1);
+  return x != Py_None && take_optional(x, b, {f->T, f->D}, &f->px) && take_optional(w[0], b, {f->D, f->F}, &f->wg) &&
+         w[1] != Py_None && take_optional(w[1], b, {f->D, f->F}, &f->wu) && w[2] != Py_None &&
+         take_optional(w[2], b, {f->F, f->D}, &f->wd) && f->D <= INT32_MAX && f->F <= INT32_MAX;
+}
+
+// ffn(x, w_gate, w_up, w_down, save, workspace, status) -> (out, gate, up) or out, a status code (not 0), or None
+PyObject* ffn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    FfnArgs f;
+    bool save;
+    void* st;
+    at::Tensor ws, gate, up;
+    if (n != 7 || !modes_off() || !take_ffn(a[0], a + 1, &f) || !take_bool(a[4], &save) || !take_status(a[6], &st) ||
+        !take_workspace(a[5], g_lib.ffn_bytes(f.T, int32_t(f.D), int32_t(f.F), 0), *f.x, &ws))
+      return none();
+    at::Tensor out = make({f.T, f.D}, at::kBFloat16, *f.x);
+    if (save) {
+      gate = make({f.T, f.F}, at::kBFloat16, *f.x);
+      up = make({f.T, f.F}, at::kBFloat16, *f.x);
+    }
+    void *const to = out.data_ptr(), *const scratch = ws.data_ptr(), *const on = stream();
+    void *const tg = save ? gate.data_ptr() : nullptr, *const tu = save ? up.data_ptr() : nullptr;
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.ffn(f.px, f.wg, f.wu, f.wd, f.T, int32_t(f.D), int32_t(f.F), to, tg, tu, scratch, static_cast<int32_t*>(st), on);
+    });
+    if (rc != PSA_OK) return PyLong_FromLong(rc);
+    return save ? tuple_of(out, gate, up) : THPVariable_Wrap(out);
+  });
+}
+
+// ffn_bwd(d_out, x, w_gate, w_up, w_down, gate, up, workspace, status) -> (dx, dw_gate, dw_up, dw_down), a status code
+// (not 0), or None
+PyObject* ffn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    FfnArgs f;
+    void *d_out, *gate, *up, *st;
+    at::Tensor ws;
+    const auto b = at::kBFloat16;
+    if (n != 9 || !modes_off() || !take_ffn(a[1], a + 2, &f) || a[0] == Py_None || a[5] == Py_None || a[6] == Py_None ||
+        !take_optional(a[0], b, {f.T, f.D}, &d_out) || !take_optional(a[5], b, {f.T, f.F}, &gate) ||
+        !take_optional(a[6], b, {f.T, f.F}, &up) || !take_status(a[8], &st) ||
+        !take_workspace(a[7], g_lib.ffn_bytes(f.T, int32_t(f.D), int32_t(f.F), 1), *f.x, &ws))
+      return none();
+    at::Tensor dx = make({f.T, f.D}, b, *f.x), dg = make({f.D, f.F}, b, *f.x), du = make({f.D, f.F}, b, *f.x),
+               dd = make({f.F, f.D}, b, *f.x);
+    void *const to = dx.data_ptr(), *const tg = dg.data_ptr(), *const tu = du.data_ptr(), *const td = dd.data_ptr();
+    void *const scratch = ws.data_ptr(), *const on = stream();
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.ffn_bwd(d_out, f.px, f.wg, f.wu, f.wd, gate, up, f.T, int32_t(f.D), int32_t(f.F), to, tg, tu, td, scratch,
+                           static_cast<int32_t*>(st), on);
+    });
+    if (rc != PSA_OK) return PyLong_FromLong(rc);
+    return tuple_of(dx, dg, du, dd);
+  });
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {{"init", init, METH_O, nullptr}, FAST(fwd),  FAST(bwd),  FAST(logp), FAST(logp_bwd),
                            FAST(loss),                      FAST(rope), FAST(plan), {"destroy", destroy, METH_O, nullptr},
+                           FAST(norm), FAST(norm_bwd), FAST(embed), FAST(embed_bwd), FAST(ffn), FAST(ffn_bwd),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "psa_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
