@@ -354,11 +354,27 @@ __device__ __forceinline__ void mbar_wait_cluster(uint32_t bar, uint32_t parity,
     }
   }
 }
-// tma_load_3d into this CTA's shared memory, completing on a barrier of either CTA of the pair (address from cluster_map).
-__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2, uint32_t cluster_bar) {
+// Warp-converged forms of the copies, as of the UMMAs above: all lanes run the loop, so that addresses and coordinates are
+// uniform, and `leader` guards the instruction alone.  (Issued by one lane of a divergent branch, with a tensor map or a
+// coordinate that the compiler does not know to be uniform, a copy costs several times as much.)
+__device__ __forceinline__ void mbar_expect_tx_w(uint32_t bar, uint32_t bytes, uint32_t leader) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}"
+               ::"r"(bar), "r"(bytes), "r"(leader) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_w(uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2, uint32_t bar, uint32_t leader) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
-      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(c0), "r"(c1), "r"(c2), "r"(cluster_bar)
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "r"(leader)
+      : "memory");
+}
+// Into this CTA's shared memory, completing on a barrier of either CTA of the pair (address from cluster_map).
+__device__ __forceinline__ void tma_load_3d_pair_w(uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2, uint32_t cluster_bar,
+                                                   uint32_t leader) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(c0), "r"(c1), "r"(c2), "r"(cluster_bar), "r"(leader)
       : "memory");
 }
 // Both CTAs of the pair allocate, and free, the same columns (a whole warp of each).
@@ -387,6 +403,15 @@ __device__ __forceinline__ void umma_commit_pair_w(uint32_t bar, uint32_t leader
       "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}"
       ::"r"(bar), "r"(leader)
       : "memory");
+}
+
+// Adds eight floats of a CTA of the cluster (address from cluster_map).
+__device__ __forceinline__ void add_cluster8(uint32_t addr, float (&x)[8]) {
+  float v[8];
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr) : "memory");
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(addr + 16u) : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] += v[i];
 }
 
 // Warpgroup register reallocation (all four warps of an aligned warpgroup must execute it).

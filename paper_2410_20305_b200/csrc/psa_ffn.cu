@@ -29,27 +29,86 @@ using namespace dev;
 
 constexpr int kBK = 64;                // K per stage: one 128-byte swizzle row of bf16
 constexpr int kChunk = 64;             // columns of an MN-major sub-tile
+constexpr uint32_t kSub = kChunk * kBK * 2;
 constexpr int kSmCount = 148;
+constexpr int kMaxProducts = 3;
 
 enum Epilogue {
-  kEpiOut,        // C rounded to bf16, or an fp32 partial sum where K is split
-  kEpiGate,       // columns [0, BN/2) are G, [BN/2, BN) are U of the same features
+  kEpiOut,        // C rounded to bf16
+  kEpiGate,       // a tile holds G and U of the same features
   kEpiGateBwd,    // C is dH
 };
 
-struct GemmParams {
+// An operand in memory: rows x cols, cols innermost.  MN-major (cols along M or N): `flat` brings 64 columns of 64 rows,
+// `pair` 128 columns of 64 rows in one copy (two copies of half the size cost 10 % of a large product's time), as long as
+// they lie within the last whole 64 columns.  K-major: `flat` brings 64 columns of 128 rows.
+struct OperandMaps {
+  CUtensorMap flat, pair;
+};
+struct ProductMaps {
+  OperandMaps a[2], b[2];      // two pairs along K, or a second B for a second output (kEpiGate: Wg, Wu)
+  CUtensorMap store[2];        // boxes of 32 rows of the outputs
+};
+struct Product {
+  __nv_bfloat16* out[2];
   int32_t M, N;                // rows and columns of one output
-  int32_t k_tiles;             // stages of one operand pair
-  int32_t k_pairs;             // operand pairs that are summed
-  int32_t n_tiles;             // tiles along N of one output
-  int32_t n_outputs;           // outputs side by side (each with a B of its own)
-  int32_t splits;              // parts of K
-  __nv_bfloat16 *out[2];       // kEpiOut: C;  kEpiGate: G, U (may be null);  kEpiGateBwd: dG, dU
-  __nv_bfloat16 *h;            // kEpiGate, kEpiGateBwd
-  const __nv_bfloat16 *gate, *up;   // kEpiGateBwd
-  float* partial;              // [splits][n_outputs][M][N]
+  int32_t k_tiles, k_pairs;    // stages of one pair of operands; pairs that are summed
+  int32_t m_tiles, n_tiles;    // tiles of one output
+  int32_t n_outputs;           // outputs side by side
+  int32_t first;               // the product's first tile in the launch
+  int32_t a_mn, b_mn;          // which way the operands lie
+};
+struct ProductList {
+  ProductMaps maps[kMaxProducts];
+  Product p[kMaxProducts];
+  CUtensorMap in[2], store_h;  // kEpiGateBwd: G, U;  H
+  const __nv_bfloat16 *gate, *up;
+  __nv_bfloat16* h;
+  int32_t n_products, n_work, splits;
   int32_t* status;
 };
+
+// The 128 rows of A, or columns of B, that a CTA loads for a tile.
+struct Strip {
+  const OperandMaps* m;
+  int mn0, way;         // way: 0 K-major, 1 MN-major in one copy, 2 in two
+  __device__ __forceinline__ Strip(const OperandMaps* maps, bool mn_major, int at, int end)
+      : m(maps), mn0(at), way(mn_major ? (at + 2 * kChunk <= end ? 1 : 2) : 0) {}
+  template <typename Load>
+  __device__ __forceinline__ void load(int which, int k0, uint32_t dst, Load&& load) const {
+    if (way == 2) {
+      load(dst, &m[which].flat, mn0, 0, k0);
+      load(dst + kSub, &m[which].flat, mn0 + kChunk, 0, k0);
+    } else {
+      const bool pair = way == 1;
+      load(dst, pair ? &m[which].pair : &m[which].flat, pair ? 0 : k0, pair ? k0 : 0, pair ? mn0 / kChunk : mn0);
+    }
+  }
+};
+
+// Output tile `tile` of the launch: its product and place.  The products' sizes are looked up in shared memory (`products`,
+// copied there by copy_products): read from the kernel's parameters by a running index they cost a trip to memory each, and
+// between two tiles the loads of the next one wait for them.
+struct Place {
+  int k, m0, n0, sel;
+};
+__device__ __forceinline__ void copy_products(const ProductList& list, Product* products) {
+  constexpr int kWords = sizeof(Product) / 4;
+  if (int(threadIdx.x) < kWords * kMaxProducts)
+    reinterpret_cast<uint32_t*>(products)[threadIdx.x] = reinterpret_cast<const uint32_t*>(list.p)[threadIdx.x];
+}
+// Tiles run down kGroup rows of tiles (0: all) before they move one column on, so that the tiles in flight share strips of A
+// and of B in L2.
+template <int kBM, int kTileN, int kGroup>
+__device__ __forceinline__ Place place_of(const Product* products, int n_products, int tile) {
+  int k = 0;
+  while (k + 1 < n_products && tile >= products[k + 1].first) ++k;
+  const Product& p = products[k];
+  const int m_tiles = p.m_tiles, n_tiles = p.n_tiles, n_all = n_tiles * p.n_outputs, at = tile - p.first;
+  const int per_group = (kGroup ? kGroup : m_tiles) * n_all, group = at / per_group, first = group * kGroup;
+  const int rows = kGroup ? min(kGroup, m_tiles - first) : m_tiles, in = at - group * per_group, n = in / rows;
+  return Place{k, (first + in % rows) * kBM, (n % n_tiles) * kTileN, n / n_tiles};
+}
 
 __device__ __forceinline__ float sigmoid(float g) { return __fdividef(1.0f, 1.0f + __expf(-g)); }
 
@@ -75,18 +134,50 @@ __device__ __forceinline__ void unpack8(const uint4& w, float* v) {
 }
 
 // ---------------------------------------------------------------- one CTA per tile of 128 x 128
+// For launches of few tiles.  Where they are fewer than the SMs can hold, a cluster of 2, 4 or 8 CTAs shares a tile's K: each
+// leaves its sums in its shared memory, and all of them add the parts, in the CTAs' order, and finish a share of the tile.
 // Warps 0-3: end of the tile (TMEM lane = row of the tile), warp 4: TMA, warp 5: UMMA.
 constexpr int kSmallBM = 128, kSmallBN = 128, kSmallStages = 3, kSmallThreads = 192;
 constexpr uint32_t kSmallStageBytes = uint32_t(kSmallBM + kSmallBN) * kBK * 2;
 constexpr uint32_t kSmallSmem = kSmallStages * kSmallStageBytes + 1024 + 256;
+constexpr int kPartPitch = kSmallBN + 4;      // floats per row of a part: rows start four banks apart
+static_assert(kSmallBM * kPartPitch * 4 <= kSmallStages * kSmallStageBytes, "a part takes the place of the stages");
 
-template <bool A_MN, bool B_MN, int EPI>
+// Eight neighbouring elements of a tile: their sums (kEpiGate: x of G, y of U) become outputs.
+template <int EPI>
+__device__ __forceinline__ void finish8(const ProductList& list, const Product& p, int sel, int row, int col, const float* x,
+                                        const float* y, const uint4& gate, const uint4& up) {
+  const int64_t to = int64_t(row) * p.N + col;
+  if (!PSA_IN_BOUNDS(to + 7, int64_t(p.M) * p.N, list.status)) return;
+  if (EPI == kEpiOut) {
+    *reinterpret_cast<uint4*>(p.out[sel] + to) = pack8(x);
+  } else if (EPI == kEpiGate) {
+    float h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = x[i] * sigmoid(x[i]) * y[i];
+    if (p.out[0]) {
+      *reinterpret_cast<uint4*>(p.out[0] + to) = pack8(x);
+      *reinterpret_cast<uint4*>(p.out[1] + to) = pack8(y);
+    }
+    *reinterpret_cast<uint4*>(list.h + to) = pack8(h);
+  } else {
+    float g[8], u[8], h[8];
+    unpack8(gate, g);
+    unpack8(up, u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) gate_bwd(x[i], g[i], u[i], h[i]);
+    *reinterpret_cast<uint4*>(p.out[0] + to) = pack8(g);
+    *reinterpret_cast<uint4*>(p.out[1] + to) = pack8(u);
+    *reinterpret_cast<uint4*>(list.h + to) = pack8(h);
+  }
+}
+
+template <int EPI>
 __global__ void __launch_bounds__(kSmallThreads)
-ffn_small_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1,
-                 const __grid_constant__ CUtensorMap b0, const __grid_constant__ CUtensorMap b1, const GemmParams prm) {
+ffn_small_kernel(const __grid_constant__ ProductList list) {
   constexpr int kBN = kSmallBN, kStages = kSmallStages;
   constexpr int kTileN = EPI == kEpiGate ? kBN / 2 : kBN;      // features per tile
-  constexpr uint32_t kABytes = kSmallBM * kBK * 2, kSub = kChunk * kBK * 2;
+  constexpr uint32_t kABytes = kSmallBM * kBK * 2;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen_base = smem_raw + (base - smem_u32(smem_raw));
@@ -96,14 +187,11 @@ ffn_small_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__
   const uint32_t done = bars + 16u * kStages;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + kStages * kSmallStageBytes + 128);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_base + kStages * kSmallStageBytes + 136);
-  const WaitCtx wctx{abort_flag, prm.status, kWaitLimitClocks};
+  const WaitCtx wctx{abort_flag, list.status, kWaitLimitClocks};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  const int m0 = int(blockIdx.x) * kSmallBM;
-  const int sel = int(blockIdx.y) / prm.n_tiles, n0 = (int(blockIdx.y) % prm.n_tiles) * kTileN;
-  const int total = prm.k_tiles * prm.k_pairs;
-  const int it0 = int(int64_t(total) * blockIdx.z / prm.splits), it1 = int(int64_t(total) * (blockIdx.z + 1) / prm.splits);
-
+  __shared__ Product products[kMaxProducts];
+  copy_products(list, products);
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int s = 0; s < kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
@@ -115,120 +203,126 @@ ffn_small_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  const int splits = list.splits, part = int(blockIdx.x) % splits;
+  const Place at = place_of<kSmallBM, kTileN, 0>(products, list.n_products, int(blockIdx.x) / splits);
+  const Product& p = products[at.k];
+  const int total = p.k_tiles * p.k_pairs;
+  const int it0 = int(int64_t(total) * part / splits), it1 = int(int64_t(total) * (part + 1) / splits);
+  behind_wait();
+  behind_go();
+
+  // Rows of this thread, for the warps that finish a tile from TMEM.
+  const int row = at.m0 + warp * 32 + lane;
+  const uint32_t lanes = tmem + (uint32_t(warp * 32) << 16);
+  auto load_gate = [&](int r, int col, uint4& g, uint4& u) {
+    if (EPI != kEpiGateBwd || r >= p.M || col >= p.N) return;
+    const int64_t from = int64_t(r) * p.N + col;
+    if (!PSA_IN_BOUNDS(from + 7, int64_t(p.M) * p.N, list.status)) return;
+    g = *reinterpret_cast<const uint4*>(list.gate + from);
+    u = *reinterpret_cast<const uint4*>(list.up + from);
+  };
 
   if (warp == 4) {
-    if (lane == 0) {
-      int n = 0;   // stages filled
-      for (int it = it0; it < it1; ++it, ++n) {
-        const int s = n % kStages;
-        if (n >= kStages) mbar_wait(empty(s), (n / kStages - 1) & 1, wctx);
-        if (*abort_flag) break;
-        const bool second = it >= prm.k_tiles;
-        const int k0 = (second ? it - prm.k_tiles : it) * kBK;
-        const CUtensorMap* am = second ? &a1 : &a0;
-        const uint32_t sa = base + s * kSmallStageBytes, sb = sa + kABytes;
-        mbar_expect_tx(full(s), kSmallStageBytes);
-        if (A_MN) {
-          for (int c = 0; c < kSmallBM / kChunk; ++c) tma_load_3d(sa + c * kSub, am, m0 + c * kChunk, 0, k0, full(s));
-        } else {
-          tma_load_3d(sa, am, k0, 0, m0, full(s));
-        }
-        if (EPI == kEpiGate) {   // the same features of two weights
-          tma_load_3d(sb, &b0, n0, 0, k0, full(s));
-          tma_load_3d(sb + kSub, &b1, n0, 0, k0, full(s));
-        } else {
-          const CUtensorMap* bm = second || sel ? &b1 : &b0;
-          if (B_MN) {
-            for (int c = 0; c < kBN / kChunk; ++c) tma_load_3d(sb + c * kSub, bm, n0 + c * kChunk, 0, k0, full(s));
-          } else {
-            tma_load_3d(sb, bm, k0, 0, n0, full(s));
-          }
-        }
+    const uint32_t issuer = elect_one();
+    const ProductMaps& maps = list.maps[at.k];
+    const Strip a(maps.a, p.a_mn, at.m0, p.M), b(maps.b, p.b_mn, at.n0, p.N);
+    const int k_tiles = p.k_tiles, sel = at.sel;
+    int n = 0;   // stages filled
+    for (int it = it0; it < it1; ++it, ++n) {
+      const int s = n % kStages;
+      if (n >= kStages) mbar_wait(empty(s), (n / kStages - 1) & 1, wctx);
+      if (*abort_flag) break;
+      const bool second = it >= k_tiles;
+      const int k0 = (second ? it - k_tiles : it) * kBK;
+      const uint32_t sa = base + s * kSmallStageBytes, sb = sa + kABytes, bar = full(s);
+      auto load = [&](uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2) { tma_load_3d_w(dst, m, c0, c1, c2, bar, issuer); };
+      mbar_expect_tx_w(bar, kSmallStageBytes, issuer);
+      a.load(second, k0, sa, load);
+      if (EPI == kEpiGate) {   // the same features of two weights
+        load(sb, &b.m[0].flat, at.n0, 0, k0);
+        load(sb + kSub, &b.m[1].flat, at.n0, 0, k0);
+      } else {
+        b.load(second || sel, k0, sb, load);
       }
-      if (*abort_flag) {   // shared memory must outlive the copies in flight
-        const long long t0 = clock64();
-        for (int i = n > kStages ? n - kStages : 0; i < n; ++i)
-          while (!mbar_try_wait(full(i % kStages), (i / kStages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
-      }
+    }
+    if (*abort_flag) {   // shared memory must outlive the copies in flight
+      const long long t0 = clock64();
+      for (int i = n > kStages ? n - kStages : 0; i < n; ++i)
+        while (!mbar_try_wait(full(i % kStages), (i / kStages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
     }
     __syncwarp();
   } else if (warp == 5) {
     const uint32_t issuer = elect_one();
-    constexpr uint32_t idesc = umma_idesc_bf16(kSmallBM, kBN, A_MN, B_MN);
+    const bool a_mn = p.a_mn, b_mn = p.b_mn;
+    const uint32_t idesc = umma_idesc_bf16(kSmallBM, kBN, false, false) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16);
+    const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
     for (int it = it0, n = 0; it < it1; ++it, ++n) {
       const int s = n % kStages;
       mbar_wait(full(s), (n / kStages) & 1, wctx);
       tc_fence_after();
       const uint32_t sa = base + s * kSmallStageBytes;
-      const uint32_t a = smem_desc_lo(sa, A_MN ? kSub : 16), b = smem_desc_lo(sa + kABytes, B_MN ? kSub : 16);
+      const uint32_t a = smem_desc_lo(sa, a_mn ? kSub : 16), b = smem_desc_lo(sa + kABytes, b_mn ? kSub : 16);
 #pragma unroll
-      for (int kk = 0; kk < kBK / 16; ++kk)
-        umma_ss_w(tmem, a + kk * ((A_MN ? 2048 : 32) >> 4), b + kk * ((B_MN ? 2048 : 32) >> 4), idesc, n > 0 || kk > 0, issuer);
+      for (int kk = 0; kk < kBK / 16; ++kk) umma_ss_w(tmem, a + kk * a_step, b + kk * b_step, idesc, n > 0 || kk > 0, issuer);
       umma_commit_w(empty(s), issuer);
     }
     umma_commit_w(done, issuer);
     __syncwarp();
   } else {
+    uint4 g[4], u[4];
+    if (splits == 1)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load_gate(row, at.n0 + 8 * j, g[j], u[j]);
     mbar_wait(done, 0, wctx);
     tc_fence_after();
-    const int row = m0 + warp * 32 + lane;
-    const uint32_t lanes = tmem + (uint32_t(warp * 32) << 16);
-    const bool live = row < prm.M && !*abort_flag;
-    uint32_t v[32];
-    if (EPI == kEpiGate) {
-      for (int c = 0; c < kTileN; c += 32) {
-        uint32_t u[32];
-        tmem_ld32_wait(lanes + c, v);
-        tmem_ld32_wait(lanes + kTileN + c, u);
+    const bool live = row < p.M && !*abort_flag;
+#pragma unroll 1
+    for (int c = 0; c < kTileN; c += 32) {
+      uint32_t v[32], w[32];
+      tmem_ld32_wait(lanes + c, v);
+      if (EPI == kEpiGate) tmem_ld32_wait(lanes + kTileN + c, w);
+      const float *x = reinterpret_cast<const float*>(v), *y = reinterpret_cast<const float*>(w);
+      if (splits > 1) {   // (every UMMA that reads the stages has completed)
+        if (it0 == it1)        // a short K leaves some of the CTAs nothing to add
 #pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-          const int col = n0 + c + j;
-          const int64_t at = int64_t(row) * prm.N + col;
-          if (!live || col >= prm.N || !PSA_IN_BOUNDS(at + 7, int64_t(prm.M) * prm.N, prm.status)) continue;
-          float g[8], w[8], h[8];
+          for (int j = 0; j < 32; ++j) v[j] = w[j] = 0u;
+        const uint32_t to = base + uint32_t(warp * 32 + lane) * kPartPitch * 4 + c * 4;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            g[i] = __uint_as_float(v[j + i]);
-            w[i] = __uint_as_float(u[j + i]);
-            h[i] = g[i] * sigmoid(g[i]) * w[i];
-          }
-          if (prm.out[0]) {
-            *reinterpret_cast<uint4*>(prm.out[0] + at) = pack8(g);
-            *reinterpret_cast<uint4*>(prm.out[1] + at) = pack8(w);
-          }
-          *reinterpret_cast<uint4*>(prm.h + at) = pack8(h);
+        for (int j = 0; j < 32; j += 4) {
+          st_shared_v4(to + 4 * j, v[j], v[j + 1], v[j + 2], v[j + 3]);
+          if (EPI == kEpiGate) st_shared_v4(to + 4 * (kTileN + j), w[j], w[j + 1], w[j + 2], w[j + 3]);
         }
+        continue;
       }
-    } else {
-      for (int c = 0; c < kTileN; c += 32) {
-        tmem_ld32_wait(lanes + c, v);
 #pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-          const int col = n0 + c + j;
-          const int64_t at = int64_t(row) * prm.N + col;
-          if (!live || col >= prm.N || !PSA_IN_BOUNDS(at + 7, int64_t(prm.M) * prm.N, prm.status)) continue;
-          float x[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(v[j + i]);
-          if (EPI == kEpiGateBwd) {
-            float g[8], u[8], h[8];
-            unpack8(*reinterpret_cast<const uint4*>(prm.gate + at), g);
-            unpack8(*reinterpret_cast<const uint4*>(prm.up + at), u);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) gate_bwd(x[i], g[i], u[i], h[i]);
-            *reinterpret_cast<uint4*>(prm.out[0] + at) = pack8(g);
-            *reinterpret_cast<uint4*>(prm.out[1] + at) = pack8(u);
-            *reinterpret_cast<uint4*>(prm.h + at) = pack8(h);
-          } else if (prm.splits > 1) {
-            float4* dst = reinterpret_cast<float4*>(prm.partial + (int64_t(blockIdx.z) * prm.n_outputs + sel) * prm.M * prm.N + at);
-            dst[0] = make_float4(x[0], x[1], x[2], x[3]);
-            dst[1] = make_float4(x[4], x[5], x[6], x[7]);
-          } else {
-            *reinterpret_cast<uint4*>((sel ? prm.out[1] : prm.out[0]) + at) = pack8(x);
-          }
-        }
+      for (int j = 0; j < 4; ++j) {
+        const int col = at.n0 + c + 8 * j;
+        const uint4 g0 = g[j], u0 = u[j];
+        if (c + 32 < kTileN) load_gate(row, col + 32, g[j], u[j]);
+        if (live && col < p.N) finish8<EPI>(list, p, at.sel, row, col, x + 8 * j, y + 8 * j, g0, u0);
       }
     }
+  }
+  if (splits > 1) {
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();
+    const int rows = min(kSmallBM, p.M - at.m0), n_eights = rows * (kTileN / 8);
+    for (int i = part * kSmallThreads + int(threadIdx.x); i < n_eights && !*abort_flag; i += splits * kSmallThreads) {
+      const int r = i / (kTileN / 8), c = (i % (kTileN / 8)) * 8, col = at.n0 + c;
+      if (col >= p.N) continue;
+      uint4 g, u;
+      load_gate(at.m0 + r, col, g, u);
+      float x[8] = {}, y[8] = {};
+      for (int s = 0; s < splits; ++s) {
+        const uint32_t from = cluster_map(base + uint32_t(r * kPartPitch + c) * 4, uint32_t(s));
+        add_cluster8(from, x);
+        if (EPI == kEpiGate) add_cluster8(from + kTileN * 4, y);
+      }
+      finish8<EPI>(list, p, at.sel, at.m0 + r, col, x, y, g, u);
+    }
+    cluster_arrive();
+    cluster_wait();     // the other CTAs have read this one's part
   }
   tc_fence_before();
   __syncthreads();
@@ -239,14 +333,14 @@ ffn_small_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__
 }
 
 // ---------------------------------------------------------------- two CTAs per tile of 256 x 256
-// A persistent kernel: 74 clusters of two CTAs take every 74th tile.  A tile's product is one UMMA stream of the pair
-// (M = 256, N = 256): each CTA loads its 128 rows of A and 128 of the tile's 256 columns of B, so a stage brings 32 KB to each
-// SM for the work of which a CTA alone would need 48.  The accumulator takes half of TMEM: while the end of one tile
+// A persistent kernel: 74 clusters of two CTAs take every 74th tile of the launch.  A tile's product is one UMMA stream of the
+// pair (M = 256, N = 256): each CTA loads its 128 rows of A and 128 of the tile's 256 columns of B, so a stage brings 32 KB to
+// each SM for the work of which a CTA alone would need 48.  The accumulator takes half of TMEM: while the end of one tile
 // drains it, the next tile's UMMAs fill the other half.
 // Warps: 0 TMA, 1 UMMA (in the CTA of rank 0), 2 TMEM, 4-7 the end of a tile, each for 32 rows of its CTA.
-// A result leaves by TMA stores of 32 rows x 64 columns, from four buffers that each warp owns: no barrier but the warp's own,
-// and the tensor map clips what lies behind the last row or column.
-constexpr int kBigBM = 256, kBigBN = 256, kBigStages = 5, kBigThreads = 256, kBigBufs = 4;
+// Results leave by TMA stores from buffers that each warp owns: no barrier but the warp's own, and the tensor map clips what
+// lies behind the last row or column.
+constexpr int kBigBM = 256, kBigBN = 256, kBigStages = 5, kBigThreads = 256, kBigBufs = 4, kBigGroup = 16;
 constexpr uint32_t kBigHalf = 128 * kBK * 2;                       // one operand's half of a stage
 constexpr uint32_t kBigStageBytes = 2 * kBigHalf;
 constexpr uint32_t kBufBytes = 32 * 64 * 2;
@@ -254,16 +348,16 @@ constexpr uint32_t kBigBufsAt = kBigStages * kBigStageBytes;
 constexpr uint32_t kBigBarsAt = kBigBufsAt + 4 * kBigBufs * kBufBytes;
 constexpr uint32_t kBigSmem = kBigBarsAt + 256 + 1024;
 static_assert(kBigSmem <= 227 * 1024, "shared memory of one CTA");
+// kEpiGateBwd: boxes of 32 rows x 32 columns.  G and U arrive in three sets of two buffers, up to two boxes ahead, and leave
+// from them as dG and dU; H leaves from two buffers of its own.
+constexpr uint32_t kBoxBytes = 32 * 32 * 2;
+constexpr int kBoxSets = 3, kBoxesPerTile = kBigBN / 32;
+static_assert((2 * kBoxSets + 2) * kBoxBytes <= kBigBufs * kBufBytes, "a warp's buffers");
 
-struct BigMaps {
-  CUtensorMap a[2], b[2], out[3], in[2];    // out: C of both outputs, or G / dG, U / dU, H;  in: G, U
-};
-
-template <bool A_MN, bool B_MN, int EPI>
+template <int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kBigThreads, 1)
-ffn_big_kernel(const __grid_constant__ BigMaps maps, const GemmParams prm) {
+ffn_big_kernel(const __grid_constant__ ProductList list) {
   constexpr int kTileN = EPI == kEpiGate ? kBigBN / 2 : kBigBN;
-  constexpr uint32_t kSub = kChunk * kBK * 2;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen_base = smem_raw + (base - smem_u32(smem_raw));
@@ -272,34 +366,25 @@ ffn_big_kernel(const __grid_constant__ BigMaps maps, const GemmParams prm) {
   auto empty = [&](int s) { return bars + 8u * (kBigStages + s); };
   auto acc_full = [&](int i) { return bars + 8u * (2 * kBigStages + i); };
   auto acc_empty = [&](int i) { return bars + 8u * (2 * kBigStages + 2 + i); };   // of rank 0: both CTAs' warps
-  auto in_full = [&](int w) { return bars + 8u * (2 * kBigStages + 4 + w); };
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + kBigBarsAt + 192);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_base + kBigBarsAt + 200);
-  const WaitCtx wctx{abort_flag, prm.status, kWaitLimitClocks};
+  auto in_full = [&](int w, int set) { return bars + 8u * (2 * kBigStages + 4 + kBoxSets * w + set); };
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + kBigBarsAt + 240);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_base + kBigBarsAt + 248);
+  static_assert(8 * (2 * kBigStages + 4 + 4 * kBoxSets) <= 240, "barriers");
+  const WaitCtx wctx{abort_flag, list.status, kWaitLimitClocks};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
-  const int cluster = int(blockIdx.x) >> 1, n_clusters = int(gridDim.x) >> 1;
-
-  const int m_tiles = (prm.M + kBigBM - 1) / kBigBM, n_all = prm.n_tiles * prm.n_outputs, n_work = m_tiles * n_all;
-  const int total = prm.k_tiles * prm.k_pairs;
-  // Tiles run down kGroup rows of tiles before they move one column on: the 74 tiles in flight share kGroup strips of A
-  // and about 74 / kGroup of B, which stay in L2.
-  constexpr int kGroup = 8;
-  struct Place { int m0, n0, sel; };
-  auto place = [&](int tile) {
-    const int per_group = kGroup * n_all, group = tile / per_group, first = group * kGroup;
-    const int rows = min(kGroup, m_tiles - first), in = tile - group * per_group;
-    const int n = in / rows;
-    return Place{(first + in % rows) * kBigBM, (n % prm.n_tiles) * kTileN, n / prm.n_tiles};
-  };
+  const int cluster = int(blockIdx.x) >> 1, n_clusters = int(gridDim.x) >> 1, n_work = list.n_work;
+  __shared__ Product products[kMaxProducts];
+  copy_products(list, products);
+  auto place = [&](int tile) { return place_of<kBigBM, kTileN, kBigGroup>(products, list.n_products, tile); };
 
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int s = 0; s < kBigStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(acc_full(i), 1); mbar_init(acc_empty(i), 8); }
-    for (int w = 0; w < 4; ++w) mbar_init(in_full(w), 1);
+    for (int w = 0; w < 4; ++w)
+      for (int s = 0; s < kBoxSets; ++s) mbar_init(in_full(w, s), 1);
     fence_mbar_init();
-    for (int i = 0; i < 2; ++i) { tma_prefetch_desc(&maps.a[i]); tma_prefetch_desc(&maps.b[i]); }
   }
   if (warp == 2) tmem_alloc_pair(smem_u32(const_cast<uint32_t*>(tmem_slot)), 512);
   tc_fence_before();
@@ -308,54 +393,50 @@ ffn_big_kernel(const __grid_constant__ BigMaps maps, const GemmParams prm) {
   cluster_wait();     // the other CTA's barriers are there
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  behind_wait();
+  behind_go();
 
   if (warp == 0) {
-    if (lane == 0) {
-      int n = 0;
-      for (int tile = cluster; tile < n_work && !*abort_flag; tile += n_clusters) {
-        const Place at = place(tile);
-        const int m0 = at.m0 + 128 * int(rank);
-        for (int it = 0; it < total; ++it, ++n) {
-          const int s = n % kBigStages;
-          if (n >= kBigStages) mbar_wait(empty(s), (n / kBigStages - 1) & 1, wctx);
-          if (*abort_flag) break;
-          const bool second = it >= prm.k_tiles;
-          const int k0 = (second ? it - prm.k_tiles : it) * kBK;
-          const uint32_t sa = base + s * kBigStageBytes, sb = sa + kBigHalf, bar = cluster_map(full(s), 0);
-          const CUtensorMap* am = &maps.a[second];
-          if (rank == 0) mbar_expect_tx(full(s), 2 * kBigStageBytes);
-          if (A_MN) {
-            tma_load_3d_pair(sa, am, m0, 0, k0, bar);
-            tma_load_3d_pair(sa + kSub, am, m0 + kChunk, 0, k0, bar);
-          } else {
-            tma_load_3d_pair(sa, am, k0, 0, m0, bar);
-          }
-          // Gate: rank 0 loads the tile's features of Wg, rank 1 the same features of Wu.
-          const CUtensorMap* bm = &maps.b[EPI == kEpiGate ? int(rank) : (second || at.sel)];
-          const int n0 = EPI == kEpiGate ? at.n0 : at.n0 + 128 * int(rank);
-          if (B_MN) {
-            tma_load_3d_pair(sb, bm, n0, 0, k0, bar);
-            tma_load_3d_pair(sb + kSub, bm, n0 + kChunk, 0, k0, bar);
-          } else {
-            tma_load_3d_pair(sb, bm, k0, 0, n0, bar);
-          }
-        }
+    const uint32_t issuer = elect_one();
+    int n = 0;
+    for (int tile = cluster; tile < n_work && !*abort_flag; tile += n_clusters) {
+      const Place at = place(tile);
+      const Product& p = products[at.k];
+      const ProductMaps& maps = list.maps[at.k];
+      // kEpiGate: rank 0 loads the tile's features of Wg, rank 1 the same features of Wu.
+      const Strip a(maps.a, p.a_mn, at.m0 + 128 * int(rank), p.M), b(maps.b, p.b_mn, EPI == kEpiGate ? at.n0 : at.n0 + 128 * int(rank), p.N);
+      const int k_tiles = p.k_tiles, total = k_tiles * p.k_pairs, sel = EPI == kEpiGate ? int(rank) : at.sel;
+      for (int it = 0; it < total; ++it, ++n) {
+        const int s = n % kBigStages;
+        if (n >= kBigStages) mbar_wait(empty(s), (n / kBigStages - 1) & 1, wctx);
+        if (*abort_flag) break;
+        const bool second = it >= k_tiles;
+        const int k0 = (second ? it - k_tiles : it) * kBK;
+        const uint32_t sa = base + s * kBigStageBytes, bar = cluster_map(full(s), 0);
+        auto load = [&](uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2) { tma_load_3d_pair_w(dst, m, c0, c1, c2, bar, issuer); };
+        mbar_expect_tx_w(full(s), 2 * kBigStageBytes, rank == 0 ? issuer : 0u);
+        a.load(second, k0, sa, load);
+        b.load(second || sel, k0, sa + kBigHalf, load);
       }
-      if (*abort_flag) {   // shared memory must outlive the copies in flight (the cluster's last barrier holds the other CTA)
-        const long long t0 = clock64();
-        if (rank == 0)
-          for (int i = n > kBigStages ? n - kBigStages : 0; i < n; ++i)
-            while (!mbar_try_wait(full(i % kBigStages), (i / kBigStages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
-        while (clock64() - t0 < 1000000) {}
-      }
+    }
+    if (*abort_flag) {   // shared memory must outlive the copies in flight (the cluster's last barrier holds the other CTA)
+      const long long t0 = clock64();
+      if (rank == 0)
+        for (int i = n > kBigStages ? n - kBigStages : 0; i < n; ++i)
+          while (!mbar_try_wait(full(i % kBigStages), (i / kBigStages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
+      while (clock64() - t0 < 1000000) {}
     }
     __syncwarp();
   } else if (warp == 1) {
     if (rank == 0) {
       const uint32_t issuer = elect_one();
-      constexpr uint32_t idesc = umma_idesc_bf16(kBigBM, kBigBN, A_MN, B_MN);
       int n = 0, i = 0;
       for (int tile = cluster; tile < n_work && !*abort_flag; tile += n_clusters, ++i) {
+        const Product& p = products[place(tile).k];
+        const bool a_mn = p.a_mn, b_mn = p.b_mn;
+        const uint32_t idesc = umma_idesc_bf16(kBigBM, kBigBN, false, false) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16);
+        const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
+        const int total = p.k_tiles * p.k_pairs;
         const uint32_t acc = tmem + uint32_t(i & 1) * 256;
         mbar_wait_cluster(acc_empty(i & 1), ((i >> 1) & 1) ^ 1, wctx);
         tc_fence_after();
@@ -365,10 +446,10 @@ ffn_big_kernel(const __grid_constant__ BigMaps maps, const GemmParams prm) {
           if (*abort_flag) break;
           tc_fence_after();
           const uint32_t sa = base + s * kBigStageBytes;
-          const uint32_t a = smem_desc_lo(sa, A_MN ? kSub : 16), b = smem_desc_lo(sa + kBigHalf, B_MN ? kSub : 16);
+          const uint32_t a = smem_desc_lo(sa, a_mn ? kSub : 16), b = smem_desc_lo(sa + kBigHalf, b_mn ? kSub : 16);
 #pragma unroll
           for (int kk = 0; kk < kBK / 16; ++kk)
-            umma_ss_pair_w(acc, a + kk * ((A_MN ? 2048 : 32) >> 4), b + kk * ((B_MN ? 2048 : 32) >> 4), idesc, it > 0 || kk > 0, issuer);
+            umma_ss_pair_w(acc, a + kk * a_step, b + kk * b_step, idesc, it > 0 || kk > 0, issuer);
           umma_commit_pair_w(empty(s), issuer);
         }
         umma_commit_pair_w(acc_full(i & 1), issuer);
@@ -378,153 +459,164 @@ ffn_big_kernel(const __grid_constant__ BigMaps maps, const GemmParams prm) {
   } else if (warp >= 4) {
     const int w = warp - 4;
     const uint32_t bufs = base + kBigBufsAt + uint32_t(w) * kBigBufs * kBufBytes;
-    auto buf = [&](uint32_t use) { return bufs + (use % kBigBufs) * kBufBytes; };
-    // 16 bytes (8 columns) of this thread's row in a buffer, in the 128-byte-swizzled layout of the tensor maps
-    auto cell = [&](uint32_t b, int eight) { return b + uint32_t(lane) * 128 + ((uint32_t(eight) ^ uint32_t(lane & 7)) << 4); };
-    uint32_t use = 0;      // buffers used so far; each is one group of stores
-    int i = 0, n_in = 0;   // n_in: loads of G and U requested so far
-    for (int tile = cluster; tile < n_work && !*abort_flag; tile += n_clusters, ++i) {
-      const Place at = place(tile);
-      const int row0 = at.m0 + 128 * int(rank) + 32 * w;
-      const uint32_t lanes = tmem + uint32_t(i & 1) * 256 + (uint32_t(w * 32) << 16);
-      auto store = [&](const CUtensorMap* m, uint32_t b, int col) {    // by one lane, after the warp's writes
-        if (row0 < prm.M && col < prm.N) tma_store_3d(m, b, col, 0, row0);
-        tma_commit_group();
-      };
-      if (EPI != kEpiGateBwd) {
+    auto drained = [&](int i) {      // this warp has read the accumulator
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(cluster_map(acc_empty(i & 1), 0));
+    };
+    if (EPI != kEpiGateBwd) {
+      auto buf = [&](uint32_t use) { return bufs + (use % kBigBufs) * kBufBytes; };
+      // 16 bytes (8 columns) of this thread's row in a buffer, in the 128-byte-swizzled layout of the tensor maps
+      auto cell = [&](uint32_t b, int eight) { return b + uint32_t(lane) * 128 + ((uint32_t(eight) ^ uint32_t(lane & 7)) << 4); };
+      uint32_t use = 0;      // buffers used so far; each is one group of stores
+      int i = 0;
+      for (int tile = cluster; tile < n_work && !*abort_flag; tile += n_clusters, ++i) {
+        const Place at = place(tile);
+        const Product& p = products[at.k];
+        const ProductMaps& maps = list.maps[at.k];
+        const int row0 = at.m0 + 128 * int(rank) + 32 * w;
+        const uint32_t lanes = tmem + uint32_t(i & 1) * 256 + (uint32_t(w * 32) << 16);
+        auto store = [&](const CUtensorMap* m, uint32_t b, int col) {    // by one lane, after the warp's writes
+          if (row0 < p.M && col < p.N) tma_store_3d(m, b, col, 0, row0);
+          tma_commit_group();
+        };
         mbar_wait(acc_full(i & 1), (i >> 1) & 1, wctx);
         tc_fence_after();
         if (*abort_flag) break;
-      }
-      if (EPI == kEpiOut) {
+        if (EPI == kEpiOut) {
 #pragma unroll 1
-        for (int c = 0; c < kBigBN / 64; ++c, ++use) {
-          uint32_t v[64];
-          tmem_ld64_wait(lanes + c * 64, v);
-          if (c == kBigBN / 64 - 1) {      // the accumulator is read
-            tc_fence_before();
+          for (int c = 0; c < kBigBN / 64; ++c, ++use) {
+            uint32_t v[64];
+            tmem_ld64_wait(lanes + c * 64, v);
+            if (c == kBigBN / 64 - 1) drained(i);
+            if (lane == 0) tma_wait_group_read<kBigBufs - 1>();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(cluster_map(acc_empty(i & 1), 0));
-          }
-          if (lane == 0) tma_wait_group_read<kBigBufs - 1>();
-          __syncwarp();
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float* x = reinterpret_cast<const float*>(v) + 8 * j;
-            const uint4 p = pack8(x);
-            st_shared_v4(cell(buf(use), j), p.x, p.y, p.z, p.w);
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) store(&maps.out[at.sel], buf(use), at.n0 + c * 64);
-        }
-      } else if (EPI == kEpiGate) {
-        const bool keep = prm.out[0] != nullptr;
-        const int n_bufs = keep ? 3 : 1;
-#pragma unroll 1
-        for (int c = 0; c < kTileN / 64; ++c, use += n_bufs) {
-          if (lane == 0) {
-            if (keep) tma_wait_group_read<kBigBufs - 3>(); else tma_wait_group_read<kBigBufs - 1>();
-          }
-          __syncwarp();
-#pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            uint32_t g[32], u[32];
-            tmem_ld32_wait(lanes + c * 64 + half * 32, g);
-            tmem_ld32_wait(lanes + kTileN + c * 64 + half * 32, u);
-            if (c == kTileN / 64 - 1 && half) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive_cluster(cluster_map(acc_empty(i & 1), 0));
+            for (int j = 0; j < 8; ++j) {
+              const uint4 q = pack8(reinterpret_cast<const float*>(v) + 8 * j);
+              st_shared_v4(cell(buf(use), j), q.x, q.y, q.z, q.w);
             }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) store(&maps.store[at.sel], buf(use), at.n0 + c * 64);
+          }
+        } else {
+          const bool keep = p.out[0] != nullptr;
+          const int n_bufs = keep ? 3 : 1;
+#pragma unroll 1
+          for (int c = 0; c < kTileN / 64; ++c, use += n_bufs) {
+            if (lane == 0) {
+              if (keep) tma_wait_group_read<kBigBufs - 3>(); else tma_wait_group_read<kBigBufs - 1>();
+            }
+            __syncwarp();
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+              uint32_t g[32], u[32];
+              tmem_ld32_wait(lanes + c * 64 + half * 32, g);
+              tmem_ld32_wait(lanes + kTileN + c * 64 + half * 32, u);
+              if (c == kTileN / 64 - 1 && half) drained(i);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float *gf = reinterpret_cast<const float*>(g) + 8 * j, *uf = reinterpret_cast<const float*>(u) + 8 * j;
-              float h[8];
+              for (int j = 0; j < 4; ++j) {
+                const float *gf = reinterpret_cast<const float*>(g) + 8 * j, *uf = reinterpret_cast<const float*>(u) + 8 * j;
+                float h[8];
 #pragma unroll
-              for (int k = 0; k < 8; ++k) h[k] = gf[k] * sigmoid(gf[k]) * uf[k];
-              const int at8 = half * 4 + j;
-              uint4 p = pack8(h);
-              st_shared_v4(cell(buf(use), at8), p.x, p.y, p.z, p.w);
+                for (int k = 0; k < 8; ++k) h[k] = gf[k] * sigmoid(gf[k]) * uf[k];
+                const int at8 = half * 4 + j;
+                uint4 q = pack8(h);
+                st_shared_v4(cell(buf(use), at8), q.x, q.y, q.z, q.w);
+                if (keep) {
+                  q = pack8(gf);
+                  st_shared_v4(cell(buf(use + 1), at8), q.x, q.y, q.z, q.w);
+                  q = pack8(uf);
+                  st_shared_v4(cell(buf(use + 2), at8), q.x, q.y, q.z, q.w);
+                }
+              }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              store(&list.store_h, buf(use), at.n0 + c * 64);
               if (keep) {
-                p = pack8(gf);
-                st_shared_v4(cell(buf(use + 1), at8), p.x, p.y, p.z, p.w);
-                p = pack8(uf);
-                st_shared_v4(cell(buf(use + 2), at8), p.x, p.y, p.z, p.w);
+                store(&maps.store[0], buf(use + 1), at.n0 + c * 64);
+                store(&maps.store[1], buf(use + 2), at.n0 + c * 64);
               }
             }
           }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            store(&maps.out[2], buf(use), at.n0 + c * 64);
-            if (keep) {
-              store(&maps.out[0], buf(use + 1), at.n0 + c * 64);
-              store(&maps.out[1], buf(use + 2), at.n0 + c * 64);
-            }
-          }
-        }
-      } else {
-        // G and U of the tile arrive in two buffers, and leave from them as dG and dU.
-#pragma unroll 1
-        for (int c = 0; c < kBigBN / 64; ++c, use += 3) {
-          if (lane == 0) {
-            tma_wait_group_read<kBigBufs - 3>();
-            mbar_expect_tx(in_full(w), 2 * kBufBytes);
-            tma_load_3d(buf(use), &maps.in[0], at.n0 + c * 64, 0, row0, in_full(w));
-            tma_load_3d(buf(use + 1), &maps.in[1], at.n0 + c * 64, 0, row0, in_full(w));
-          }
-          if (c == 0) {
-            mbar_wait(acc_full(i & 1), (i >> 1) & 1, wctx);
-            tc_fence_after();
-          }
-          mbar_wait(in_full(w), n_in & 1, wctx);
-          ++n_in;
-          __syncwarp();
-#pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            uint32_t v[32];
-            tmem_ld32_wait(lanes + c * 64 + half * 32, v);
-            if (c == kBigBN / 64 - 1 && half) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive_cluster(cluster_map(acc_empty(i & 1), 0));
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float* x = reinterpret_cast<const float*>(v) + 8 * j;
-              const int at8 = half * 4 + j;
-              float g[8], u[8], h[8];
-              unpack8(ld_shared_v4(cell(buf(use), at8)), g);
-              unpack8(ld_shared_v4(cell(buf(use + 1), at8)), u);
-#pragma unroll
-              for (int k = 0; k < 8; ++k) gate_bwd(x[k], g[k], u[k], h[k]);
-              uint4 p = pack8(g);
-              st_shared_v4(cell(buf(use), at8), p.x, p.y, p.z, p.w);
-              p = pack8(u);
-              st_shared_v4(cell(buf(use + 1), at8), p.x, p.y, p.z, p.w);
-              p = pack8(h);
-              st_shared_v4(cell(buf(use + 2), at8), p.x, p.y, p.z, p.w);
-            }
-          }
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (*abort_flag) break;
-          if (lane == 0) {
-            store(&maps.out[0], buf(use), at.n0 + c * 64);
-            store(&maps.out[1], buf(use + 1), at.n0 + c * 64);
-            store(&maps.out[2], buf(use + 2), at.n0 + c * 64);
-          }
         }
       }
-    }
-    if (lane == 0) {
-      if (EPI == kEpiGateBwd && *abort_flag && n_in > 0) {   // loads of G and U in flight
+    } else {
+      // Box q of the warp: box q % 8 of its (q / 8)-th tile.
+      const int n_tiles = cluster < n_work ? (n_work - cluster + n_clusters - 1) / n_clusters : 0, n_boxes = n_tiles * kBoxesPerTile;
+      const int M = products[0].M, N = products[0].N, row_of = 128 * int(rank) + 32 * w;
+      const ProductMaps& maps = list.maps[0];
+      auto set_buf = [&](int q, int k) { return bufs + uint32_t(2 * (q % kBoxSets) + k) * kBoxBytes; };
+      auto h_buf = [&](int q) { return bufs + uint32_t(2 * kBoxSets + (q & 1)) * kBoxBytes; };
+      // as above, 64-byte-swizzled
+      auto cell = [&](uint32_t b, int eight) { return b + uint32_t(lane) * 64 + ((uint32_t(eight) ^ uint32_t((lane >> 1) & 3)) << 4); };
+      int asked = 0;
+      Place ahead{};
+      auto ask = [&]() {     // one lane requests G and U of the next box
+        if (asked >= n_boxes) return;
+        const int c = asked % kBoxesPerTile;
+        if (c == 0) ahead = place(cluster + asked / kBoxesPerTile * n_clusters);
+        const uint32_t bar = in_full(w, asked % kBoxSets);
+        mbar_expect_tx(bar, 2 * kBoxBytes);
+        tma_load_3d(set_buf(asked, 0), &list.in[0], ahead.n0 + c * 32, 0, ahead.m0 + row_of, bar);
+        tma_load_3d(set_buf(asked, 1), &list.in[1], ahead.n0 + c * 32, 0, ahead.m0 + row_of, bar);
+        ++asked;
+      };
+      if (lane == 0) { ask(); ask(); }
+      Place at{};
+#pragma unroll 1
+      for (int q = 0; q < n_boxes && !*abort_flag; ++q) {
+        const int i = q / kBoxesPerTile, c = q % kBoxesPerTile;
+        if (c == 0) {
+          at = place(cluster + i * n_clusters);
+          mbar_wait(acc_full(i & 1), (i >> 1) & 1, wctx);
+          tc_fence_after();
+        }
+        mbar_wait(in_full(w, q % kBoxSets), (q / kBoxSets) & 1, wctx);
+        __syncwarp();
+        if (*abort_flag) break;
+        uint32_t v[32];
+        tmem_ld32_wait(tmem + uint32_t(i & 1) * 256 + (uint32_t(w * 32) << 16) + c * 32, v);
+        if (c == kBoxesPerTile - 1) drained(i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float* x = reinterpret_cast<const float*>(v) + 8 * j;
+          float g[8], u[8], h[8];
+          unpack8(ld_shared_v4(cell(set_buf(q, 0), j)), g);
+          unpack8(ld_shared_v4(cell(set_buf(q, 1), j)), u);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) gate_bwd(x[k], g[k], u[k], h[k]);
+          uint4 o = pack8(g);
+          st_shared_v4(cell(set_buf(q, 0), j), o.x, o.y, o.z, o.w);
+          o = pack8(u);
+          st_shared_v4(cell(set_buf(q, 1), j), o.x, o.y, o.z, o.w);
+          o = pack8(h);
+          st_shared_v4(cell(h_buf(q), j), o.x, o.y, o.z, o.w);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          const int row = at.m0 + row_of, col = at.n0 + c * 32;
+          if (row < M && col < N) {
+            tma_store_3d(&maps.store[0], set_buf(q, 0), col, 0, row);
+            tma_store_3d(&maps.store[1], set_buf(q, 1), col, 0, row);
+            tma_store_3d(&list.store_h, h_buf(q), col, 0, row);
+          }
+          tma_commit_group();
+          tma_wait_group_read<1>();    // the set of the box before this one is free for the box after the next
+          ask();
+        }
+      }
+      if (lane == 0 && *abort_flag) {   // loads of G and U in flight
         const long long t0 = clock64();
-        while (!mbar_try_wait(in_full(w), (n_in - 1) & 1) && clock64() - t0 < kWaitLimitClocks) {}
+        for (int q = asked > kBoxSets ? asked - kBoxSets : 0; q < asked; ++q)
+          while (!mbar_try_wait(in_full(w, q % kBoxSets), (q / kBoxSets) & 1) && clock64() - t0 < kWaitLimitClocks) {}
       }
-      tma_wait_group_read<0>();   // shared memory must outlive the stores' reads
     }
+    if (lane == 0) tma_wait_group_read<0>();   // shared memory must outlive the stores' reads
     __syncwarp();
   }
   tc_fence_before();
@@ -537,134 +629,123 @@ ffn_big_kernel(const __grid_constant__ BigMaps maps, const GemmParams prm) {
   }
 }
 
-// The parts of K summed in their order and rounded once.  blockIdx.y: output.
-__global__ void __launch_bounds__(256)
-ffn_sum_kernel(const float* partial, __nv_bfloat16* out0, __nv_bfloat16* out1, int64_t n, int32_t splits) {
-  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8;
-  if (i >= n) return;
-  const float* p = partial + int64_t(blockIdx.y) * n + i;
-  const int64_t step = int64_t(gridDim.y) * n;
-  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const float4 a = *reinterpret_cast<const float4*>(p + s * step), b = *reinterpret_cast<const float4*>(p + s * step + 4);
-    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-    v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
-  }
-  *reinterpret_cast<uint4*>((blockIdx.y ? out1 : out0) + i) = pack8(v);
-}
-
 // ---------------------------------------------------------------- host
-// A row-major matrix, `rows` x `cols`, read in boxes of `box_rows` x 64.
-bool matrix_map(CUtensorMap* m, const void* p, int64_t rows, int64_t cols, int box_rows) {
-  return make_tile_map(m, p, rows, 1, int(cols), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, kBK, box_rows);
+bool encode(CUtensorMap* m, const void* p, cuuint64_t d0, cuuint64_t d1, cuuint64_t d2, cuuint64_t s1, cuuint64_t s2, cuuint32_t b0,
+            cuuint32_t b1, cuuint32_t b2, CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  const cuuint64_t dims[3] = {d0, d1, d2}, strides[2] = {s1, s2};
+  const cuuint32_t box[3] = {b0, b1, b2}, step[3] = {1, 1, 1};
+  return fn && fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Boxes of `box_rows` x `box_cols` of a row-major matrix; coordinates (column, 0, row).
+bool matrix_map(CUtensorMap* m, const void* p, int64_t rows, int64_t cols, int box_rows, int box_cols = kBK) {
+  return encode(m, p, cols, 1, rows, cols * 2, cols * 2, box_cols, 1, box_rows,
+                box_cols == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// Boxes of two times 64 columns of 64 rows, the second behind the first; coordinates (0, row, column / 64).
+bool pair_map(CUtensorMap* m, const void* p, int64_t rows, int64_t cols) {
+  return encode(m, p, kChunk, rows, cols / kChunk, cols * 2, kChunk * 2, kChunk, kBK, 2, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+bool operand_maps(OperandMaps* o, const void* p, bool mn_major, int64_t mn, int64_t k) {
+  if (!mn_major) return matrix_map(&o->flat, p, mn, k, 128);
+  return matrix_map(&o->flat, p, k, mn, kBK) && (mn < 2 * kChunk || pair_map(&o->pair, p, k, mn));
 }
 
-// One product: operands as they lie in memory.
-struct Product {
+struct Matrix {
+  const void* p;
+  bool mn_major;
+};
+// C[M, N] = sum of A B over K, for up to two pairs of operands or two outputs.
+struct Wanted {
   int64_t M, N, K;
-  const void *a[2] = {nullptr, nullptr}, *b[2] = {nullptr, nullptr};
-  int k_pairs = 1, n_outputs = 1;
+  Matrix a[2], b[2];
+  __nv_bfloat16* out[2];
+  int k_pairs, n_outputs;
 };
 
-bool takes_big(int64_t M, int64_t N, int n_outputs);
-
-int split_count(int64_t M, int64_t N, int64_t K, int k_pairs, int n_outputs) {
-  const int64_t tiles = ((M + kSmallBM - 1) / kSmallBM) * ((N + kSmallBN - 1) / kSmallBN) * n_outputs;
-  if (tiles == 0) return 1;
-  const int64_t its = (K + kBK - 1) / kBK * k_pairs;
-  return int(std::max<int64_t>(1, std::min<int64_t>(2 * kSmCount / tiles, its / 8)));
+int64_t tiles_of(const Wanted& w, int edge_m, int edge_n) {
+  return (w.M + edge_m - 1) / edge_m * ((w.N + edge_n - 1) / edge_n) * w.n_outputs;
 }
+int64_t stages_of(const Wanted& w) { return (w.K + kBK - 1) / kBK * w.k_pairs; }
 
-int64_t partial_bytes(int64_t M, int64_t N, int64_t K, int k_pairs, int n_outputs) {
-  if (takes_big(M, N, n_outputs)) return 0;
-  const int s = split_count(M, N, K, k_pairs, n_outputs);
-  return s > 1 ? 4 * M * N * n_outputs * s : 0;
-}
-
-bool takes_big(int64_t M, int64_t N, int n_outputs) {
-  return ((M + kBigBM - 1) / kBigBM) * ((N + kBigBN - 1) / kBigBN) * n_outputs >= kSmCount / 2;
-}
-
-template <bool A_MN, bool B_MN, int EPI>
-psa_status_t launch_big(const Product& p, GemmParams prm, cudaStream_t stream) {
-  constexpr int kTileN = EPI == kEpiGate ? kBigBN / 2 : kBigBN;
-  BigMaps maps;
-  bool ok = true;
-  for (int i = 0; i < 2; ++i) {
-    const void *pa = p.a[i] ? p.a[i] : p.a[0], *pb = p.b[i] ? p.b[i] : p.b[0];
-    ok = ok && (A_MN ? matrix_map(&maps.a[i], pa, p.K, p.M, kBK) : matrix_map(&maps.a[i], pa, p.M, p.K, 128));
-    ok = ok && (B_MN ? matrix_map(&maps.b[i], pb, p.K, p.N, kBK) : matrix_map(&maps.b[i], pb, p.N, p.K, 128));
-    const void *out = prm.out[i] ? prm.out[i] : prm.out[0], *in = i ? prm.up : prm.gate;
-    ok = ok && matrix_map(&maps.out[i], out ? out : prm.h, p.M, p.N, 32);
-    maps.in[i] = maps.a[i];
-    if (EPI == kEpiGateBwd) ok = ok && matrix_map(&maps.in[i], in, p.M, p.N, 32);
-  }
-  ok = ok && matrix_map(&maps.out[2], prm.h ? prm.h : prm.out[0], p.M, p.N, 32);
-  if (!ok) return PSA_ERR_CUDA;
-  prm.M = int32_t(p.M);
-  prm.N = int32_t(p.N);
-  prm.k_tiles = int32_t((p.K + kBK - 1) / kBK);
-  prm.k_pairs = p.k_pairs;
-  prm.n_tiles = int32_t((p.N + kTileN - 1) / kTileN);
-  prm.n_outputs = p.n_outputs;
-  prm.splits = 1;
-  auto kernel = ffn_big_kernel<A_MN, B_MN, EPI>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem) != cudaSuccess) return PSA_ERR_CUDA;
-  const int64_t tiles = (p.M + kBigBM - 1) / kBigBM * prm.n_tiles * p.n_outputs;
-  const unsigned grid = unsigned(2 * std::min<int64_t>(tiles, kSmCount / 2));
-  kernel<<<grid, kBigThreads, kBigSmem, stream>>>(maps, prm);
+template <typename Kernel>
+psa_status_t launch(Kernel kernel, int64_t grid, unsigned threads, uint32_t smem, int cluster, cudaStream_t stream, const ProductList& list) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return PSA_ERR_CUDA;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(grid));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {unsigned(cluster), 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster ? 2 : 1;
+  cudaLaunchKernelEx(&cfg, kernel, list);
   return check_last_cuda_error("psa_ffn launch");
 }
 
-template <bool A_MN, bool B_MN, int EPI>
-psa_status_t launch_product(const Product& p, GemmParams prm, cudaStream_t stream) {
-  if (takes_big(p.M, EPI == kEpiGate ? 2 * p.N : p.N, p.n_outputs)) return launch_big<A_MN, B_MN, EPI>(p, prm, stream);
-  constexpr int kTileN = EPI == kEpiGate ? kSmallBN / 2 : kSmallBN;
-  CUtensorMap a[2], b[2];
-  for (int i = 0; i < 2; ++i) {
-    const void *pa = p.a[i] ? p.a[i] : p.a[0], *pb = p.b[i] ? p.b[i] : p.b[0];
-    if (!(A_MN ? matrix_map(&a[i], pa, p.K, p.M, kBK) : matrix_map(&a[i], pa, p.M, p.K, kSmallBM)) ||
-        !(B_MN ? matrix_map(&b[i], pb, p.K, p.N, kBK) : matrix_map(&b[i], pb, p.N, p.K, kSmallBN)))
+// Products that do not depend on one another, in one launch.
+template <int EPI>
+psa_status_t run(const Wanted* wanted, int n, ProductList list, cudaStream_t stream) {
+  int64_t big = 0, small = 0, longest = 0;
+  constexpr int kBigN = EPI == kEpiGate ? kBigBN / 2 : kBigBN, kSmallN = EPI == kEpiGate ? kSmallBN / 2 : kSmallBN;
+  for (int i = 0; i < n; ++i) {
+    big += tiles_of(wanted[i], kBigBM, kBigN);
+    small += tiles_of(wanted[i], kSmallBM, kSmallN);
+    longest = std::max(longest, stages_of(wanted[i]));
+  }
+  const bool pairs = big >= 40 && wanted[0].M > kSmallBM;
+  const int edge_m = pairs ? kBigBM : kSmallBM, edge_n = pairs ? kBigN : kSmallN;
+  list.n_products = n;
+  int64_t first = 0;
+  for (int i = 0; i < n; ++i) {
+    const Wanted& w = wanted[i];
+    Product& p = list.p[i];
+    ProductMaps& maps = list.maps[i];
+    for (int k = 0; k < 2; ++k) {
+      if (w.a[k].p && !operand_maps(&maps.a[k], w.a[k].p, w.a[k].mn_major, w.M, w.K)) return PSA_ERR_CUDA;
+      if (w.b[k].p && !operand_maps(&maps.b[k], w.b[k].p, w.b[k].mn_major, w.N, w.K)) return PSA_ERR_CUDA;
+      p.out[k] = w.out[k];
+      if (pairs && w.out[k] && !matrix_map(&maps.store[k], w.out[k], w.M, w.N, 32, EPI == kEpiGateBwd ? 32 : 64)) return PSA_ERR_CUDA;
+    }
+    p.M = int32_t(w.M);
+    p.N = int32_t(w.N);
+    p.k_tiles = int32_t((w.K + kBK - 1) / kBK);
+    p.k_pairs = w.k_pairs;
+    p.m_tiles = int32_t((w.M + edge_m - 1) / edge_m);
+    p.n_tiles = int32_t((w.N + edge_n - 1) / edge_n);
+    p.n_outputs = w.n_outputs;
+    p.first = int32_t(first);
+    p.a_mn = w.a[0].mn_major;
+    p.b_mn = w.b[0].mn_major;
+    first += tiles_of(w, edge_m, edge_n);
+  }
+  if (first > 0x7fffffff / 8) return PSA_ERR_UNSUPPORTED;
+  list.n_work = int32_t(first);
+  list.splits = 1;
+  if (pairs) {
+    const Wanted& w = wanted[0];
+    if (EPI != kEpiOut && !matrix_map(&list.store_h, list.h, w.M, w.N, 32, EPI == kEpiGateBwd ? 32 : 64)) return PSA_ERR_CUDA;
+    if (EPI == kEpiGateBwd && (!matrix_map(&list.in[0], list.gate, w.M, w.N, 32, 32) || !matrix_map(&list.in[1], list.up, w.M, w.N, 32, 32)))
       return PSA_ERR_CUDA;
+    return launch(ffn_big_kernel<EPI>, 2 * std::min<int64_t>(first, kSmCount / 2), kBigThreads, kBigSmem, 0, stream, list);
   }
-  prm.M = int32_t(p.M);
-  prm.N = int32_t(p.N);
-  prm.k_tiles = int32_t((p.K + kBK - 1) / kBK);
-  prm.k_pairs = p.k_pairs;
-  prm.n_tiles = int32_t((p.N + kTileN - 1) / kTileN);
-  prm.n_outputs = p.n_outputs;
-  prm.splits = EPI == kEpiOut ? split_count(p.M, p.N, p.K, p.k_pairs, p.n_outputs) : 1;
-  auto kernel = ffn_small_kernel<A_MN, B_MN, EPI>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem) != cudaSuccess) return PSA_ERR_CUDA;
-  const dim3 grid(unsigned((p.M + kSmallBM - 1) / kSmallBM), unsigned(prm.n_tiles * p.n_outputs), unsigned(prm.splits));
-  kernel<<<grid, kSmallThreads, kSmallSmem, stream>>>(a[0], a[1], b[0], b[1], prm);
-  if (prm.splits > 1) {
-    const int64_t n = p.M * p.N;
-    ffn_sum_kernel<<<dim3(unsigned((n + 2047) / 2048), unsigned(p.n_outputs)), 256, 0, stream>>>(prm.partial, prm.out[0], prm.out[1],
-                                                                                                 n, prm.splits);
-  }
-  return check_last_cuda_error("psa_ffn launch");
+  while (list.splits < 8 && 2 * list.splits * small <= 2 * kSmCount && longest >= 8 * list.splits) list.splits *= 2;
+  return launch(ffn_small_kernel<EPI>, first * list.splits, kSmallThreads, kSmallSmem, list.splits, stream, list);
 }
 
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
 
 struct FfnWorkspace {
-  size_t h, d_gate, d_up, partial, total;
+  size_t h, d_gate, d_up, total;
 };
-
-FfnWorkspace workspace_layout(int64_t T, int64_t D, int64_t F, bool backward) {
-  FfnWorkspace w{};
+FfnWorkspace workspace_layout(int64_t T, int64_t F, bool backward) {
   const size_t act = aligned(size_t(T) * F * 2);
-  size_t at = act;   // h
-  if (backward) {
-    w.d_gate = at; at += act;
-    w.d_up = at; at += act;
-  }
-  w.partial = at;
-  int64_t part = backward ? std::max({partial_bytes(T, D, F, 2, 1), partial_bytes(D, F, T, 1, 2), partial_bytes(F, D, T, 1, 1)})
-                          : partial_bytes(T, D, F, 1, 1);
-  w.total = at + aligned(size_t(part));
-  return w;
+  return backward ? FfnWorkspace{0, act, 2 * act, 3 * act} : FfnWorkspace{0, 0, 0, act};
 }
 
 psa_status_t check_sizes(int64_t T, int32_t D, int32_t F) {
@@ -681,13 +762,14 @@ bool all_aligned(std::initializer_list<const void*> ptrs) {
   for (const void* p : ptrs) if (reinterpret_cast<uintptr_t>(p) & 15) return false;
   return true;
 }
+__nv_bfloat16* bf(void* p) { return static_cast<__nv_bfloat16*>(p); }
 
 }  // namespace
 }  // namespace psa
 
 extern "C" size_t psa_ffn_workspace_bytes(int64_t n_tokens, int32_t hidden, int32_t ffn, int32_t backward) {
   if (psa::check_sizes(n_tokens, hidden, ffn) != PSA_OK) return 0;
-  return psa::workspace_layout(n_tokens, hidden, ffn, backward != 0).total;
+  return psa::workspace_layout(n_tokens, ffn, backward != 0).total;
 }
 
 extern "C" psa_status_t psa_ffn(const void* x, const void* w_gate, const void* w_up, const void* w_down, int64_t n_tokens,
@@ -700,30 +782,15 @@ extern "C" psa_status_t psa_ffn(const void* x, const void* w_gate, const void* w
   if (n_tokens == 0) return PSA_OK;
   if (!all_set({x, w_gate, w_up, w_down, out, workspace})) return PSA_ERR_INVALID_ARG;
   if (!all_aligned({x, w_gate, w_up, w_down, out, gate, up, workspace})) return PSA_ERR_ALIGNMENT;
-  const FfnWorkspace w = workspace_layout(n_tokens, hidden, ffn, false);
-  char* ws = static_cast<char*>(workspace);
-  __nv_bfloat16* h = reinterpret_cast<__nv_bfloat16*>(ws + w.h);
   cudaStream_t st = cudaStream_t(stream);
-
-  GemmParams prm{};
-  prm.status = device_status;
-  prm.out[0] = static_cast<__nv_bfloat16*>(gate);
-  prm.out[1] = static_cast<__nv_bfloat16*>(up);
-  prm.h = h;
-  Product first{n_tokens, ffn, hidden};
-  first.a[0] = x;
-  first.b[0] = w_gate;
-  first.b[1] = w_up;
-  psa_status_t rc = launch_product<false, true, kEpiGate>(first, prm, st);
+  ProductList list{};
+  list.status = device_status;
+  list.h = bf(workspace);
+  const Wanted first{n_tokens, ffn, hidden, {{x, false}}, {{w_gate, true}, {w_up, true}}, {bf(gate), bf(up)}, 1, 1};
+  const psa_status_t rc = run<kEpiGate>(&first, 1, list, st);
   if (rc != PSA_OK) return rc;
-
-  prm.out[0] = static_cast<__nv_bfloat16*>(out);
-  prm.out[1] = nullptr;
-  prm.partial = reinterpret_cast<float*>(ws + w.partial);
-  Product second{n_tokens, hidden, ffn};
-  second.a[0] = h;
-  second.b[0] = w_down;
-  return launch_product<false, true, kEpiOut>(second, prm, st);
+  const Wanted second{n_tokens, hidden, ffn, {{list.h, false}}, {{w_down, true}}, {bf(out)}, 1, 1};
+  return run<kEpiOut>(&second, 1, list, st);
 }
 
 extern "C" psa_status_t psa_ffn_bwd(const void* d_out, const void* x, const void* w_gate, const void* w_up, const void* w_down,
@@ -746,50 +813,24 @@ extern "C" psa_status_t psa_ffn_bwd(const void* d_out, const void* x, const void
   }
   if (!all_set({d_out, x, w_gate, w_up, w_down, gate, up, dx, workspace})) return PSA_ERR_INVALID_ARG;
   if (!all_aligned({d_out, x, w_gate, w_up, w_down, gate, up, dx, dw_gate, dw_up, dw_down, workspace})) return PSA_ERR_ALIGNMENT;
-  const FfnWorkspace w = workspace_layout(n_tokens, hidden, ffn, true);
+  const FfnWorkspace w = workspace_layout(n_tokens, ffn, true);
   char* ws = static_cast<char*>(workspace);
-  auto bf = [](void* p) { return static_cast<__nv_bfloat16*>(p); };
   __nv_bfloat16 *h = bf(ws + w.h), *d_gate = bf(ws + w.d_gate), *d_up = bf(ws + w.d_up);
-
-  GemmParams prm{};
-  prm.status = device_status;
-  prm.partial = reinterpret_cast<float*>(ws + w.partial);
-  prm.out[0] = d_gate;
-  prm.out[1] = d_up;
-  prm.h = h;
-  prm.gate = static_cast<const __nv_bfloat16*>(gate);
-  prm.up = static_cast<const __nv_bfloat16*>(up);
-  Product dh{n_tokens, ffn, hidden};   // dH = dY Wd^T: Wd has K (hidden) innermost
-  dh.a[0] = d_out;
-  dh.b[0] = w_down;
-  psa_status_t rc = launch_product<false, false, kEpiGateBwd>(dh, prm, st);
+  ProductList list{};
+  list.status = device_status;
+  list.h = h;
+  list.gate = static_cast<const __nv_bfloat16*>(gate);
+  list.up = static_cast<const __nv_bfloat16*>(up);
+  // dH = dY Wd^T: Wd has K (hidden) innermost
+  const Wanted dh{n_tokens, ffn, hidden, {{d_out, false}}, {{w_down, false}}, {d_gate, d_up}, 1, 1};
+  const psa_status_t rc = run<kEpiGateBwd>(&dh, 1, list, st);
   if (rc != PSA_OK) return rc;
-
-  Product in{n_tokens, hidden, ffn};   // dX = dG Wg^T + dU Wu^T
-  in.a[0] = d_gate;
-  in.a[1] = d_up;
-  in.b[0] = w_gate;
-  in.b[1] = w_up;
-  in.k_pairs = 2;
-  prm.out[0] = bf(dx);
-  prm.out[1] = nullptr;
-  rc = launch_product<false, false, kEpiOut>(in, prm, st);
-  if (rc != PSA_OK) return rc;
-
-  Product gu{hidden, ffn, n_tokens};   // dWg = X^T dG and dWu = X^T dU
-  gu.a[0] = x;
-  gu.b[0] = d_gate;
-  gu.b[1] = d_up;
-  gu.n_outputs = 2;
-  prm.out[0] = bf(dw_gate);
-  prm.out[1] = bf(dw_up);
-  rc = launch_product<true, true, kEpiOut>(gu, prm, st);
-  if (rc != PSA_OK) return rc;
-
-  Product down{ffn, hidden, n_tokens};   // dWd = H^T dY
-  down.a[0] = h;
-  down.b[0] = d_out;
-  prm.out[0] = bf(dw_down);
-  prm.out[1] = nullptr;
-  return launch_product<true, true, kEpiOut>(down, prm, st);
+  const Wanted last[3] = {
+      // dX = dG Wg^T + dU Wu^T
+      {n_tokens, hidden, ffn, {{d_gate, false}, {d_up, false}}, {{w_gate, false}, {w_up, false}}, {bf(dx)}, 2, 1},
+      // dWg = X^T dG and dWu = X^T dU
+      {hidden, ffn, n_tokens, {{x, true}}, {{d_gate, true}, {d_up, true}}, {bf(dw_gate), bf(dw_up)}, 1, 2},
+      // dWd = H^T dY
+      {ffn, hidden, n_tokens, {{h, true}}, {{d_out, true}}, {bf(dw_down)}, 1, 1}};
+  return run<kEpiOut>(last, 3, list, st);
 }
