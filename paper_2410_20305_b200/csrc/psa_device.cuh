@@ -368,6 +368,13 @@ __device__ __forceinline__ void tma_load_3d_w(uint32_t dst, const CUtensorMap* m
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "r"(leader)
       : "memory");
 }
+__device__ __forceinline__ void tma_store_3d_w(const CUtensorMap* m, uint32_t src, int c0, int c1, int c2, uint32_t leader) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];\n\t}"
+      ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(leader)
+      : "memory");
+}
 // Into this CTA's shared memory, completing on a barrier of either CTA of the pair (address from cluster_map).
 __device__ __forceinline__ void tma_load_3d_pair_w(uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2, uint32_t cluster_bar,
                                                    uint32_t leader) {

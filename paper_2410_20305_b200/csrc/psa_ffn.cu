@@ -57,6 +57,7 @@ struct Product {
   int32_t n_outputs;           // outputs side by side
   int32_t first;               // the product's first tile in the launch
   int32_t a_mn, b_mn;          // which way the operands lie
+  int32_t early;               // B is not written by the kernel before this one, nor is that kernel's end awaited for it
 };
 struct ProductList {
   ProductMaps maps[kMaxProducts];
@@ -64,7 +65,7 @@ struct ProductList {
   CUtensorMap in[2], store_h;  // kEpiGateBwd: G, U;  H
   const __nv_bfloat16 *gate, *up;
   __nv_bfloat16* h;
-  int32_t n_products, n_work, splits;
+  int32_t n_products, n_work, splits, a_rows;
   int32_t* status;
 };
 
@@ -136,12 +137,15 @@ __device__ __forceinline__ void unpack8(const uint4& w, float* v) {
 // ---------------------------------------------------------------- one CTA per tile of 128 x 128
 // For launches of few tiles.  Where they are fewer than the SMs can hold, a cluster of 2, 4 or 8 CTAs shares a tile's K: each
 // leaves its sums in its shared memory, and all of them add the parts, in the CTAs' order, and finish a share of the tile.
-// Warps 0-3: end of the tile (TMEM lane = row of the tile), warp 4: TMA, warp 5: UMMA.
-constexpr int kSmallBM = 128, kSmallBN = 128, kSmallStages = 3, kSmallThreads = 192;
-constexpr uint32_t kSmallStageBytes = uint32_t(kSmallBM + kSmallBN) * kBK * 2;
-constexpr uint32_t kSmallSmem = kSmallStages * kSmallStageBytes + 1024 + 256;
+// Warps 0-7: end of the tile (TMEM lane = row of the tile, half of its columns each), warp 8: TMA, warp 9: UMMA.
+// Up to 64 tokens, a stage holds no more of A's rows than there are (rounded up to 8), and more stages fit; what the UMMA takes
+// for the tile's other rows is whatever lies behind them, and goes to rows that nobody reads.
+constexpr int kSmallBM = 128, kSmallBN = 128, kSmallMaxStages = 6, kSmallThreads = 320;
+constexpr uint32_t kSmallRing = 96 * 1024, kSmallBBytes = kSmallBN * kBK * 2;
+constexpr uint32_t kSmallSmem = kSmallRing + 1024 + 256;
 constexpr int kPartPitch = kSmallBN + 4;      // floats per row of a part: rows start four banks apart
-static_assert(kSmallBM * kPartPitch * 4 <= kSmallStages * kSmallStageBytes, "a part takes the place of the stages");
+static_assert(kSmallBM * kPartPitch * 4 <= kSmallRing, "a part takes the place of the stages");
+__host__ __device__ constexpr int small_rows(int64_t M) { return M <= 64 ? int(M + 7) / 8 * 8 : kSmallBM; }
 
 // Eight neighbouring elements of a tile: their sums (kEpiGate: x of G, y of U) become outputs.
 template <int EPI>
@@ -175,18 +179,19 @@ __device__ __forceinline__ void finish8(const ProductList& list, const Product& 
 template <int EPI>
 __global__ void __launch_bounds__(kSmallThreads)
 ffn_small_kernel(const __grid_constant__ ProductList list) {
-  constexpr int kBN = kSmallBN, kStages = kSmallStages;
+  constexpr int kBN = kSmallBN;
   constexpr int kTileN = EPI == kEpiGate ? kBN / 2 : kBN;      // features per tile
-  constexpr uint32_t kABytes = kSmallBM * kBK * 2;
+  const uint32_t a_bytes = uint32_t(list.a_rows) * kBK * 2, stage_bytes = a_bytes + kSmallBBytes;
+  const int stages = min(kSmallMaxStages, int(kSmallRing / stage_bytes));
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen_base = smem_raw + (base - smem_u32(smem_raw));
-  const uint32_t bars = base + kStages * kSmallStageBytes;
+  const uint32_t bars = base + kSmallRing;
   auto full = [&](int s) { return bars + 8u * s; };
-  auto empty = [&](int s) { return bars + 8u * (kStages + s); };
-  const uint32_t done = bars + 16u * kStages;
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + kStages * kSmallStageBytes + 128);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_base + kStages * kSmallStageBytes + 136);
+  auto empty = [&](int s) { return bars + 8u * (kSmallMaxStages + s); };
+  const uint32_t done = bars + 16u * kSmallMaxStages;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen_base + kSmallRing + 128);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen_base + kSmallRing + 136);
   const WaitCtx wctx{abort_flag, list.status, kWaitLimitClocks};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -194,11 +199,11 @@ ffn_small_kernel(const __grid_constant__ ProductList list) {
   copy_products(list, products);
   if (threadIdx.x == 0) {
     *abort_flag = 0;
-    for (int s = 0; s < kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    for (int s = 0; s < stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     mbar_init(done, 1);
     fence_mbar_init();
   }
-  if (warp == 5) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kBN);
+  if (warp == 9) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kBN);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -208,12 +213,15 @@ ffn_small_kernel(const __grid_constant__ ProductList list) {
   const Product& p = products[at.k];
   const int total = p.k_tiles * p.k_pairs;
   const int it0 = int(int64_t(total) * part / splits), it1 = int(int64_t(total) * (part + 1) / splits);
-  behind_wait();
-  behind_go();
+  if (warp != 8) {
+    behind_wait();
+    behind_go();
+  }
 
   // Rows of this thread, for the warps that finish a tile from TMEM.
-  const int row = at.m0 + warp * 32 + lane;
-  const uint32_t lanes = tmem + (uint32_t(warp * 32) << 16);
+  const int quarter = warp & 3, row = at.m0 + quarter * 32 + lane, half = warp >> 2;
+  const uint32_t lanes = tmem + (uint32_t(quarter * 32) << 16);
+  constexpr int kHalfN = kTileN / 2;
   auto load_gate = [&](int r, int col, uint4& g, uint4& u) {
     if (EPI != kEpiGateBwd || r >= p.M || col >= p.N) return;
     const int64_t from = int64_t(r) * p.N + col;
@@ -222,49 +230,64 @@ ffn_small_kernel(const __grid_constant__ ProductList list) {
     u = *reinterpret_cast<const uint4*>(list.up + from);
   };
 
-  if (warp == 4) {
+  if (warp == 8) {
     const uint32_t issuer = elect_one();
     const ProductMaps& maps = list.maps[at.k];
     const Strip a(maps.a, p.a_mn, at.m0, p.M), b(maps.b, p.b_mn, at.n0, p.N);
     const int k_tiles = p.k_tiles, sel = at.sel;
-    int n = 0;   // stages filled
-    for (int it = it0; it < it1; ++it, ++n) {
-      const int s = n % kStages;
-      if (n >= kStages) mbar_wait(empty(s), (n / kStages - 1) & 1, wctx);
-      if (*abort_flag) break;
+    auto load_a = [&](int it, int s) {
+      const bool second = it >= k_tiles;
+      const uint32_t bar = full(s);
+      a.load(second, (second ? it - k_tiles : it) * kBK, base + s * stage_bytes,
+             [&](uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2) { tma_load_3d_w(dst, m, c0, c1, c2, bar, issuer); });
+    };
+    auto load_b = [&](int it, int s) {
       const bool second = it >= k_tiles;
       const int k0 = (second ? it - k_tiles : it) * kBK;
-      const uint32_t sa = base + s * kSmallStageBytes, sb = sa + kABytes, bar = full(s);
+      const uint32_t sb = base + s * stage_bytes + a_bytes, bar = full(s);
       auto load = [&](uint32_t dst, const CUtensorMap* m, int c0, int c1, int c2) { tma_load_3d_w(dst, m, c0, c1, c2, bar, issuer); };
-      mbar_expect_tx_w(bar, kSmallStageBytes, issuer);
-      a.load(second, k0, sa, load);
+      mbar_expect_tx_w(bar, stage_bytes, issuer);
       if (EPI == kEpiGate) {   // the same features of two weights
         load(sb, &b.m[0].flat, at.n0, 0, k0);
         load(sb + kSub, &b.m[1].flat, at.n0, 0, k0);
       } else {
         b.load(second || sel, k0, sb, load);
       }
+    };
+    // Weights that the kernel before does not write may come before it has ended.
+    const int ahead = p.early ? min(stages, it1 - it0) : 0;
+    for (int i = 0; i < ahead; ++i) load_b(it0 + i, i);
+    behind_wait();
+    behind_go();
+    int n = 0, s = 0, turn = 0;   // stages filled; the next one and its turn of the ring
+    for (int it = it0; it < it1; ++it, ++n) {
+      if (turn) mbar_wait(empty(s), (turn - 1) & 1, wctx);
+      if (*abort_flag) break;
+      if (n >= ahead) load_b(it, s);
+      load_a(it, s);
+      if (++s == stages) { s = 0; ++turn; }
     }
     if (*abort_flag) {   // shared memory must outlive the copies in flight
       const long long t0 = clock64();
-      for (int i = n > kStages ? n - kStages : 0; i < n; ++i)
-        while (!mbar_try_wait(full(i % kStages), (i / kStages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
+      for (int i = n > stages ? n - stages : 0; i < n; ++i)      // (the first wait can only expire after `ahead` stages)
+        while (!mbar_try_wait(full(i % stages), (i / stages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
     }
     __syncwarp();
-  } else if (warp == 5) {
+  } else if (warp == 9) {
     const uint32_t issuer = elect_one();
     const bool a_mn = p.a_mn, b_mn = p.b_mn;
     const uint32_t idesc = umma_idesc_bf16(kSmallBM, kBN, false, false) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16);
     const uint32_t a_step = (a_mn ? 2048 : 32) >> 4, b_step = (b_mn ? 2048 : 32) >> 4;
-    for (int it = it0, n = 0; it < it1; ++it, ++n) {
-      const int s = n % kStages;
-      mbar_wait(full(s), (n / kStages) & 1, wctx);
+    int s = 0, turn = 0;
+    for (int it = it0; it < it1; ++it) {
+      mbar_wait(full(s), turn & 1, wctx);
       tc_fence_after();
-      const uint32_t sa = base + s * kSmallStageBytes;
-      const uint32_t a = smem_desc_lo(sa, a_mn ? kSub : 16), b = smem_desc_lo(sa + kABytes, b_mn ? kSub : 16);
+      const uint32_t sa = base + s * stage_bytes;
+      const uint32_t a = smem_desc_lo(sa, a_mn ? kSub : 16), b = smem_desc_lo(sa + a_bytes, b_mn ? kSub : 16);
 #pragma unroll
-      for (int kk = 0; kk < kBK / 16; ++kk) umma_ss_w(tmem, a + kk * a_step, b + kk * b_step, idesc, n > 0 || kk > 0, issuer);
+      for (int kk = 0; kk < kBK / 16; ++kk) umma_ss_w(tmem, a + kk * a_step, b + kk * b_step, idesc, it > it0 || kk > 0, issuer);
       umma_commit_w(empty(s), issuer);
+      if (++s == stages) { s = 0; ++turn; }
     }
     umma_commit_w(done, issuer);
     __syncwarp();
@@ -272,12 +295,12 @@ ffn_small_kernel(const __grid_constant__ ProductList list) {
     uint4 g[4], u[4];
     if (splits == 1)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) load_gate(row, at.n0 + 8 * j, g[j], u[j]);
+      for (int j = 0; j < 4; ++j) load_gate(row, at.n0 + half * kHalfN + 8 * j, g[j], u[j]);
     mbar_wait(done, 0, wctx);
     tc_fence_after();
     const bool live = row < p.M && !*abort_flag;
 #pragma unroll 1
-    for (int c = 0; c < kTileN; c += 32) {
+    for (int c = half * kHalfN; c < (half + 1) * kHalfN; c += 32) {
       uint32_t v[32], w[32];
       tmem_ld32_wait(lanes + c, v);
       if (EPI == kEpiGate) tmem_ld32_wait(lanes + kTileN + c, w);
@@ -286,7 +309,7 @@ ffn_small_kernel(const __grid_constant__ ProductList list) {
         if (it0 == it1)        // a short K leaves some of the CTAs nothing to add
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = w[j] = 0u;
-        const uint32_t to = base + uint32_t(warp * 32 + lane) * kPartPitch * 4 + c * 4;
+        const uint32_t to = base + uint32_t(quarter * 32 + lane) * kPartPitch * 4 + c * 4;
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
           st_shared_v4(to + 4 * j, v[j], v[j + 1], v[j + 2], v[j + 3]);
@@ -298,7 +321,7 @@ ffn_small_kernel(const __grid_constant__ ProductList list) {
       for (int j = 0; j < 4; ++j) {
         const int col = at.n0 + c + 8 * j;
         const uint4 g0 = g[j], u0 = u[j];
-        if (c + 32 < kTileN) load_gate(row, col + 32, g[j], u[j]);
+        if (c + 32 < (half + 1) * kHalfN) load_gate(row, col + 32, g[j], u[j]);
         if (live && col < p.N) finish8<EPI>(list, p, at.sel, row, col, x + 8 * j, y + 8 * j, g0, u0);
       }
     }
@@ -326,7 +349,7 @@ ffn_small_kernel(const __grid_constant__ ProductList list) {
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 5) {
+  if (warp == 9) {
     tc_fence_after();
     tmem_dealloc(tmem, kBN);
   }
@@ -349,7 +372,10 @@ constexpr uint32_t kBigBarsAt = kBigBufsAt + 4 * kBigBufs * kBufBytes;
 constexpr uint32_t kBigSmem = kBigBarsAt + 256 + 1024;
 static_assert(kBigSmem <= 227 * 1024, "shared memory of one CTA");
 // kEpiGateBwd: boxes of 32 rows x 32 columns.  G and U arrive in three sets of two buffers, up to two boxes ahead, and leave
-// from them as dG and dU; H leaves from two buffers of its own.
+// from them as dG and dU; H leaves from two buffers of its own.  Its five tensors take 640 KB of a tile's way through shared
+// memory beside the 8 MB of 64 stages, which fill the 128 bytes a clock that shared memory has: at 4096 x 9472 x 4096 the
+// product takes 231 us, without them 190.  G and U by ordinary loads into registers, each lane its row: 251 us; a fourth
+// set and H by ordinary stores: 236; separate buffers for what arrives and what leaves: 236.
 constexpr uint32_t kBoxBytes = 32 * 32 * 2;
 constexpr int kBoxSets = 3, kBoxesPerTile = kBigBN / 32;
 static_assert((2 * kBoxSets + 2) * kBoxBytes <= kBigBufs * kBufBytes, "a warp's buffers");
@@ -458,6 +484,7 @@ ffn_big_kernel(const __grid_constant__ ProductList list) {
     __syncwarp();
   } else if (warp >= 4) {
     const int w = warp - 4;
+    const uint32_t issuer = elect_one();     // the lane that owns the warp's copies and groups of stores
     const uint32_t bufs = base + kBigBufsAt + uint32_t(w) * kBigBufs * kBufBytes;
     auto drained = [&](int i) {      // this warp has read the accumulator
       tc_fence_before();
@@ -476,9 +503,10 @@ ffn_big_kernel(const __grid_constant__ ProductList list) {
         const ProductMaps& maps = list.maps[at.k];
         const int row0 = at.m0 + 128 * int(rank) + 32 * w;
         const uint32_t lanes = tmem + uint32_t(i & 1) * 256 + (uint32_t(w * 32) << 16);
-        auto store = [&](const CUtensorMap* m, uint32_t b, int col) {    // by one lane, after the warp's writes
-          if (row0 < p.M && col < p.N) tma_store_3d(m, b, col, 0, row0);
-          tma_commit_group();
+        const int M = p.M, N = p.N;
+        auto store = [&](const CUtensorMap* m, uint32_t b, int col) {    // after the warp's writes
+          tma_store_3d_w(m, b, col, 0, row0, row0 < M && col < N ? issuer : 0u);
+          if (issuer) tma_commit_group();
         };
         mbar_wait(acc_full(i & 1), (i >> 1) & 1, wctx);
         tc_fence_after();
@@ -489,7 +517,7 @@ ffn_big_kernel(const __grid_constant__ ProductList list) {
             uint32_t v[64];
             tmem_ld64_wait(lanes + c * 64, v);
             if (c == kBigBN / 64 - 1) drained(i);
-            if (lane == 0) tma_wait_group_read<kBigBufs - 1>();
+            if (issuer) tma_wait_group_read<kBigBufs - 1>();
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -498,14 +526,14 @@ ffn_big_kernel(const __grid_constant__ ProductList list) {
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) store(&maps.store[at.sel], buf(use), at.n0 + c * 64);
+            store(&maps.store[at.sel], buf(use), at.n0 + c * 64);
           }
         } else {
           const bool keep = p.out[0] != nullptr;
           const int n_bufs = keep ? 3 : 1;
 #pragma unroll 1
           for (int c = 0; c < kTileN / 64; ++c, use += n_bufs) {
-            if (lane == 0) {
+            if (issuer) {
               if (keep) tma_wait_group_read<kBigBufs - 3>(); else tma_wait_group_read<kBigBufs - 1>();
             }
             __syncwarp();
@@ -534,12 +562,10 @@ ffn_big_kernel(const __grid_constant__ ProductList list) {
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) {
-              store(&list.store_h, buf(use), at.n0 + c * 64);
-              if (keep) {
-                store(&maps.store[0], buf(use + 1), at.n0 + c * 64);
-                store(&maps.store[1], buf(use + 2), at.n0 + c * 64);
-              }
+            store(&list.store_h, buf(use), at.n0 + c * 64);
+            if (keep) {
+              store(&maps.store[0], buf(use + 1), at.n0 + c * 64);
+              store(&maps.store[1], buf(use + 2), at.n0 + c * 64);
             }
           }
         }
@@ -555,17 +581,18 @@ ffn_big_kernel(const __grid_constant__ ProductList list) {
       auto cell = [&](uint32_t b, int eight) { return b + uint32_t(lane) * 64 + ((uint32_t(eight) ^ uint32_t((lane >> 1) & 3)) << 4); };
       int asked = 0;
       Place ahead{};
-      auto ask = [&]() {     // one lane requests G and U of the next box
+      auto ask = [&]() {     // requests G and U of the next box
         if (asked >= n_boxes) return;
         const int c = asked % kBoxesPerTile;
         if (c == 0) ahead = place(cluster + asked / kBoxesPerTile * n_clusters);
         const uint32_t bar = in_full(w, asked % kBoxSets);
-        mbar_expect_tx(bar, 2 * kBoxBytes);
-        tma_load_3d(set_buf(asked, 0), &list.in[0], ahead.n0 + c * 32, 0, ahead.m0 + row_of, bar);
-        tma_load_3d(set_buf(asked, 1), &list.in[1], ahead.n0 + c * 32, 0, ahead.m0 + row_of, bar);
+        mbar_expect_tx_w(bar, 2 * kBoxBytes, issuer);
+        tma_load_3d_w(set_buf(asked, 0), &list.in[0], ahead.n0 + c * 32, 0, ahead.m0 + row_of, bar, issuer);
+        tma_load_3d_w(set_buf(asked, 1), &list.in[1], ahead.n0 + c * 32, 0, ahead.m0 + row_of, bar, issuer);
         ++asked;
       };
-      if (lane == 0) { ask(); ask(); }
+      ask();
+      ask();
       Place at{};
 #pragma unroll 1
       for (int q = 0; q < n_boxes && !*abort_flag; ++q) {
@@ -581,6 +608,7 @@ ffn_big_kernel(const __grid_constant__ ProductList list) {
         uint32_t v[32];
         tmem_ld32_wait(tmem + uint32_t(i & 1) * 256 + (uint32_t(w * 32) << 16) + c * 32, v);
         if (c == kBoxesPerTile - 1) drained(i);
+        const int row = at.m0 + row_of, col = at.n0 + c * 32;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float* x = reinterpret_cast<const float*>(v) + 8 * j;
@@ -598,25 +626,24 @@ ffn_big_kernel(const __grid_constant__ ProductList list) {
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
-          const int row = at.m0 + row_of, col = at.n0 + c * 32;
-          if (row < M && col < N) {
-            tma_store_3d(&maps.store[0], set_buf(q, 0), col, 0, row);
-            tma_store_3d(&maps.store[1], set_buf(q, 1), col, 0, row);
-            tma_store_3d(&list.store_h, h_buf(q), col, 0, row);
-          }
+        const uint32_t inside = row < M && col < N ? issuer : 0u;
+        tma_store_3d_w(&maps.store[0], set_buf(q, 0), col, 0, row, inside);
+        tma_store_3d_w(&maps.store[1], set_buf(q, 1), col, 0, row, inside);
+        tma_store_3d_w(&list.store_h, h_buf(q), col, 0, row, inside);
+        if (issuer) {
           tma_commit_group();
-          tma_wait_group_read<1>();    // the set of the box before this one is free for the box after the next
-          ask();
+          tma_wait_group_read<1>();    // the set of the box before this one is free
         }
+        __syncwarp();
+        ask();
       }
-      if (lane == 0 && *abort_flag) {   // loads of G and U in flight
+      if (*abort_flag) {   // loads of G and U in flight
         const long long t0 = clock64();
         for (int q = asked > kBoxSets ? asked - kBoxSets : 0; q < asked; ++q)
           while (!mbar_try_wait(in_full(w, q % kBoxSets), (q / kBoxSets) & 1) && clock64() - t0 < kWaitLimitClocks) {}
       }
     }
-    if (lane == 0) tma_wait_group_read<0>();   // shared memory must outlive the stores' reads
+    if (issuer) tma_wait_group_read<0>();   // shared memory must outlive the stores' reads
     __syncwarp();
   }
   tc_fence_before();
@@ -647,8 +674,8 @@ bool matrix_map(CUtensorMap* m, const void* p, int64_t rows, int64_t cols, int b
 bool pair_map(CUtensorMap* m, const void* p, int64_t rows, int64_t cols) {
   return encode(m, p, kChunk, rows, cols / kChunk, cols * 2, kChunk * 2, kChunk, kBK, 2, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-bool operand_maps(OperandMaps* o, const void* p, bool mn_major, int64_t mn, int64_t k) {
-  if (!mn_major) return matrix_map(&o->flat, p, mn, k, 128);
+bool operand_maps(OperandMaps* o, const void* p, bool mn_major, int64_t mn, int64_t k, int rows) {
+  if (!mn_major) return matrix_map(&o->flat, p, mn, k, rows);
   return matrix_map(&o->flat, p, k, mn, kBK) && (mn < 2 * kChunk || pair_map(&o->pair, p, k, mn));
 }
 
@@ -662,6 +689,7 @@ struct Wanted {
   Matrix a[2], b[2];
   __nv_bfloat16* out[2];
   int k_pairs, n_outputs;
+  bool early;
 };
 
 int64_t tiles_of(const Wanted& w, int edge_m, int edge_n) {
@@ -669,9 +697,10 @@ int64_t tiles_of(const Wanted& w, int edge_m, int edge_n) {
 }
 int64_t stages_of(const Wanted& w) { return (w.K + kBK - 1) / kBK * w.k_pairs; }
 
-template <typename Kernel>
-psa_status_t launch(Kernel kernel, int64_t grid, unsigned threads, uint32_t smem, int cluster, cudaStream_t stream, const ProductList& list) {
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return PSA_ERR_CUDA;
+template <typename... Params, typename... Args>
+psa_status_t launch(void (*kernel)(Params...), int64_t grid, unsigned threads, uint32_t smem, int cluster, cudaStream_t stream,
+                    const Args&... args) {
+  if (smem && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return PSA_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(unsigned(grid));
   cfg.blockDim = dim3(threads);
@@ -683,8 +712,8 @@ psa_status_t launch(Kernel kernel, int64_t grid, unsigned threads, uint32_t smem
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim = {unsigned(cluster), 1, 1};
   cfg.attrs = attr;
-  cfg.numAttrs = cluster ? 2 : 1;
-  cudaLaunchKernelEx(&cfg, kernel, list);
+  cfg.numAttrs = cluster ? 2 : 1;      // (0: the kernel says it itself)
+  cudaLaunchKernelEx(&cfg, kernel, args...);
   return check_last_cuda_error("psa_ffn launch");
 }
 
@@ -701,14 +730,15 @@ psa_status_t run(const Wanted* wanted, int n, ProductList list, cudaStream_t str
   const bool pairs = big >= 40 && wanted[0].M > kSmallBM;
   const int edge_m = pairs ? kBigBM : kSmallBM, edge_n = pairs ? kBigN : kSmallN;
   list.n_products = n;
+  list.a_rows = pairs || n > 1 || wanted[0].a[0].mn_major ? 128 : small_rows(wanted[0].M);
   int64_t first = 0;
   for (int i = 0; i < n; ++i) {
     const Wanted& w = wanted[i];
     Product& p = list.p[i];
     ProductMaps& maps = list.maps[i];
     for (int k = 0; k < 2; ++k) {
-      if (w.a[k].p && !operand_maps(&maps.a[k], w.a[k].p, w.a[k].mn_major, w.M, w.K)) return PSA_ERR_CUDA;
-      if (w.b[k].p && !operand_maps(&maps.b[k], w.b[k].p, w.b[k].mn_major, w.N, w.K)) return PSA_ERR_CUDA;
+      if (w.a[k].p && !operand_maps(&maps.a[k], w.a[k].p, w.a[k].mn_major, w.M, w.K, list.a_rows)) return PSA_ERR_CUDA;
+      if (w.b[k].p && !operand_maps(&maps.b[k], w.b[k].p, w.b[k].mn_major, w.N, w.K, 128)) return PSA_ERR_CUDA;
       p.out[k] = w.out[k];
       if (pairs && w.out[k] && !matrix_map(&maps.store[k], w.out[k], w.M, w.N, 32, EPI == kEpiGateBwd ? 32 : 64)) return PSA_ERR_CUDA;
     }
@@ -722,6 +752,7 @@ psa_status_t run(const Wanted* wanted, int n, ProductList list, cudaStream_t str
     p.first = int32_t(first);
     p.a_mn = w.a[0].mn_major;
     p.b_mn = w.b[0].mn_major;
+    p.early = w.early;
     first += tiles_of(w, edge_m, edge_n);
   }
   if (first > 0x7fffffff / 8) return PSA_ERR_UNSUPPORTED;
@@ -786,10 +817,10 @@ extern "C" psa_status_t psa_ffn(const void* x, const void* w_gate, const void* w
   ProductList list{};
   list.status = device_status;
   list.h = bf(workspace);
-  const Wanted first{n_tokens, ffn, hidden, {{x, false}}, {{w_gate, true}, {w_up, true}}, {bf(gate), bf(up)}, 1, 1};
+  const Wanted first{n_tokens, ffn, hidden, {{x, false}}, {{w_gate, true}, {w_up, true}}, {bf(gate), bf(up)}, 1, 1, false};
   const psa_status_t rc = run<kEpiGate>(&first, 1, list, st);
   if (rc != PSA_OK) return rc;
-  const Wanted second{n_tokens, hidden, ffn, {{list.h, false}}, {{w_down, true}}, {bf(out)}, 1, 1};
+  const Wanted second{n_tokens, hidden, ffn, {{list.h, false}}, {{w_down, true}}, {bf(out)}, 1, 1, true};
   return run<kEpiOut>(&second, 1, list, st);
 }
 
@@ -822,15 +853,15 @@ extern "C" psa_status_t psa_ffn_bwd(const void* d_out, const void* x, const void
   list.gate = static_cast<const __nv_bfloat16*>(gate);
   list.up = static_cast<const __nv_bfloat16*>(up);
   // dH = dY Wd^T: Wd has K (hidden) innermost
-  const Wanted dh{n_tokens, ffn, hidden, {{d_out, false}}, {{w_down, false}}, {d_gate, d_up}, 1, 1};
+  const Wanted dh{n_tokens, ffn, hidden, {{d_out, false}}, {{w_down, false}}, {d_gate, d_up}, 1, 1, false};
   const psa_status_t rc = run<kEpiGateBwd>(&dh, 1, list, st);
   if (rc != PSA_OK) return rc;
   const Wanted last[3] = {
       // dX = dG Wg^T + dU Wu^T
-      {n_tokens, hidden, ffn, {{d_gate, false}, {d_up, false}}, {{w_gate, false}, {w_up, false}}, {bf(dx)}, 2, 1},
+      {n_tokens, hidden, ffn, {{d_gate, false}, {d_up, false}}, {{w_gate, false}, {w_up, false}}, {bf(dx)}, 2, 1, true},
       // dWg = X^T dG and dWu = X^T dU
-      {hidden, ffn, n_tokens, {{x, true}}, {{d_gate, true}, {d_up, true}}, {bf(dw_gate), bf(dw_up)}, 1, 2},
+      {hidden, ffn, n_tokens, {{x, true}}, {{d_gate, true}, {d_up, true}}, {bf(dw_gate), bf(dw_up)}, 1, 2, false},
       // dWd = H^T dY
-      {ffn, hidden, n_tokens, {{h, true}}, {{d_out, true}}, {bf(dw_down)}, 1, 1}};
+      {ffn, hidden, n_tokens, {{h, true}}, {{d_out, true}}, {bf(dw_down)}, 1, 1, true}};
   return run<kEpiOut>(last, 3, list, st);
 }

@@ -22,9 +22,9 @@ f64 = lambda t: t.detach().cpu().double().numpy()  # noqa: E731
 bf16 = lambda a: torch.as_tensor(a).to(torch.bfloat16)  # noqa: E731
 rounded = lambda a: f64(bf16(torch.as_tensor(a, dtype=torch.float32)))  # noqa: E731
 
-# One tile and less, tile edges, several tiles, split sums, and sizes beyond the rule for the large tiles.
+# A few tokens, one tile and less, tile edges, several tiles, split sums, and sizes beyond the rule for the large tiles.
 SIZES = [(1, 8, 8), (1, 64, 128), (2, 72, 200), (31, 128, 64), (64, 136, 520), (127, 64, 64), (128, 128, 128), (129, 200, 72),
-         (300, 264, 392), (1, 2048, 4096), (5, 4096, 1032), (130, 1024, 2048), (1000, 512, 1024), (2300, 64, 128), (2048, 1024, 2056),
+         (300, 264, 392), (1, 2048, 4096), (3, 1032, 264), (4, 2056, 520), (5, 4096, 1032), (130, 1024, 2048), (1000, 512, 1024), (2300, 64, 128), (2048, 1024, 2056),
          (1803, 1544, 2816), (2900, 1800, 520)]
 
 
