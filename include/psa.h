@@ -522,6 +522,7 @@ psa_status_t psa_norm(const void* x, const void* residual, const void* weight, c
  *   dx        device (out): the gradient of x and of residual; may be d_out, d_total or x
  *   dweight, dbias   device [hidden] of `weight_dtype` (out); dbias may be NULL, and is NULL if rms
  *   workspace device scratch of psa_norm_bwd_workspace_bytes() bytes, 16-byte aligned
+ *   device_status  device int32 or NULL; PSA_DEVSTAT_WAIT_EXPIRED is ORed in as by psa_fwd
  * The sums over tokens are taken in an order that depends on the sizes alone.  n_tokens = 0 writes zeros to dweight, dbias.
  * Errors: as psa_norm.
  */
@@ -529,7 +530,7 @@ size_t psa_norm_bwd_workspace_bytes(int64_t n_tokens, int32_t hidden);
 psa_status_t psa_norm_bwd(const void* d_out, const void* x, const void* weight, const float* stats,
                           const void* d_total, int32_t dtype, int32_t weight_dtype, int64_t n_tokens,
                           int32_t hidden, int32_t rms, void* dx, void* dweight, void* dbias,
-                          void* workspace, void* stream);
+                          void* workspace, int32_t* device_status, void* stream);
 
 /*
  * psa_embed -- token embedding: out[t] = scale * table[token_ids[t]]  (the paper has no counterpart).

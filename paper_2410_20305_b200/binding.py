@@ -99,7 +99,7 @@ def load_library():
     lib.dpo_logp.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp]
     lib.dpo_logp_f64sum.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
     lib.psa_norm.argtypes = [vp, vp, vp, vp, i32, i32, i64, i32, f32, i32, vp, vp, vp, vp]
-    lib.psa_norm_bwd.argtypes = [vp, vp, vp, vp, vp, i32, i32, i64, i32, i32, vp, vp, vp, vp, vp]
+    lib.psa_norm_bwd.argtypes = [vp, vp, vp, vp, vp, i32, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.psa_norm_bwd_workspace_bytes.argtypes = [i64, i32]
     lib.psa_embed.argtypes = [vp, vp, i32, i64, i64, i32, f32, vp, vp, vp]
     lib.psa_embed_bwd.argtypes = [vp, vp, i32, i32, i64, i64, i32, f32, i32, vp, vp, vp, vp]
@@ -824,13 +824,13 @@ def _want_in_place(outputs, inputs, allowed):
 
 
 def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=False, dx=None, dweight=None, dbias=None,
-                 workspace=None, stream=None):
+                 workspace=None, status=None, stream=None):
     """Gradient of psa_norm: x is what was normalised (`total` where there was a residual), d_total, if given, the gradient
     that reaches it by the residual stream.  Returns (dx, dweight, dbias), dbias None unless with_bias; dx is the gradient of
     x and of residual, and may be d_out, d_total or x."""
     fast = _fast(stream) if dx is None and dweight is None and dbias is None else None
     if fast:
-        got = fast.norm_bwd(d_out, x, weight, stats, rms, d_total, with_bias, workspace)
+        got = fast.norm_bwd(d_out, x, weight, stats, rms, d_total, with_bias, workspace, status)
         if type(got) is tuple:
             return got if with_bias else got + (None,)
         if got is not None:
@@ -844,6 +844,7 @@ def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=Fal
     if rms and (with_bias or dbias is not None):
         raise ValueError("dbias: the root-mean-square form has no bias")
     _want_given(given)
+    _want_status(status)
     dx = torch.empty_like(x) if dx is None else dx
     dweight = torch.empty_like(weight) if dweight is None else dweight
     outputs = [("dx", dx, (T, D), x.dtype), ("dweight", dweight, (D,), weight.dtype)]
@@ -856,7 +857,7 @@ def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=Fal
     need = lib.psa_norm_bwd_workspace_bytes(T, D)
     workspace = _scratch(workspace, need, x, stream)
     _check("psa_norm_bwd", lib.psa_norm_bwd(_ptr(d_out), _ptr(x), _ptr(weight), _ptr(stats), _ptr(d_total), dtype, wtype, T, D,
-                                            1 if rms else 0, _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                                            1 if rms else 0, _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(workspace), _ptr(status),
                                             _stream(stream)))
     return dx, dweight, dbias
 

@@ -12,6 +12,7 @@
 
 #include "psa.h"
 #include "psa_internal.h"
+#include "psa_launch.cuh"
 #include "psa_vector.cuh"
 
 namespace psa {
@@ -22,27 +23,34 @@ using namespace dev;
 constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------- forward
-// A CTA writes `rows` consecutive tokens' rows, V elements a load.
-template <typename T, int V>
+// A CTA writes `rows` consecutive tokens' rows, 16 bytes at a time: `windows` of them hold a row wherever it starts.
+template <typename T, bool kRagged>
 __global__ void __launch_bounds__(kThreads)
-embed_kernel(const int32_t* ids, const T* table, int64_t n_tokens, int64_t vocab, int32_t hidden, int32_t rows, float scale,
-             T* out, int32_t* status) {
+embed_kernel(const int32_t* ids, const T* table, int64_t n_tokens, int64_t vocab, int32_t hidden, int32_t windows, int32_t rows,
+             float scale, T* out, int32_t* status) {
+  constexpr int V = 16 / int(sizeof(T));
   const int64_t t0 = int64_t(blockIdx.x) * rows;
-  const int n_vec = hidden / V, n = int(min(int64_t(rows), n_tokens - t0)) * n_vec;
+  const int n = int(min(int64_t(rows), n_tokens - t0)) * windows;
+  behind_wait();
+  behind_go();
   for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int r = i / n_vec, c = (i - r * n_vec) * V;
+    const int r = i / windows, k = i - r * windows;
+    const int64_t at = (t0 + r) * hidden;
+    const int col = k * V - (kRagged ? int(at & (V - 1)) : 0);
+    if (col >= hidden) continue;
     const int32_t id = ids[t0 + r];
-    float v[V];
+    float v[V] = {};
     if (id >= 0 && id < vocab) {
-      load_vec<T, V>(table + int64_t(id) * hidden + c).get(v);
+      const int64_t from = int64_t(id) * hidden + col;
+      Span<T, V, kRagged> in;
+      in.load(table, from, vocab * hidden);
+      in.at(from).get(v);
 #pragma unroll
       for (int j = 0; j < V; ++j) v[j] *= scale;
-    } else {   // reported; the row is zeros
-      if (c == 0 && status) atomicOr(status, PSA_DEVSTAT_BAD_TARGET);
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = 0.f;
+    } else if (k == 0 && status) {   // reported; the row is zeros
+      atomicOr(status, PSA_DEVSTAT_BAD_TARGET);
     }
-    store_vec<T, V>(out + (t0 + r) * hidden + c, v);
+    store_window(out, at + col, v, -col, hidden - col);
   }
 }
 
@@ -64,6 +72,8 @@ embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t 
   const int begin = int(min(first, int64_t(n_tokens))), end = int(min(first + share, int64_t(n_tokens)));
   int32_t* mine = counts + warp * bins;
   for (int i = threadIdx.x; i < 32 * bins; i += kIndexThreads) counts[i] = 0;
+  behind_wait();
+  behind_go();
   __syncthreads();
 
   int below = 0;
@@ -145,58 +155,77 @@ embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t 
 // The other CTAs write the rows of ids that do not occur (dense gradients only).  blockIdx.y: a slice of the columns.
 constexpr int kRun = 32, kZeroRows = 16, kUnroll = 4;
 
-template <typename XT, typename GT, int V>
+// A thread holds one window of V columns: of the row of the table that it adds to, so that what it writes is aligned.
+template <typename XT, typename GT, bool kRagged>
 __global__ void __launch_bounds__(kThreads)
 embed_sum_kernel(const XT* d_out, const int32_t* start, const int32_t* order, const int32_t* sorted_id, int32_t n_runs,
-                 int32_t vocab, int32_t hidden, float scale, int32_t accumulate, GT* dtable, float* partial) {
-  const int col = (int(blockIdx.y) * kThreads + int(threadIdx.x)) * V;
+                 int64_t n_tokens, int32_t vocab, int32_t hidden, int32_t windows, float scale, int32_t accumulate, GT* dtable,
+                 float* partial) {
+  constexpr int V = 16 / int(sizeof(XT)), W = 16 / int(sizeof(GT));
+  const int k = int(blockIdx.y) * kThreads + int(threadIdx.x);
+  behind_wait();
+  behind_go();
+  // The thread's first column in the row of id v (may be negative: elements of the row before).
+  auto column = [&](int64_t v) { return k * V - (kRagged ? int(v * hidden & (W - 1)) : 0); };
   if (int(blockIdx.x) >= n_runs) {
-    if (col >= hidden) return;
     const int64_t v0 = (int64_t(blockIdx.x) - n_runs) * kZeroRows;
-    float zero[V] = {};
-    for (int k = 0; k < kZeroRows && v0 + k < vocab; ++k)
-      if (start[v0 + k] == start[v0 + k + 1]) store_vec<GT, V>(dtable + (v0 + k) * hidden + col, zero);
+    const float zero[V] = {};
+    for (int r = 0; r < kZeroRows && v0 + r < vocab; ++r) {
+      const int col = column(v0 + r);
+      if (start[v0 + r] == start[v0 + r + 1] && col < hidden) store_window(dtable, (v0 + r) * hidden + col, zero, -col, hidden - col);
+    }
     return;
   }
-  __shared__ int32_t s_pos[kRun], s_id[kRun + 2];     // s_id: one before, the run, one after
+  const int lane = threadIdx.x & 31;
   const int n_valid = start[vocab], first = int(blockIdx.x) * kRun, n = min(kRun, n_valid - first);
   if (n <= 0) return;
-  if (threadIdx.x < kRun + 2) {
-    const int i = first + int(threadIdx.x) - 1;
-    s_id[threadIdx.x] = i >= 0 && i < n_valid ? sorted_id[i] : -1;
-  }
-  if (int(threadIdx.x) < n) s_pos[threadIdx.x] = order[first + threadIdx.x];
-  __syncthreads();
-  if (col >= hidden) return;
+  // Lane l holds the run's l-th token and its id; `ends`: the next token's id is another one.
+  const int mine = first + lane;
+  const int pos = lane < n ? order[mine] : 0, id = lane < n ? sorted_id[mine] : -1;
+  const unsigned ends = __ballot_sync(0xffffffffu, lane < n && (mine + 1 >= n_valid || sorted_id[mine + 1] != id));
+  bool began_here = first == 0 || sorted_id[first - 1] != __shfl_sync(0xffffffffu, id, 0);
   float acc[V] = {};
-  bool began_here = s_id[0] != s_id[1];
   for (int e0 = 0; e0 < n; e0 += kUnroll) {
-    Vec<XT, V> raw[kUnroll];
+    Span<XT, V, kRagged> raw[kUnroll];
+    int64_t from[kUnroll];
+    int col[kUnroll];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k)
-      if (e0 + k < n) raw[k] = load_vec<XT, V>(d_out + int64_t(s_pos[e0 + k]) * hidden + col);
+    for (int u = 0; u < kUnroll; ++u) {
+      col[u] = column(__shfl_sync(0xffffffffu, id, (e0 + u) & 31));
+      from[u] = int64_t(__shfl_sync(0xffffffffu, pos, (e0 + u) & 31)) * hidden + col[u];
+      if (e0 + u < n && col[u] < hidden) raw[u].load(d_out, from[u], n_tokens * hidden);
+    }
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-      const int e = e0 + k;
+    for (int u = 0; u < kUnroll; ++u) {
+      const int e = e0 + u;
       if (e >= n) break;
-      float x[V];
-      raw[k].get(x);
+      const int64_t v = __shfl_sync(0xffffffffu, id, e);
+      if (col[u] < hidden) {
+        float x[V];
+        raw[u].at(from[u]).get(x);
 #pragma unroll
-      for (int j = 0; j < V; ++j) acc[j] += x[j];
-      const int id = s_id[e + 1];
-      const bool ends = s_id[e + 2] != id;
-      if (!ends && e + 1 < n) continue;
-      if (ends && began_here) {
-        GT* row = dtable + int64_t(id) * hidden + col;
-        float old[V] = {};
-        if (accumulate) load_vec<GT, V>(row).get(old);
+        for (int j = 0; j < V; ++j) acc[j] += x[j];
+      }
+      const bool end = ends >> e & 1u;
+      if (!end && e + 1 < n) continue;
+      if (k < windows && col[u] < hidden) {
+        if (end && began_here) {
+          const int64_t to = v * hidden + col[u];
+          if (accumulate) {
+            Span<GT, V, kRagged> old;
+            float o[V];
+            old.load(dtable, to, int64_t(vocab) * hidden);
+            old.at(to).get(o);
 #pragma unroll
-        for (int j = 0; j < V; ++j) acc[j] = old[j] + scale * acc[j];
-        store_vec<GT, V>(row, acc);
-      } else {
-        float* p = partial + (int64_t(blockIdx.x) * 2 + (began_here ? 1 : 0)) * hidden + col;
+            for (int j = 0; j < V; ++j) acc[j] = o[j] + scale * acc[j];
+          } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) p[j] = acc[j];
+            for (int j = 0; j < V; ++j) acc[j] *= scale;
+          }
+          store_window(dtable, to, acc, -col[u], hidden - col[u]);
+        } else {
+          store_vec<float, V>(partial + ((int64_t(blockIdx.x) * 2 + (began_here ? 1 : 0)) * windows + k) * V, acc);
+        }
       }
 #pragma unroll
       for (int j = 0; j < V; ++j) acc[j] = 0.f;
@@ -206,29 +235,38 @@ embed_sum_kernel(const XT* d_out, const int32_t* start, const int32_t* order, co
 }
 
 // The ids that spread over several runs: the CTA of the run in which one begins adds the runs' sums in their order.
-template <typename GT, int V>
+template <typename GT, int V, bool kRagged>
 __global__ void __launch_bounds__(kThreads)
-embed_join_kernel(const int32_t* start, const int32_t* sorted_id, int32_t vocab, int32_t hidden, float scale, int32_t accumulate,
-                  const float* partial, GT* dtable) {
-  const int col = (int(blockIdx.y) * kThreads + int(threadIdx.x)) * V;
-  const int run = blockIdx.x, last = run * kRun + kRun - 1;
-  if (last >= start[vocab]) return;
+embed_join_kernel(const int32_t* start, const int32_t* sorted_id, int32_t vocab, int32_t hidden, int32_t windows, float scale,
+                  int32_t accumulate, const float* partial, GT* dtable) {
+  constexpr int W = 16 / int(sizeof(GT));
+  const int k = int(blockIdx.y) * kThreads + int(threadIdx.x), run = blockIdx.x, last = run * kRun + kRun - 1;
+  behind_wait();
+  behind_go();
+  if (k >= windows || last >= start[vocab]) return;
   const int id = sorted_id[last], from = start[id], to = start[id + 1];
-  if (from < run * kRun || to <= last + 1 || col >= hidden) return;
-  const int last_run = (to - 1) / kRun;
+  if (from < run * kRun || to <= last + 1) return;
+  const int64_t row = int64_t(id) * hidden;
+  const int col = k * V - (kRagged ? int(row & (W - 1)) : 0), last_run = (to - 1) / kRun;
+  if (col >= hidden) return;
   float acc[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) acc[j] = partial[(int64_t(run) * 2 + 1) * hidden + col + j];
+  load_vec<float, V>(partial + ((int64_t(run) * 2 + 1) * windows + k) * V).get(acc);
 #pragma unroll 8
-  for (int r = run + 1; r <= last_run; ++r)
+  for (int r = run + 1; r <= last_run; ++r) {
+    float v[V];
+    load_vec<float, V>(partial + (int64_t(r) * 2 * windows + k) * V).get(v);
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] += partial[int64_t(r) * 2 * hidden + col + j];
-  GT* row = dtable + int64_t(id) * hidden + col;
+    for (int j = 0; j < V; ++j) acc[j] += v[j];
+  }
   float old[V] = {};
-  if (accumulate) load_vec<GT, V>(row).get(old);
+  if (accumulate) {
+    Span<GT, V, kRagged> in;
+    in.load(dtable, row + col, int64_t(vocab) * hidden);
+    in.at(row + col).get(old);
+  }
 #pragma unroll
   for (int j = 0; j < V; ++j) acc[j] = old[j] + scale * acc[j];
-  store_vec<GT, V>(row, acc);
+  store_window(dtable, row + col, acc, -col, hidden - col);
 }
 
 // ---------------------------------------------------------------- host
@@ -248,7 +286,7 @@ EmbedWorkspace workspace_layout(int64_t T, int64_t vocab, int64_t hidden) {
   w.sorted_id = at;
   at += aligned(size_t(T) * 4);
   w.partial = at;
-  w.total = at + size_t((T + kRun - 1) / kRun) * 2 * size_t(hidden) * 4;
+  w.total = at + size_t((T + kRun - 1) / kRun) * 2 * size_t(hidden / 8 + 2) * 8 * 4;
   return w;
 }
 
@@ -259,38 +297,44 @@ psa_status_t check_sizes(int64_t n_tokens, int64_t vocab, int32_t hidden) {
 }
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
-template <typename T, int V>
+// Windows of V columns that a row reaches into; where its width is no multiple of V, it starts up to `align` - 1 elements into
+// the first one.
+int windows_of(int32_t hidden, int V, int align) { return hidden % V ? (hidden + align - 1 + V - 1) / V : hidden / V; }
+
+template <typename T, bool kRagged>
 psa_status_t embed_fwd(const int32_t* ids, const void* table, int64_t n_tokens, int64_t vocab, int32_t hidden, float scale,
                        void* out, int32_t* status, cudaStream_t stream) {
-  const int rows = std::max(1, 2 * kThreads / (hidden / V));    // two loads a thread
-  embed_kernel<T, V><<<unsigned((n_tokens + rows - 1) / rows), kThreads, 0, stream>>>(
-      ids, static_cast<const T*>(table), n_tokens, vocab, hidden, rows, scale, static_cast<T*>(out), status);
+  constexpr int V = 16 / int(sizeof(T));
+  const int windows = windows_of(hidden, V, V), rows = std::max(1, 2 * kThreads / windows);    // two loads a thread
+  launch_behind(true, embed_kernel<T, kRagged>, dim3(unsigned((n_tokens + rows - 1) / rows)), kThreads, 0, stream, ids,
+                static_cast<const T*>(table), n_tokens, vocab, hidden, windows, rows, scale, static_cast<T*>(out), status);
   return check_last_cuda_error("psa_embed launch");
 }
 
-template <typename XT, typename GT, int V>
+template <typename XT, typename GT, bool kRagged>
 psa_status_t embed_bwd(const void* d_out, const int32_t* ids, int64_t n_tokens, int64_t vocab, int32_t hidden, float scale,
                        int32_t accumulate, void* dtable, char* ws, int32_t* status, cudaStream_t stream) {
+  constexpr int V = 16 / int(sizeof(XT));
   const EmbedWorkspace w = workspace_layout(n_tokens, vocab, hidden);
   auto ints = [&](size_t off) { return reinterpret_cast<int32_t*>(ws + off); };
   // A range of ids per SM, of at least 32 and at most kMaxBins ids.
   const int bins = int(std::min<int64_t>(kMaxBins, std::max<int64_t>(32, (vocab + 147) / 148)));
-  const int smem = 32 * bins * 4;
   if (cudaFuncSetAttribute(embed_index_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * kMaxBins * 4) != cudaSuccess)
     return PSA_ERR_CUDA;
-  embed_index_kernel<<<unsigned((vocab + bins - 1) / bins), kIndexThreads, smem, stream>>>(
-      ids, int32_t(n_tokens), int32_t(vocab), bins, ints(w.start), ints(w.order), ints(w.sorted_id), status);
+  launch_behind(true, embed_index_kernel, dim3(unsigned((vocab + bins - 1) / bins)), kIndexThreads, size_t(32) * bins * 4, stream,
+                ids, int32_t(n_tokens), int32_t(vocab), bins, ints(w.start), ints(w.order), ints(w.sorted_id), status);
   const int n_runs = int((n_tokens + kRun - 1) / kRun);
-  const unsigned slices = unsigned((hidden + kThreads * V - 1) / (kThreads * V));
+  const int windows = windows_of(hidden, V, 16 / int(sizeof(GT)));
+  const unsigned slices = unsigned((windows + kThreads - 1) / kThreads);
   const unsigned zero = accumulate ? 0u : unsigned((vocab + kZeroRows - 1) / kZeroRows);
   float* partial = reinterpret_cast<float*>(ws + w.partial);
   if (n_runs + zero > 0)
-    embed_sum_kernel<XT, GT, V><<<dim3(unsigned(n_runs) + zero, slices), kThreads, 0, stream>>>(
-        static_cast<const XT*>(d_out), ints(w.start), ints(w.order), ints(w.sorted_id), n_runs, int32_t(vocab), hidden, scale,
-        accumulate, static_cast<GT*>(dtable), partial);
+    launch_behind(true, embed_sum_kernel<XT, GT, kRagged>, dim3(unsigned(n_runs) + zero, slices), kThreads, 0, stream,
+                  static_cast<const XT*>(d_out), ints(w.start), ints(w.order), ints(w.sorted_id), n_runs, n_tokens, int32_t(vocab),
+                  hidden, windows, scale, accumulate, static_cast<GT*>(dtable), partial);
   if (n_runs > 1)
-    embed_join_kernel<GT, V><<<dim3(unsigned(n_runs), slices), kThreads, 0, stream>>>(
-        ints(w.start), ints(w.sorted_id), int32_t(vocab), hidden, scale, accumulate, partial, static_cast<GT*>(dtable));
+    launch_behind(true, embed_join_kernel<GT, V, kRagged>, dim3(unsigned(n_runs), slices), kThreads, 0, stream, ints(w.start),
+                  ints(w.sorted_id), int32_t(vocab), hidden, windows, scale, accumulate, partial, static_cast<GT*>(dtable));
   return check_last_cuda_error("psa_embed_bwd launch");
 }
 
@@ -307,14 +351,10 @@ extern "C" psa_status_t psa_embed(const int32_t* token_ids, const void* table, i
   if (!token_ids || !table || !out) return PSA_ERR_INVALID_ARG;
   if (misaligned(table, 16) || misaligned(out, 16) || misaligned(token_ids, 4)) return PSA_ERR_ALIGNMENT;
   cudaStream_t st = cudaStream_t(stream);
-  if (dtype == PSA_DTYPE_F32) {
-    if (hidden % 4 == 0) return embed_fwd<float, 4>(token_ids, table, n_tokens, vocab, hidden, scale, out, device_status, st);
-    if (hidden % 2 == 0) return embed_fwd<float, 2>(token_ids, table, n_tokens, vocab, hidden, scale, out, device_status, st);
-    return embed_fwd<float, 1>(token_ids, table, n_tokens, vocab, hidden, scale, out, device_status, st);
-  }
-  if (hidden % 8 == 0) return embed_fwd<__nv_bfloat16, 8>(token_ids, table, n_tokens, vocab, hidden, scale, out, device_status, st);
-  if (hidden % 2 == 0) return embed_fwd<__nv_bfloat16, 2>(token_ids, table, n_tokens, vocab, hidden, scale, out, device_status, st);
-  return embed_fwd<__nv_bfloat16, 1>(token_ids, table, n_tokens, vocab, hidden, scale, out, device_status, st);
+  const bool f32 = dtype == PSA_DTYPE_F32, ragged = hidden * (f32 ? 4 : 2) % 16 != 0;
+  auto run = f32 ? (ragged ? embed_fwd<float, true> : embed_fwd<float, false>)
+                 : (ragged ? embed_fwd<__nv_bfloat16, true> : embed_fwd<__nv_bfloat16, false>);
+  return run(token_ids, table, n_tokens, vocab, hidden, scale, out, device_status, st);
 }
 
 extern "C" size_t psa_embed_bwd_workspace_bytes(int64_t n_tokens, int64_t vocab, int32_t hidden) {
@@ -335,10 +375,9 @@ extern "C" psa_status_t psa_embed_bwd(const void* d_out, const int32_t* token_id
   if (misaligned(d_out, 16) || misaligned(dtable, 16) || misaligned(workspace, 16) || misaligned(token_ids, 4)) return PSA_ERR_ALIGNMENT;
   char* ws = static_cast<char*>(workspace);
   cudaStream_t st = cudaStream_t(stream);
-#define PSA_EMBED_BWD(XT, GT, V) embed_bwd<XT, GT, V>(d_out, token_ids, n_tokens, vocab, hidden, scale, accumulate, dtable, ws, device_status, st)
-  if (f32) return hidden % 4 == 0 ? PSA_EMBED_BWD(float, float, 4) : hidden % 2 == 0 ? PSA_EMBED_BWD(float, float, 2) : PSA_EMBED_BWD(float, float, 1);
-  if (grad_dtype == PSA_DTYPE_F32)
-    return hidden % 8 == 0 ? PSA_EMBED_BWD(__nv_bfloat16, float, 8) : hidden % 2 == 0 ? PSA_EMBED_BWD(__nv_bfloat16, float, 2) : PSA_EMBED_BWD(__nv_bfloat16, float, 1);
-  return hidden % 8 == 0 ? PSA_EMBED_BWD(__nv_bfloat16, __nv_bfloat16, 8) : hidden % 2 == 0 ? PSA_EMBED_BWD(__nv_bfloat16, __nv_bfloat16, 2) : PSA_EMBED_BWD(__nv_bfloat16, __nv_bfloat16, 1);
-#undef PSA_EMBED_BWD
+  const bool to_f32 = grad_dtype == PSA_DTYPE_F32, ragged = hidden * (f32 ? 4 : 2) % 16 != 0;
+  auto run = f32      ? (ragged ? embed_bwd<float, float, true> : embed_bwd<float, float, false>)
+             : to_f32 ? (ragged ? embed_bwd<__nv_bfloat16, float, true> : embed_bwd<__nv_bfloat16, float, false>)
+                      : (ragged ? embed_bwd<__nv_bfloat16, __nv_bfloat16, true> : embed_bwd<__nv_bfloat16, __nv_bfloat16, false>);
+  return run(d_out, token_ids, n_tokens, vocab, hidden, scale, accumulate, dtable, ws, device_status, st);
 }

@@ -445,15 +445,15 @@ PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// norm_bwd(d_out, x, weight, stats, rms, d_total, with_bias, workspace) -> (dx, dweight) or (dx, dweight, dbias), a status
+// norm_bwd(d_out, x, weight, stats, rms, d_total, with_bias, workspace, status) -> (dx, dweight) or (dx, dweight, dbias), a status
 // code (not 0), or None
 PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     NormArgs m;
     bool rms, with_bias;
-    void *d_out, *stats, *d_total;
+    void *d_out, *stats, *d_total, *word;
     at::Tensor ws;
-    if (n != 8 || !modes_off() || !take_norm(a[1], a[2], &m) || !take_bool(a[4], &rms) || !take_bool(a[6], &with_bias) ||
+    if (n != 9 || !take_status(a[8], &word) || !modes_off() || !take_norm(a[1], a[2], &m) || !take_bool(a[4], &rms) || !take_bool(a[6], &with_bias) ||
         a[0] == Py_None || !take_optional(a[0], m.x->scalar_type(), {m.T, m.hidden}, &d_out) || a[3] == Py_None ||
         !take_optional(a[3], at::kFloat, {2, m.T}, &stats) ||
         !take_optional(a[5], m.x->scalar_type(), {m.T, m.hidden}, &d_total) || (rms && with_bias) ||
@@ -466,7 +466,7 @@ PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void *const tb = with_bias ? db.data_ptr() : nullptr, *const scratch = ws.data_ptr(), *const on = stream();
     const psa_status_t rc = unlocked([&] {
       return g_lib.norm_bwd(d_out, x, w, static_cast<float*>(stats), d_total, m.dtype, m.wtype, m.T, int32_t(m.hidden), rms, to,
-                            tw, tb, scratch, on);
+                            tw, tb, scratch, static_cast<int32_t*>(word), on);
     });
     if (rc != PSA_OK) return PyLong_FromLong(rc);
     return with_bias ? tuple_of(dx, dw, db) : tuple_of(dx, dw);

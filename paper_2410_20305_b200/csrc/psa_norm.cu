@@ -5,7 +5,7 @@
 //     ds = r * (g - u * mean(g u) - mean(g)) + d_total      (no mean(g) in the RMS form),
 //     dw = sum over tokens of dy * u,   db = sum over tokens of dy.
 // Bound by HBM: a row is read once into registers, its sums are taken from there (the variance after the mean, so a row far
-// from 0 loses nothing), and it is written once.  Sums are fp32.
+// from 0 loses nothing), and it is written once.  Sums are fp32.  Rows of any width are moved 16 bytes at a time (psa_vector.cuh).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -13,7 +13,9 @@
 #include <algorithm>
 
 #include "psa.h"
+#include "psa_device.cuh"
 #include "psa_internal.h"
+#include "psa_launch.cuh"
 #include "psa_vector.cuh"
 
 namespace psa {
@@ -25,10 +27,14 @@ constexpr int kSmCount = 148;
 constexpr int kMaxHidden = 16384;
 constexpr int kRowsPerCta = 8;      // rows of a CTA where a warp holds a row
 
-// The most threads that divide() below gives a CTA, for the compiler's share of registers.
-template <int V, int NV, bool kWarp>
+// The most threads that divide() and divide_bwd() below give a CTA.
+template <typename XT, int NV, bool kWarp>
 constexpr int max_threads() {
-  return kWarp ? 32 * kRowsPerCta : V == 1 ? 1024 : NV < 4 ? 256 : kMaxHidden / (V * NV);
+  return kWarp ? 32 * kRowsPerCta : NV < 4 ? 256 : std::min(1024, kMaxHidden / (16 / int(sizeof(XT)) * NV) + 32);
+}
+template <typename XT, int NV, bool kWarp>
+constexpr int bwd_threads() {
+  return kWarp ? 32 * kRowsPerCta : NV * 16 / int(sizeof(XT)) < 32 ? 512 : 544;
 }
 
 // Sum over the threads that share a row: a warp (kWarp) or the CTA.  `slot` alternates, so that one barrier is enough.
@@ -45,57 +51,74 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*s_part)[32], int 
   for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < n_warps ? s_part[slot * 2 + i][lane] : 0.f);
 }
 
-template <typename XT, typename WT, int V, int NV, bool kWarp>
-__global__ void __launch_bounds__(max_threads<V, NV, kWarp>())
+// A thread's columns in a row that starts `a` elements behind an aligned one: window k holds the columns [k V - a, (k + 1) V - a).
+template <typename XT, typename WT, int NV, bool kWarp, bool kRagged>
+__global__ void __launch_bounds__(max_threads<XT, NV, kWarp>())
 norm_kernel(const XT* x, const XT* residual, const WT* weight, const WT* bias, int64_t n_tokens, int32_t hidden, float eps,
             int32_t rms, XT* out, XT* total, float* stats) {
+  constexpr int V = 16 / int(sizeof(XT));
+  using Weight = Span<WT, V, kRagged>;
   __shared__ float s_part[4][32];
   const int group = kWarp ? 32 : int(blockDim.x), tid = kWarp ? int(threadIdx.x) & 31 : int(threadIdx.x);
   const int64_t row = kWarp ? int64_t(blockIdx.x) * kRowsPerCta + (threadIdx.x >> 5) : int64_t(blockIdx.x);
+  behind_wait();
+  behind_go();
   if (kWarp && row >= n_tokens) return;
-  const int64_t at = row * hidden;
-  float s[NV][V];
+  const int64_t at = row * hidden, all = n_tokens * hidden;
+  const int a = kRagged ? int(at & (V - 1)) : 0;
+  uint4 rx[NV], rr[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int col = (i * group + tid) * V;
-    if (col < hidden) {
-      load_vec<XT, V>(x + at + col).get(s[i]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) s[i][j] = 0.f;
-    }
+    const int col = (i * group + tid) * V - a;
+    if (col >= hidden) continue;
+    rx[i] = kRagged ? load_window(x, at + col, all) : *reinterpret_cast<const uint4*>(x + at + col);
+    if (residual) rr[i] = kRagged ? load_window(residual, at + col, all) : *reinterpret_cast<const uint4*>(residual + at + col);
   }
-  if (residual) {
+  float s[NV][V], sum[1] = {0.f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int col = (i * group + tid) * V;
-      if (col >= hidden) continue;
+  for (int i = 0; i < NV; ++i) {
+    const int col = (i * group + tid) * V - a;
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[i][j] = 0.f;
+    if (col >= hidden) continue;
+    Vec<XT, V> v;
+    memcpy(&v, &rx[i], 16);
+    v.get(s[i]);
+    if (residual) {
       float r[V];
-      load_vec<XT, V>(residual + at + col).get(r);
+      memcpy(&v, &rr[i], 16);
+      v.get(r);
 #pragma unroll
       for (int j = 0; j < V; ++j) s[i][j] += r[j];
-      Vec<XT, V> w;     // what is normalised is what the residual stream holds
-      w.set(s[i]);
-      *reinterpret_cast<Vec<XT, V>*>(total + at + col) = w;
-      w.get(s[i]);
+      v.set(s[i]);     // what is normalised is what the residual stream holds
+      v.get(s[i]);
+      store_window(total, at + col, s[i], -col, hidden - col);
     }
+    if (kRagged && (col < 0 || col + V > hidden))
+#pragma unroll
+      for (int j = 0; j < V; ++j) s[i][j] = col + j >= 0 && col + j < hidden ? s[i][j] : 0.f;
+    if (!rms)
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[0] += s[i][j];
   }
   float mean = 0.f;
   if (!rms) {
-    float sum[1] = {0.f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < V; ++j) sum[0] += s[i][j];
     row_sum<kWarp>(sum, s_part, 0);
     mean = sum[0] / float(hidden);
   }
   float sq[1] = {0.f};
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    if ((i * group + tid) * V >= hidden) continue;
+    const int col = (i * group + tid) * V - a;
+    if (col >= hidden) continue;
+    if (kRagged && (col < 0 || col + V > hidden)) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) sq[0] += (s[i][j] - mean) * (s[i][j] - mean);
+      for (int j = 0; j < V; ++j)
+        if (col + j >= 0 && col + j < hidden) sq[0] += (s[i][j] - mean) * (s[i][j] - mean);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) sq[0] += (s[i][j] - mean) * (s[i][j] - mean);
+    }
   }
   row_sum<kWarp>(sq, s_part, 1);
   const float rstd = 1.0f / sqrtf(sq[0] / float(hidden) + eps);
@@ -105,111 +128,284 @@ norm_kernel(const XT* x, const XT* residual, const WT* weight, const WT* bias, i
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int col = (i * group + tid) * V;
+    const int col = (i * group + tid) * V - a;
     if (col >= hidden) continue;
+    Weight ww, wb;
     float w[V], b[V], y[V];
-    load_vec<WT, V>(weight + col).get(w);
-    if (bias) load_vec<WT, V>(bias + col).get(b);
+    ww.load(weight, col, hidden);
+    if (bias) wb.load(bias, col, hidden);
+    ww.at(col).get(w);
+    wb.at(col).get(b);
 #pragma unroll
     for (int j = 0; j < V; ++j) y[j] = (s[i][j] - mean) * rstd * w[j] + (bias ? b[j] : 0.f);
-    store_vec<XT, V>(out + at + col, y);
+    store_window(out, at + col, y, -col, hidden - col);
   }
 }
 
-// A CTA takes every gridDim.x-th row (or set of rows); a thread keeps its columns, and their parts of dw and db, throughout.
-// partial: [gridDim.x][2][hidden].
-template <typename XT, typename WT, int V, int NV, bool kWarp>
-__global__ void __launch_bounds__(max_threads<V, NV, kWarp>())
+// V elements of a tile in shared memory, `a` elements behind a 16-byte boundary.
+template <typename T, bool kRagged>
+__device__ __forceinline__ Vec<T, 16 / int(sizeof(T))> shared_vec(const T* p, int a) {
+  constexpr int V = 16 / int(sizeof(T));
+  if (!kRagged) return load_vec<T, V>(p);
+  const uint4* q = reinterpret_cast<const uint4*>(p - a);
+  const uint4 w = shift_pair<int(sizeof(T))>(q[0], q[1], a);
+  Vec<T, V> v;
+  memcpy(&v, &w, 16);
+  return v;
+}
+template <typename T, int V>
+__device__ __forceinline__ void zero_behind(Vec<T, V>& v, int n) {
+  float f[V];
+  v.get(f);
+#pragma unroll
+  for (int j = 0; j < V; ++j) f[j] = j < n ? f[j] : 0.f;
+  v.set(f);
+}
+// V floats as pairs for packed arithmetic.
+template <typename T, int V>
+__device__ __forceinline__ void pairs(const Vec<T, V>& v, uint64_t (&p)[V / 2]) {
+  float f[V];
+  v.get(f);
+#pragma unroll
+  for (int j = 0; j < V / 2; ++j) p[j] = pack_f32x2(f[2 * j], f[2 * j + 1]);
+}
+
+// The backward.  A CTA takes every gridDim.x-th tile of rows: one row for all its threads, or, of narrow rows, some for each of
+// its warps.  Tiles are contiguous in memory and come by bulk copies into a ring of stages, so that several are in flight
+// whatever the arithmetic waits for (31041 x 4096 bf16 with d_total: 346 us with loads where the values are used, 253 with the
+// next row's in registers, @NB@ so).  For the sums over tokens a thread keeps its columns [k V, (k + 1) V) throughout; of dx it
+// writes window k of each row (the same columns where rows are aligned).  partial: [gridDim.x][2][hidden].
+struct BwdShape {
+  int32_t rows, stages;                   // rows of a tile; tiles in flight
+  int32_t staged;                         // tensors that come by the ring: x, d_out and, where there is room, d_total
+  uint32_t slot_bytes, w_bytes;           // of a tile of one tensor; of the weight with zeros around it
+};
+constexpr uint32_t kWeightPad = 64;       // zeros in front of the weight and behind it
+
+template <typename XT, typename WT, int NV, bool kWarp, bool kRagged>
+__global__ void __launch_bounds__(bwd_threads<XT, NV, kWarp>())
 norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* stats, const XT* d_total, int64_t n_tokens,
-                int32_t hidden, int32_t rms, XT* dx, float* partial) {
+                int32_t hidden, int32_t rms, XT* dx, float* partial, BwdShape shape, int32_t* status) {
+  constexpr int V = 16 / int(sizeof(XT)), kE = int(sizeof(XT));
+  constexpr bool kKeep = !kRagged && NV * V <= 16;
+  extern __shared__ uint8_t smem_raw[];        // [stages][2 or 3 tensors][slot], weight, [2][hidden] sums (over the stages, at the end)
   __shared__ float s_part[4][32];
-  extern __shared__ float s_sum[];    // [2][hidden], kWarp only
-  const int group = kWarp ? 32 : int(blockDim.x), tid = kWarp ? int(threadIdx.x) & 31 : int(threadIdx.x);
-  const int rows = kWarp ? kRowsPerCta : 1, mine = kWarp ? int(threadIdx.x) >> 5 : 0;
-  float dw[NV][V], db[NV][V], w[NV][V];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int col = (i * group + tid) * V;
-#pragma unroll
-    for (int j = 0; j < V; ++j) dw[i][j] = db[i][j] = w[i][j] = 0.f;
-    if (col < hidden) load_vec<WT, V>(weight + col).get(w[i]);
+  __shared__ uint64_t s_bar[8];
+  __shared__ int s_abort;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int group = kWarp ? 32 : int(blockDim.x), tid = kWarp ? lane : int(threadIdx.x);
+  const uint32_t base = (smem_u32(smem_raw) + 15u) & ~15u, n_tensors = uint32_t(shape.staged);
+  uint8_t* ring = smem_raw + (base - smem_u32(smem_raw));
+  uint8_t* s_weight = ring + uint32_t(shape.stages) * n_tensors * shape.slot_bytes + kWeightPad;
+  const WaitCtx wctx{&s_abort, status, kWaitLimitClocks};
+  const int64_t all = n_tokens * hidden, tile_elems = int64_t(shape.rows) * hidden, n_tiles = (n_tokens + shape.rows - 1) / shape.rows;
+
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int s = 0; s < shape.stages; ++s) mbar_init(smem_u32(&s_bar[s]), 1);
+    fence_mbar_init();
   }
+  behind_wait();
+  behind_go();
+  for (int i = threadIdx.x; i < int(shape.w_bytes / 4); i += blockDim.x)
+    reinterpret_cast<uint32_t*>(s_weight - kWeightPad)[i] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < hidden; i += blockDim.x) reinterpret_cast<WT*>(s_weight)[i] = weight[i];
+
+  // One thread requests a tile: from the 16-byte boundary at or before its first element to the one at or behind its last; the
+  // tensor's last elements, if no boundary follows them within it, by hand.
+  auto request = [&](int64_t tile, int stage) {
+    const int64_t first = tile * tile_elems, from = first & ~int64_t(V - 1);
+    if (!kRagged) {      // whole rows are whole vectors
+      const uint32_t n = uint32_t(min(tile_elems, all - first)) * kE, bar = smem_u32(&s_bar[stage]);
+      uint32_t to = base + uint32_t(stage) * n_tensors * shape.slot_bytes;
+      mbar_expect_tx(bar, n_tensors * n);
+      bulk_load(to, x + first, n, bar);
+      bulk_load(to + shape.slot_bytes, d_out + first, n, bar);
+      if (n_tensors == 3) bulk_load(to + 2 * shape.slot_bytes, d_total + first, n, bar);
+      return;
+    }
+    const int64_t end = min(all, first + tile_elems), to = min(all & ~int64_t(V - 1), (end + V - 1) & ~int64_t(V - 1));
+    const uint32_t bytes = to > from ? uint32_t(to - from) * kE : 0u, bar = smem_u32(&s_bar[stage]);
+    for (uint32_t t = 0; t < n_tensors; ++t) {
+      const XT* src = t == 0 ? x : t == 1 ? d_out : d_total;
+      XT* slot = reinterpret_cast<XT*>(ring + (uint32_t(stage) * n_tensors + t) * shape.slot_bytes);
+      for (int64_t e = max(to, from); e < end; ++e) slot[e - from] = src[e];
+    }
+    mbar_expect_tx(bar, n_tensors * bytes);
+    if (bytes)
+      for (uint32_t t = 0; t < n_tensors; ++t) {
+        const XT* src = t == 0 ? x : t == 1 ? d_out : d_total;
+        bulk_load(base + (uint32_t(stage) * n_tensors + t) * shape.slot_bytes, src + from, bytes, bar);
+      }
+  };
+  int64_t asked = blockIdx.x;     // the next tile to request, and how many have been (thread 0's)
+  int n_asked = 0;
+  if (threadIdx.x == 0)
+    for (int s = 0; s < shape.stages && asked < n_tiles; ++s, asked += gridDim.x, ++n_asked) request(asked, s);
+  __syncthreads();
+
+  uint64_t dw[NV][V / 2], db[NV][V / 2];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) dw[i][j] = db[i][j] = 0;
   const float inv = 1.0f / float(hidden);
-  int slot = 0;
-  for (int64_t row = int64_t(blockIdx.x) * rows + mine; row < n_tokens; row += int64_t(gridDim.x) * rows, slot ^= 1) {
-    const int64_t at = row * hidden;
-    const float mean = stats[row], rstd = stats[n_tokens + row];
-    float u[NV][V], g[NV][V], sum[2] = {0.f, 0.f};
+  int stage = 0, turn = 0, slot = 0, before = -1;     // before: the stage that the last tile was in
+  float next_mean = 0.f, next_rstd = 0.f;             // of the row after this one
+  auto fetch_stats = [&](int64_t row) {
+    if (row >= n_tokens) return;
+    next_mean = stats[row];
+    next_rstd = stats[n_tokens + row];
+  };
+  const int first_r = kWarp ? warp : 0;
+  fetch_stats(int64_t(blockIdx.x) * shape.rows + first_r);
+  for (int64_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
+    mbar_wait(smem_u32(&s_bar[stage]), turn & 1, wctx);
+    const uint8_t* tx = ring + uint32_t(stage) * n_tensors * shape.slot_bytes;
+    const int64_t row0 = tile * shape.rows;
+    const int n_rows = int(min(int64_t(shape.rows), n_tokens - row0));
+    const int lead = kRagged ? int(row0 * hidden & (V - 1)) : 0;      // elements in front of the tile in its slot
+    for (int r = first_r; r < n_rows; r += kWarp ? kRowsPerCta : 1, slot ^= 1) {
+      const int64_t row = row0 + r, at = row * hidden;
+      const int o = lead + r * hidden, a = kRagged ? o & (V - 1) : 0;
+      const XT *sx = reinterpret_cast<const XT*>(tx) + o, *sg = reinterpret_cast<const XT*>(tx + shape.slot_bytes) + o;
+      const XT* sd = reinterpret_cast<const XT*>(tx + 2 * shape.slot_bytes) + o;
+      const float mean = next_mean, rstd = next_rstd;
+      fetch_stats(kWarp && r + kRowsPerCta < n_rows ? row + kRowsPerCta : (tile + gridDim.x) * shape.rows + first_r);
+      // u = x rstd - mean rstd, in pairs
+      const uint64_t r2 = pack_f32x2(rstd, rstd), m2 = pack_f32x2(-mean * rstd, -mean * rstd);
+      uint64_t sum_u = 0, sum_1 = 0;
+      uint64_t ku[kKeep ? NV : 1][V / 2], kg[kKeep ? NV : 1][V / 2];     // u and g w, where there are registers for them
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int col = (i * group + tid) * V;
-      if (col < hidden) {
-        load_vec<XT, V>(x + at + col).get(u[i]);
-        load_vec<XT, V>(d_out + at + col).get(g[i]);
-      } else {
+      for (int i = 0; i < NV; ++i) {
+        const int col = (i * group + tid) * V;
+        if (col >= hidden) continue;
+        Vec<XT, V> px = shared_vec<XT, kRagged>(sx + col, a), pg = shared_vec<XT, kRagged>(sg + col, a);
+        if (kRagged && col + V > hidden) {    // what follows the row
+          zero_behind(px, hidden - col);
+          zero_behind(pg, hidden - col);
+        }
+        uint64_t u[V / 2], g[V / 2], wp[V / 2];
+        pairs(px, u);
+        pairs(pg, g);
+        pairs(load_vec<WT, V>(reinterpret_cast<const WT*>(s_weight) + col), wp);
 #pragma unroll
-        for (int j = 0; j < V; ++j) { u[i][j] = mean; g[i][j] = 0.f; }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        u[i][j] = (u[i][j] - mean) * rstd;
-        dw[i][j] += g[i][j] * u[i][j];
-        db[i][j] += g[i][j];
-        g[i][j] *= w[i][j];
-        sum[0] += g[i][j] * u[i][j];
-        sum[1] += g[i][j];
-      }
-    row_sum<kWarp>(sum, s_part, slot);
-    const float c_u = sum[0] * inv, c_1 = rms ? 0.f : sum[1] * inv;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int col = (i * group + tid) * V;
-      if (col >= hidden) continue;
-      float d[V];
-#pragma unroll
-      for (int j = 0; j < V; ++j) d[j] = (g[i][j] - u[i][j] * c_u - c_1) * rstd;
-      if (d_total) {
-        float t[V];
-        load_vec<XT, V>(d_total + at + col).get(t);
-#pragma unroll
-        for (int j = 0; j < V; ++j) d[j] += t[j];
-      }
-      store_vec<XT, V>(dx + at + col, d);
-    }
-  }
-  float* mine_dw = partial + int64_t(blockIdx.x) * 2 * hidden;
-  if (kWarp) {   // the rows of a CTA are added in their order
-    for (int k = 0; k < kRowsPerCta; ++k) {
-      if (k == mine) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int col = (i * group + tid) * V;
-          if (col >= hidden) continue;
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            s_sum[col + j] = (k ? s_sum[col + j] : 0.f) + dw[i][j];
-            s_sum[hidden + col + j] = (k ? s_sum[hidden + col + j] : 0.f) + db[i][j];
+        for (int j = 0; j < V / 2; ++j) {
+          u[j] = fma_f32x2(u[j], r2, m2);
+          dw[i][j] = fma_f32x2(g[j], u[j], dw[i][j]);
+          db[i][j] = add_f32x2(db[i][j], g[j]);
+          g[j] = mul_f32x2(g[j], wp[j]);
+          sum_u = fma_f32x2(g[j], u[j], sum_u);
+          sum_1 = add_f32x2(sum_1, g[j]);
+          if (kKeep) {
+            ku[kKeep ? i : 0][j] = u[j];
+            kg[kKeep ? i : 0][j] = g[j];
           }
         }
       }
-      __syncthreads();
-    }
-    for (int c = threadIdx.x; c < 2 * hidden; c += blockDim.x) mine_dw[c] = s_sum[c];
-  } else {
+      float sum[2], odd[2];
+      unpack_f32x2(sum_u, sum[0], odd[0]);
+      unpack_f32x2(sum_1, sum[1], odd[1]);
+      sum[0] += odd[0];
+      sum[1] += odd[1];
+      row_sum<kWarp>(sum, s_part, slot);
+      // (a row for all threads: they have left the tile before this one)
+      if (!kWarp && before >= 0 && threadIdx.x == 0 && asked < n_tiles && !s_abort) {
+        request(asked, before);
+        asked += gridDim.x;
+        ++n_asked;
+      }
+      // dx = (g w - u c_u - c_1) rstd + d_total
+      const float c_u = -sum[0] * inv * rstd, c_1 = rms ? 0.f : -sum[1] * inv * rstd;
+      const uint64_t cu2 = pack_f32x2(c_u, c_u), c12 = pack_f32x2(c_1, c_1);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int col = (i * group + tid) * V;
-      if (col >= hidden) continue;
+      for (int i = 0; i < NV; ++i) {
+        const int col = (i * group + tid) * V - a;
+        if (col >= hidden) continue;
+        uint64_t u[V / 2], g[V / 2], wp[V / 2], t[V / 2];
+        const WT* sw = reinterpret_cast<const WT*>(s_weight) + col;
+        if (kKeep) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        mine_dw[col + j] = dw[i][j];
-        mine_dw[hidden + col + j] = db[i][j];
+          for (int j = 0; j < V / 2; ++j) { u[j] = ku[kKeep ? i : 0][j]; g[j] = kg[kKeep ? i : 0][j]; }
+        } else {
+          pairs(load_vec<XT, V>(sx + col), u);
+          pairs(load_vec<XT, V>(sg + col), g);
+        }
+        if (kKeep) {
+        } else if (kRagged) {
+          constexpr int kPer = 16 / int(sizeof(WT)), P = V / kPer;      // the weights from column -a on: k elements into their vectors
+          const int k = -a & (kPer - 1);
+          const uint4* q = reinterpret_cast<const uint4*>(sw - k);
+          uint4 w4[P];
+#pragma unroll
+          for (int n = 0; n < P; ++n) w4[n] = shift_pair<int(sizeof(WT))>(q[n], q[n + 1], k);
+          Vec<WT, V> v;
+          memcpy(&v, w4, sizeof(w4));
+          pairs(v, wp);
+        } else {
+          pairs(load_vec<WT, V>(sw), wp);
+        }
+        if (d_total) {
+          if (n_tensors == 3) {
+            pairs(load_vec<XT, V>(sd + col), t);
+          } else {
+            const uint4 q = load_window(d_total, at + col, all);
+            Vec<XT, V> v;
+            memcpy(&v, &q, 16);
+            pairs(v, t);
+          }
+        }
+        float d[V];
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+          const uint64_t un = kKeep ? u[j] : fma_f32x2(u[j], r2, m2), gw = kKeep ? g[j] : mul_f32x2(g[j], wp[j]);
+          uint64_t v = fma_f32x2(gw, r2, fma_f32x2(un, cu2, c12));
+          if (d_total) v = add_f32x2(v, t[j]);
+          unpack_f32x2(v, d[2 * j], d[2 * j + 1]);
+        }
+        store_window(dx, at + col, d, -col, hidden - col);
       }
     }
+    if (kWarp || shape.stages == 1) {     // all warps have left the tile
+      __syncthreads();
+      if (threadIdx.x == 0 && asked < n_tiles && !s_abort) {
+        request(asked, stage);
+        asked += gridDim.x;
+        ++n_asked;
+      }
+    } else {
+      before = stage;
+    }
+    if (++stage == shape.stages) { stage = 0; ++turn; }
   }
+  if (s_abort && threadIdx.x == 0) {      // shared memory must outlive the copies in flight
+    const long long t0 = clock64();
+    for (int q = max(0, n_asked - shape.stages); q < n_asked; ++q)
+      while (!mbar_try_wait(smem_u32(&s_bar[q % shape.stages]), (q / shape.stages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
+  }
+  __syncthreads();
+  float* mine_dw = partial + int64_t(blockIdx.x) * 2 * hidden;
+  float* s_sum = reinterpret_cast<float*>(ring);
+  for (int k = 0; k < (kWarp ? kRowsPerCta : 1); ++k) {     // the warps' rows are added in the warps' order
+    if (!kWarp || k == warp) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int col = (i * group + tid) * V;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          if (col + j >= hidden) continue;
+          float e[2], f[2];
+          unpack_f32x2(dw[i][j / 2], e[0], e[1]);
+          unpack_f32x2(db[i][j / 2], f[0], f[1]);
+          s_sum[col + j] = (k ? s_sum[col + j] : 0.f) + e[j & 1];
+          s_sum[hidden + col + j] = (k ? s_sum[hidden + col + j] : 0.f) + f[j & 1];
+        }
+      }
+    }
+    __syncthreads();
+  }
+  for (int c = threadIdx.x; c < 2 * hidden; c += blockDim.x) mine_dw[c] = s_sum[c];
 }
 
 // dw (blockIdx.y = 0) and db (1): the parts of all CTAs, added in a fixed order.
@@ -219,50 +415,71 @@ __global__ void __launch_bounds__(32 * kSumRows)
 norm_sum_kernel(const float* partial, int32_t n_parts, int32_t hidden, WT* dweight, WT* dbias) {
   __shared__ float s[kSumRows][33];
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+  behind_wait();
+  behind_go();
   float v = 0.f;
-  if (col < hidden)
-    for (int p = part; p < n_parts; p += kSumRows) v += partial[(int64_t(p) * 2 + blockIdx.y) * hidden + col];
+  if (col < hidden) {
+    int p = part;
+    for (; p + 7 * kSumRows < n_parts; p += 8 * kSumRows) {
+      float w[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = partial[(int64_t(p + k * kSumRows) * 2 + blockIdx.y) * hidden + col];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v += w[k];
+    }
+    for (; p < n_parts; p += kSumRows) v += partial[(int64_t(p) * 2 + blockIdx.y) * hidden + col];
+  }
   s[part][lane] = v;
   __syncthreads();
   if (part == 0 && col < hidden) {
     for (int p = 1; p < kSumRows; ++p) v += s[p][lane];
-    const float one[1] = {v};
-    store_vec<WT, 1>((blockIdx.y ? dbias : dweight) + col, one);
+    set_element((blockIdx.y ? dbias : dweight) + col, v);
   }
 }
 
-// How a row is divided: V elements a load, NV loads a thread, `threads` of them (32: a warp).
+// How a row is divided: NV vectors of 16 bytes a thread, `threads` threads (32: a warp).  Rows that start anywhere reach into
+// one vector more.
 struct Division {
-  int v, nv, threads;
+  int nv, threads;
 };
+int vectors(int32_t hidden, int elem_bytes) {
+  const int bytes = hidden * elem_bytes;
+  return bytes % 16 ? (bytes + 16 - elem_bytes + 15) / 16 : bytes / 16;     // (16 - elem_bytes in front of it at most)
+}
 Division divide(int32_t hidden, int elem_bytes) {
-  const int v = 16 / elem_bytes;
-  if (hidden % v == 0) {
-    const int n = hidden / v;
-    if (n <= 128) return {v, n <= 32 ? 1 : n <= 64 ? 2 : 4, 32};
-    const int nv = n <= 256 ? 1 : n <= 512 ? 2 : 4;
-    return {v, nv, ((n + nv - 1) / nv + 31) / 32 * 32};
-  }
-  if (hidden <= 128) return {1, 4, 32};
-  const int nv = hidden <= 4096 ? 4 : 16;
-  return {1, nv, ((hidden + nv - 1) / nv + 31) / 32 * 32};
+  const int n = vectors(hidden, elem_bytes);
+  if (n <= 128) return {n <= 32 ? 1 : n <= 64 ? 2 : 4, 32};
+  const int nv = n <= 256 ? 1 : n <= 512 ? 2 : n <= 4096 ? 4 : 8;
+  return {nv, ((n + nv - 1) / nv + 31) / 32 * 32};
+}
+// The backward: a warp a row of up to 1024 columns, else 16 columns a thread for up to 512 threads, else 32.
+Division divide_bwd(int32_t hidden, int elem_bytes) {
+  const int n = vectors(hidden, elem_bytes), wide = elem_bytes / 2;     // 8 columns: `wide` vectors
+  if (n <= 128 * wide) return {n <= 32 * wide ? wide : n <= 64 * wide ? 2 * wide : 4 * wide, 32};
+  const int nv = n <= 1024 * wide ? 2 * wide : 4 * wide;
+  return {nv, ((n + nv - 1) / nv + 31) / 32 * 32};
 }
 
-int64_t part_count(int64_t n_tokens, int32_t hidden) {
-  const int64_t most = hidden > 4096 ? kSmCount : 2 * kSmCount;
-  return std::max<int64_t>(1, std::min(most, n_tokens));
+// CTAs of the backward for an SM: 512 threads of 128 registers.
+int ctas_per_sm(const Division& d) { return d.threads == 32 ? 2 : std::max(1, std::min(4, 512 / d.threads)); }
+// Rows of a tile: one, or 8 for each of a CTA's warps, fewer where all tiles would not fill the SMs, and 8 KB of a tensor at most.
+int tile_rows(const Division& d, int64_t n_tokens, int32_t hidden, int elem_bytes) {
+  if (d.threads != 32) return 1;
+  int rows = kRowsPerCta;
+  while (rows < 8 * kRowsPerCta && 2 * rows * hidden * elem_bytes <= 8192 && n_tokens >= 4 * int64_t(rows) * kSmCount) rows *= 2;
+  return rows;
+}
+int64_t part_count(const Division& d, int64_t n_tokens, int rows) {
+  return std::max<int64_t>(1, std::min<int64_t>((n_tokens + rows - 1) / rows, int64_t(kSmCount) * ctas_per_sm(d)));
 }
 
 template <typename F>
-psa_status_t with_division(const Division& d, int elem_bytes, F&& f) {
+psa_status_t with_division(const Division& d, bool ragged, F&& f) {
   const bool warp = d.threads == 32;
-  const int v = d.v == 1 ? 1 : 16 / elem_bytes;
-  if (v != 1) {
-    if (warp) return d.nv == 1 ? f.template run<0, 1, true>() : d.nv == 2 ? f.template run<0, 2, true>() : f.template run<0, 4, true>();
-    return d.nv == 1 ? f.template run<0, 1, false>() : d.nv == 2 ? f.template run<0, 2, false>() : f.template run<0, 4, false>();
-  }
-  if (warp) return f.template run<1, 4, true>();
-  return d.nv == 4 ? f.template run<1, 4, false>() : f.template run<1, 16, false>();
+#define PSA_NORM(NV) (warp ? (ragged ? f.template run<NV, true, true>() : f.template run<NV, true, false>()) \
+                           : (ragged ? f.template run<NV, false, true>() : f.template run<NV, false, false>()))
+  return d.nv == 1 ? PSA_NORM(1) : d.nv == 2 ? PSA_NORM(2) : d.nv == 4 ? PSA_NORM(4) : PSA_NORM(8);
+#undef PSA_NORM
 }
 
 template <typename XT, typename WT>
@@ -276,11 +493,15 @@ struct Forward {
   float* stats;
   int threads;
   cudaStream_t stream;
-  template <int kScalar, int NV, bool kWarp>
+  template <int NV, bool kWarp, bool kRagged>
   psa_status_t run() {
-    constexpr int V = kScalar ? 1 : 16 / int(sizeof(XT));
+    if constexpr (NV == 8 && (sizeof(XT) == 2 || kWarp || !kRagged)) return PSA_ERR_UNSUPPORTED;     // (divide() does not say so)
+    else return go<NV, kWarp, kRagged>();
+  }
+  template <int NV, bool kWarp, bool kRagged>
+  psa_status_t go() {
     const int64_t grid = kWarp ? (n_tokens + kRowsPerCta - 1) / kRowsPerCta : n_tokens;
-    norm_kernel<XT, WT, V, NV, kWarp><<<unsigned(grid), kWarp ? 32 * kRowsPerCta : threads, 0, stream>>>(
+    launch_behind(true, norm_kernel<XT, WT, NV, kWarp, kRagged>, dim3(unsigned(grid)), kWarp ? 32 * kRowsPerCta : threads, 0, stream,
         static_cast<const XT*>(x), static_cast<const XT*>(residual), static_cast<const WT*>(weight), static_cast<const WT*>(bias),
         n_tokens, hidden, eps, rms, static_cast<XT*>(out), static_cast<XT*>(total), stats);
     return check_last_cuda_error("psa_norm launch");
@@ -296,18 +517,34 @@ struct Backward {
   int32_t hidden, rms;
   void *dx, *dweight, *dbias;
   float* partial;
-  int threads;
+  Division d;
+  int32_t* status;
   cudaStream_t stream;
-  template <int kScalar, int NV, bool kWarp>
+  template <int NV, bool kWarp, bool kRagged>
   psa_status_t run() {
-    constexpr int V = kScalar ? 1 : 16 / int(sizeof(XT));
-    const int rows = kWarp ? kRowsPerCta : 1;
-    const int64_t parts = std::min(part_count(n_tokens, hidden), std::max<int64_t>(1, (n_tokens + rows - 1) / rows));
-    norm_bwd_kernel<XT, WT, V, NV, kWarp><<<unsigned(parts), kWarp ? 32 * kRowsPerCta : threads, kWarp ? 8 * hidden : 0, stream>>>(
-        static_cast<const XT*>(d_out), static_cast<const XT*>(x), static_cast<const WT*>(weight), stats,
-        static_cast<const XT*>(d_total), n_tokens, hidden, rms, static_cast<XT*>(dx), partial);
-    norm_sum_kernel<WT><<<dim3(unsigned((hidden + 31) / 32), dbias ? 2 : 1), 32 * kSumRows, 0, stream>>>(
-        partial, int32_t(parts), hidden, static_cast<WT*>(dweight), static_cast<WT*>(dbias));
+    constexpr int kWide = int(sizeof(XT)) / 2;
+    if constexpr (NV < kWide || NV > 4 * kWide || (!kWarp && NV < 2 * kWide)) return PSA_ERR_UNSUPPORTED;   // (divide_bwd() does not say so)
+    else return go<NV, kWarp, kRagged>();
+  }
+  template <int NV, bool kWarp, bool kRagged>
+  psa_status_t go() {
+    BwdShape shape{};
+    shape.rows = tile_rows(d, n_tokens, hidden, int(sizeof(XT)));
+    shape.slot_bytes = uint32_t((int64_t(shape.rows) * hidden * int(sizeof(XT)) + 47) / 16 * 16);    // and a vector around it
+    shape.w_bytes = uint32_t((hidden * int(sizeof(WT)) + 15) / 16 * 16) + 2 * kWeightPad;
+    const uint32_t room = 224 * 1024 / ctas_per_sm(d) - 1024 - shape.w_bytes;
+    shape.staged = d_total && 3 * shape.slot_bytes <= room ? 3 : 2;
+    const uint32_t stage = uint32_t(shape.staged) * shape.slot_bytes;
+    shape.stages = int(std::max(1u, std::min(8u, std::min(room / stage, 1 + 98304 / stage))));
+    const uint32_t smem = std::max(shape.stages * stage, uint32_t(hidden) * 8) + shape.w_bytes + 16;
+    const int64_t parts = part_count(d, n_tokens, shape.rows);
+    auto kernel = norm_bwd_kernel<XT, WT, NV, kWarp, kRagged>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return PSA_ERR_CUDA;
+    launch_behind(true, kernel, dim3(unsigned(parts)), kWarp ? 32 * kRowsPerCta : d.threads, smem, stream,
+                  static_cast<const XT*>(d_out), static_cast<const XT*>(x), static_cast<const WT*>(weight), stats,
+                  static_cast<const XT*>(d_total), n_tokens, hidden, rms, static_cast<XT*>(dx), partial, shape, status);
+    launch_behind(true, norm_sum_kernel<WT>, dim3(unsigned((hidden + 31) / 32), dbias ? 2 : 1), 32 * kSumRows, 0, stream, partial,
+                  int32_t(parts), hidden, static_cast<WT*>(dweight), static_cast<WT*>(dbias));
     return check_last_cuda_error("psa_norm_bwd launch");
   }
 };
@@ -344,20 +581,26 @@ extern "C" psa_status_t psa_norm(const void* x, const void* residual, const void
   const Division d = divide(hidden, e);
   cudaStream_t st = cudaStream_t(stream);
   if (dtype == PSA_DTYPE_F32)
-    return with_division(d, e, Forward<float, float>{x, residual, weight, bias, n_tokens, hidden, eps, rms, out, total, stats, d.threads, st});
+    return with_division(d, hidden * e % 16 != 0, Forward<float, float>{x, residual, weight, bias, n_tokens, hidden, eps, rms, out, total, stats, d.threads, st});
   if (weight_dtype == PSA_DTYPE_F32)
-    return with_division(d, e, Forward<__nv_bfloat16, float>{x, residual, weight, bias, n_tokens, hidden, eps, rms, out, total, stats, d.threads, st});
-  return with_division(d, e, Forward<__nv_bfloat16, __nv_bfloat16>{x, residual, weight, bias, n_tokens, hidden, eps, rms, out, total, stats, d.threads, st});
+    return with_division(d, hidden * e % 16 != 0, Forward<__nv_bfloat16, float>{x, residual, weight, bias, n_tokens, hidden, eps, rms, out, total, stats, d.threads, st});
+  return with_division(d, hidden * e % 16 != 0, Forward<__nv_bfloat16, __nv_bfloat16>{x, residual, weight, bias, n_tokens, hidden, eps, rms, out, total, stats, d.threads, st});
 }
 
 extern "C" size_t psa_norm_bwd_workspace_bytes(int64_t n_tokens, int32_t hidden) {
   if (n_tokens < 0 || hidden <= 0 || hidden > psa::kMaxHidden) return 0;
-  return size_t(psa::part_count(n_tokens, hidden)) * 2 * size_t(hidden) * 4;
+  size_t parts = 0;
+  for (int e : {2, 4}) {
+    const psa::Division d = psa::divide_bwd(hidden, e);
+    parts = std::max(parts, size_t(psa::part_count(d, n_tokens, psa::tile_rows(d, n_tokens, hidden, e))));
+  }
+  return parts * 2 * size_t(hidden) * 4;
 }
 
 extern "C" psa_status_t psa_norm_bwd(const void* d_out, const void* x, const void* weight, const float* stats,
                                      const void* d_total, int32_t dtype, int32_t weight_dtype, int64_t n_tokens, int32_t hidden,
-                                     int32_t rms, void* dx, void* dweight, void* dbias, void* workspace, void* stream) {
+                                     int32_t rms, void* dx, void* dweight, void* dbias, void* workspace, int32_t* device_status,
+                                     void* stream) {
   using namespace psa;
   const psa_status_t sizes = check_sizes(n_tokens, hidden, dtype, weight_dtype);
   if (sizes != PSA_OK) return sizes;
@@ -367,12 +610,12 @@ extern "C" psa_status_t psa_norm_bwd(const void* d_out, const void* x, const voi
                         static_cast<const void*>(dweight), static_cast<const void*>(dbias), static_cast<const void*>(workspace)})
     if (misaligned(p, 16)) return PSA_ERR_ALIGNMENT;
   const int e = dtype == PSA_DTYPE_F32 ? 4 : 2;
-  const Division d = divide(hidden, e);
+  const Division d = divide_bwd(hidden, e);
   cudaStream_t st = cudaStream_t(stream);
   float* part = static_cast<float*>(workspace);
   if (dtype == PSA_DTYPE_F32)
-    return with_division(d, e, Backward<float, float>{d_out, x, weight, stats, d_total, n_tokens, hidden, rms, dx, dweight, dbias, part, d.threads, st});
+    return with_division(d, hidden * e % 16 != 0, Backward<float, float>{d_out, x, weight, stats, d_total, n_tokens, hidden, rms, dx, dweight, dbias, part, d, device_status, st});
   if (weight_dtype == PSA_DTYPE_F32)
-    return with_division(d, e, Backward<__nv_bfloat16, float>{d_out, x, weight, stats, d_total, n_tokens, hidden, rms, dx, dweight, dbias, part, d.threads, st});
-  return with_division(d, e, Backward<__nv_bfloat16, __nv_bfloat16>{d_out, x, weight, stats, d_total, n_tokens, hidden, rms, dx, dweight, dbias, part, d.threads, st});
+    return with_division(d, hidden * e % 16 != 0, Backward<__nv_bfloat16, float>{d_out, x, weight, stats, d_total, n_tokens, hidden, rms, dx, dweight, dbias, part, d, device_status, st});
+  return with_division(d, hidden * e % 16 != 0, Backward<__nv_bfloat16, __nv_bfloat16>{d_out, x, weight, stats, d_total, n_tokens, hidden, rms, dx, dweight, dbias, part, d, device_status, st});
 }
