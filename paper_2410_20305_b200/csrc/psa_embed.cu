@@ -55,18 +55,20 @@ embed_kernel(const int32_t* ids, const T* table, int64_t n_tokens, int64_t vocab
 }
 
 // ---------------------------------------------------------------- tokens sorted by id
-// CTA b owns the ids of [b * bins, (b + 1) * bins).  Its 32 warps walk 32 consecutive parts of the tokens: once to count
-// every bin (a count per warp) and the tokens of smaller ids, and, when the counts have become places, once more to put
-// the tokens down.  Tokens are met in their order, so equal ids keep it.  Every CTA reads all ids (from L2).
+// CTA b of a power of two owns the ids that leave b: frequent tokens often have neighbouring ids, and a CTA with a range of
+// them would have most of the work.  Its 32 warps walk 32 consecutive parts of the tokens: once to count every id of theirs
+// (a count per warp) and the tokens of the CTAs before, and, when the counts have become places, once more to put the
+// tokens down.  Tokens are met in their order, so equal ids keep it.  Every CTA reads all ids (from L2).
 constexpr int kIndexThreads = 1024, kMaxBins = 1024, kAhead = 8;
 
 __global__ void __launch_bounds__(kIndexThreads)
-embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t bins, int32_t* start, int32_t* order,
-                   int32_t* sorted_id, int32_t* status) {
+embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t bins, int32_t* start, int32_t* count,
+                   int32_t* order, int32_t* sorted_id, int32_t* status) {
   extern __shared__ int32_t counts[];     // [32][bins]
   __shared__ int32_t s_warp[32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int lo = int(blockIdx.x) * bins, n_bins = min(bins, vocab - lo);
+  const uint32_t rest = blockIdx.x, mask = gridDim.x - 1, n_ids = uint32_t(vocab);
+  const int log2_ctas = 31 - __clz(int(gridDim.x));
   const int share = ((n_tokens + 31) / 32 + 31) / 32 * 32;
   const int64_t first = int64_t(warp) * share;
   const int begin = int(min(first, int64_t(n_tokens))), end = int(min(first + share, int64_t(n_tokens)));
@@ -76,21 +78,24 @@ embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t 
   behind_go();
   __syncthreads();
 
+  // (ids as unsigned numbers: a negative one is larger than all others)
   int below = 0;
   bool bad = false;
   for (int t = begin; t < end; t += 32 * kAhead) {
-    int32_t id[kAhead];
+    uint32_t id[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) id[k] = t + k * 32 + lane < end ? ids[t + k * 32 + lane] : vocab;
+    for (int k = 0; k < kAhead; ++k) id[k] = t + k * 32 + lane < end ? uint32_t(ids[t + k * 32 + lane]) : 0xffffffffu;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      if (t + k * 32 + lane < end) bad |= id[k] < 0 || id[k] >= vocab;
-      if (id[k] < 0 || id[k] >= lo + n_bins) continue;
-      if (id[k] < lo) ++below;
-      else atomicAdd(mine + (id[k] - lo), 1);
+      if (id[k] >= n_ids) continue;
+      below += (id[k] & mask) < rest;
+      if ((id[k] & mask) == rest) atomicAdd(mine + (id[k] >> log2_ctas), 1);
     }
+    if (blockIdx.x == 0)
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) bad |= t + k * 32 + lane < end && id[k] >= n_ids;
   }
-  if (bad && blockIdx.x == 0 && status) atomicOr(status, PSA_DEVSTAT_BAD_TARGET);
+  if (bad && status) atomicOr(status, PSA_DEVSTAT_BAD_TARGET);
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) s_warp[warp] = below;
   __syncthreads();
@@ -98,8 +103,10 @@ embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t 
   __syncthreads();
 
   // Thread i owns bin i: its tokens in all, the bins before it, then the warps before each warp.
+  const int id = (int(threadIdx.x) << log2_ctas) + int(rest);
+  const bool owner = int(threadIdx.x) < bins && id < vocab;
   int total = 0;
-  if (threadIdx.x < n_bins)
+  if (owner)
     for (int w = 0; w < 32; ++w) total += counts[w * bins + threadIdx.x];
   int scan = total;
 #pragma unroll
@@ -112,9 +119,10 @@ embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t 
   int before = 0;
   for (int w = 0; w < warp; ++w) before += s_warp[w];
   int at = below + before + scan - total;
-  if (threadIdx.x < n_bins) {
-    start[lo + threadIdx.x] = at;
-    if (lo + int(threadIdx.x) == vocab - 1) start[vocab] = at + total;
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == kIndexThreads - 1) start[vocab] = at + total;     // tokens with a good id
+  if (owner) {
+    start[id] = at;
+    count[id] = total;
     for (int w = 0; w < 32; ++w) {
       const int c = counts[w * bins + threadIdx.x];
       counts[w * bins + threadIdx.x] = at;
@@ -124,25 +132,26 @@ embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t 
   __syncthreads();
 
   for (int t = begin; t < end; t += 32 * kAhead) {
-    int32_t id[kAhead];
+    uint32_t v[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) id[k] = t + k * 32 + lane < end ? ids[t + k * 32 + lane] : vocab;
+    for (int k = 0; k < kAhead; ++k) v[k] = t + k * 32 + lane < end ? uint32_t(ids[t + k * 32 + lane]) : 0xffffffffu;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const bool here = id[k] >= lo && id[k] < lo + n_bins;
+      const bool here = v[k] < n_ids && (v[k] & mask) == rest;
       const unsigned any = __ballot_sync(0xffffffffu, here);
       if (!any) continue;
+      const uint32_t bin = v[k] >> log2_ctas;
       int place = 0;
       unsigned same = 0;
       if (here) {
-        same = __match_any_sync(any, id[k]);
-        place = mine[id[k] - lo] + __popc(same & ((1u << lane) - 1u));
+        same = __match_any_sync(any, bin);
+        place = mine[bin] + __popc(same & ((1u << lane) - 1u));
       }
       __syncwarp();
       if (here) {
-        if (lane == __ffs(same) - 1) mine[id[k] - lo] += __popc(same);
+        if (lane == __ffs(same) - 1) mine[bin] += __popc(same);
         order[place] = t + k * 32 + lane;
-        sorted_id[place] = id[k];
+        sorted_id[place] = int(v[k]);
       }
       __syncwarp();
     }
@@ -153,16 +162,16 @@ embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t 
 // blockIdx.x < n_runs: the sorted tokens [r * kRun, (r + 1) * kRun).  An id that lies within the run is written; the part of
 // one that began in an earlier run goes to slot 0 of the run, of one that only goes on in the next run to slot 1.
 // The other CTAs write the rows of ids that do not occur (dense gradients only).  blockIdx.y: a slice of the columns.
-constexpr int kRun = 32, kZeroRows = 16, kUnroll = 4;
+constexpr int kRun = 32, kZeroRows = 16;
 
 // A thread holds one window of V columns: of the row of the table that it adds to, so that what it writes is aligned.
 template <typename XT, typename GT, bool kRagged>
 __global__ void __launch_bounds__(kThreads)
-embed_sum_kernel(const XT* d_out, const int32_t* start, const int32_t* order, const int32_t* sorted_id, int32_t n_runs,
+embed_sum_kernel(const XT* d_out, const int32_t* start, const int32_t* count, const int32_t* order, const int32_t* sorted_id, int32_t n_runs,
                  int64_t n_tokens, int32_t vocab, int32_t hidden, int32_t windows, float scale, int32_t accumulate, GT* dtable,
                  float* partial) {
-  constexpr int V = 16 / int(sizeof(XT)), W = 16 / int(sizeof(GT));
-  const int k = int(blockIdx.y) * kThreads + int(threadIdx.x);
+  constexpr int V = 16 / int(sizeof(XT)), W = 16 / int(sizeof(GT)), kUnroll = kRagged ? 4 : 8;     // rows in flight
+  const int k = int(blockIdx.y) * int(blockDim.x) + int(threadIdx.x);
   behind_wait();
   behind_go();
   // The thread's first column in the row of id v (may be negative: elements of the row before).
@@ -172,7 +181,7 @@ embed_sum_kernel(const XT* d_out, const int32_t* start, const int32_t* order, co
     const float zero[V] = {};
     for (int r = 0; r < kZeroRows && v0 + r < vocab; ++r) {
       const int col = column(v0 + r);
-      if (start[v0 + r] == start[v0 + r + 1] && col < hidden) store_window(dtable, (v0 + r) * hidden + col, zero, -col, hidden - col);
+      if (count[v0 + r] == 0 && col < hidden) store_window(dtable, (v0 + r) * hidden + col, zero, -col, hidden - col);
     }
     return;
   }
@@ -234,30 +243,45 @@ embed_sum_kernel(const XT* d_out, const int32_t* start, const int32_t* order, co
   }
 }
 
-// The ids that spread over several runs: the CTA of the run in which one begins adds the runs' sums in their order.
+// The ids that spread over several runs: the CTAs of the run in which one begins add the runs' sums, each warp every eighth of
+// them, then the warps' sums in their order (one thread all of them one after the other: 17 us at 16215 tokens, of which
+// the most frequent id has a twelfth).  A CTA holds 32 windows.
+constexpr int kJoinWarps = 8;
+
 template <typename GT, int V, bool kRagged>
-__global__ void __launch_bounds__(kThreads)
-embed_join_kernel(const int32_t* start, const int32_t* sorted_id, int32_t vocab, int32_t hidden, int32_t windows, float scale,
+__global__ void __launch_bounds__(32 * kJoinWarps)
+embed_join_kernel(const int32_t* start, const int32_t* count, const int32_t* sorted_id, int32_t vocab, int32_t hidden, int32_t windows, float scale,
                   int32_t accumulate, const float* partial, GT* dtable) {
   constexpr int W = 16 / int(sizeof(GT));
-  const int k = int(blockIdx.y) * kThreads + int(threadIdx.x), run = blockIdx.x, last = run * kRun + kRun - 1;
+  __shared__ float s_sum[kJoinWarps][V][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = int(blockIdx.y) * 32 + lane;
+  const int run = blockIdx.x, last = run * kRun + kRun - 1;
   behind_wait();
   behind_go();
-  if (k >= windows || last >= start[vocab]) return;
-  const int id = sorted_id[last], from = start[id], to = start[id + 1];
+  if (last >= start[vocab]) return;
+  const int id = sorted_id[last], from = start[id], to = from + count[id];
   if (from < run * kRun || to <= last + 1) return;
   const int64_t row = int64_t(id) * hidden;
-  const int col = k * V - (kRagged ? int(row & (W - 1)) : 0), last_run = (to - 1) / kRun;
-  if (col >= hidden) return;
-  float acc[V];
-  load_vec<float, V>(partial + ((int64_t(run) * 2 + 1) * windows + k) * V).get(acc);
-#pragma unroll 8
-  for (int r = run + 1; r <= last_run; ++r) {
-    float v[V];
-    load_vec<float, V>(partial + (int64_t(r) * 2 * windows + k) * V).get(v);
+  const int col = k * V - (kRagged ? int(row & (W - 1)) : 0), n = (to - 1) / kRun - run + 1;
+  const bool live = k < windows && col < hidden;
+  float acc[V] = {};
+  if (live) {
+#pragma unroll 4
+    for (int r = warp; r < n; r += kJoinWarps) {      // the run that the id begins in has its sum in slot 1, the others in slot 0
+      float v[V];
+      load_vec<float, V>(partial + ((int64_t(run + r) * 2 + (r == 0 ? 1 : 0)) * windows + k) * V).get(v);
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] += v[j];
+      for (int j = 0; j < V; ++j) acc[j] += v[j];
+    }
   }
+#pragma unroll
+  for (int j = 0; j < V; ++j) s_sum[warp][j][lane] = acc[j];
+  __syncthreads();
+  if (warp != 0 || !live) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWarps; ++w)
+#pragma unroll
+    for (int j = 0; j < V; ++j) acc[j] += s_sum[w][j][lane];
   float old[V] = {};
   if (accumulate) {
     Span<GT, V, kRagged> in;
@@ -276,11 +300,13 @@ constexpr int kMaxEmbed = 1 << 20;
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
 
 struct EmbedWorkspace {
-  size_t start, order, sorted_id, partial, total;
+  size_t start, count, order, sorted_id, partial, total;
 };
 EmbedWorkspace workspace_layout(int64_t T, int64_t vocab, int64_t hidden) {
   EmbedWorkspace w{};
   size_t at = aligned(size_t(vocab + 1) * 4);
+  w.count = at;
+  at += aligned(size_t(vocab) * 4);
   w.order = at;
   at += aligned(size_t(T) * 4);
   w.sorted_id = at;
@@ -317,24 +343,26 @@ psa_status_t embed_bwd(const void* d_out, const int32_t* ids, int64_t n_tokens, 
   constexpr int V = 16 / int(sizeof(XT));
   const EmbedWorkspace w = workspace_layout(n_tokens, vocab, hidden);
   auto ints = [&](size_t off) { return reinterpret_cast<int32_t*>(ws + off); };
-  // A range of ids per SM, of at least 32 and at most kMaxBins ids.
-  const int bins = int(std::min<int64_t>(kMaxBins, std::max<int64_t>(32, (vocab + 147) / 148)));
+  int ctas = 128;
+  while (vocab > int64_t(ctas) * kMaxBins) ctas *= 2;
+  const int bins = int((vocab + ctas - 1) / ctas);
   if (cudaFuncSetAttribute(embed_index_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * kMaxBins * 4) != cudaSuccess)
     return PSA_ERR_CUDA;
-  launch_behind(true, embed_index_kernel, dim3(unsigned((vocab + bins - 1) / bins)), kIndexThreads, size_t(32) * bins * 4, stream,
-                ids, int32_t(n_tokens), int32_t(vocab), bins, ints(w.start), ints(w.order), ints(w.sorted_id), status);
+  launch_behind(true, embed_index_kernel, dim3(unsigned(ctas)), kIndexThreads, size_t(32) * bins * 4, stream, ids,
+                int32_t(n_tokens), int32_t(vocab), bins, ints(w.start), ints(w.count), ints(w.order), ints(w.sorted_id), status);
   const int n_runs = int((n_tokens + kRun - 1) / kRun);
   const int windows = windows_of(hidden, V, 16 / int(sizeof(GT)));
   const unsigned slices = unsigned((windows + kThreads - 1) / kThreads);
+  const unsigned threads = unsigned((windows + int(slices) * 32 - 1) / (int(slices) * 32)) * 32;     // even slices of whole warps
   const unsigned zero = accumulate ? 0u : unsigned((vocab + kZeroRows - 1) / kZeroRows);
   float* partial = reinterpret_cast<float*>(ws + w.partial);
   if (n_runs + zero > 0)
-    launch_behind(true, embed_sum_kernel<XT, GT, kRagged>, dim3(unsigned(n_runs) + zero, slices), kThreads, 0, stream,
-                  static_cast<const XT*>(d_out), ints(w.start), ints(w.order), ints(w.sorted_id), n_runs, n_tokens, int32_t(vocab),
+    launch_behind(true, embed_sum_kernel<XT, GT, kRagged>, dim3(unsigned(n_runs) + zero, slices), threads, 0, stream,
+                  static_cast<const XT*>(d_out), ints(w.start), ints(w.count), ints(w.order), ints(w.sorted_id), n_runs, n_tokens, int32_t(vocab),
                   hidden, windows, scale, accumulate, static_cast<GT*>(dtable), partial);
   if (n_runs > 1)
-    launch_behind(true, embed_join_kernel<GT, V, kRagged>, dim3(unsigned(n_runs), slices), kThreads, 0, stream, ints(w.start),
-                  ints(w.sorted_id), int32_t(vocab), hidden, windows, scale, accumulate, partial, static_cast<GT*>(dtable));
+    launch_behind(true, embed_join_kernel<GT, V, kRagged>, dim3(unsigned(n_runs), unsigned((windows + 31) / 32)), 32 * kJoinWarps, 0, stream, ints(w.start),
+                  ints(w.count), ints(w.sorted_id), int32_t(vocab), hidden, windows, scale, accumulate, partial, static_cast<GT*>(dtable));
   return check_last_cuda_error("psa_embed_bwd launch");
 }
 

@@ -142,15 +142,18 @@ norm_kernel(const XT* x, const XT* residual, const WT* weight, const WT* bias, i
   }
 }
 
-// V elements of a tile in shared memory, `a` elements behind a 16-byte boundary.
-template <typename T, bool kRagged>
-__device__ __forceinline__ Vec<T, 16 / int(sizeof(T))> shared_vec(const T* p, int a) {
-  constexpr int V = 16 / int(sizeof(T));
-  if (!kRagged) return load_vec<T, V>(p);
-  const uint4* q = reinterpret_cast<const uint4*>(p - a);
-  const uint4 w = shift_pair<int(sizeof(T))>(q[0], q[1], a);
+// V elements in shared memory from an address on that lies `a` elements behind a 16-byte boundary.
+template <typename T, int V, bool kRagged>
+__device__ __forceinline__ Vec<T, V> shared_vec(uint32_t addr, int a) {
+  constexpr int kE = int(sizeof(T)), P = V * kE / 16;
+  uint4 q[P + 1], w[P];
+  if (kRagged) addr -= uint32_t(a * kE);
+#pragma unroll
+  for (int k = 0; k < (kRagged ? P + 1 : P); ++k) q[k] = ld_shared_v4(addr + 16 * k);
+#pragma unroll
+  for (int k = 0; k < P; ++k) w[k] = kRagged ? shift_pair<kE>(q[k], q[k + 1], a) : q[k];
   Vec<T, V> v;
-  memcpy(&v, &w, 16);
+  memcpy(&v, w, sizeof(w));
   return v;
 }
 template <typename T, int V>
@@ -161,20 +164,14 @@ __device__ __forceinline__ void zero_behind(Vec<T, V>& v, int n) {
   for (int j = 0; j < V; ++j) f[j] = j < n ? f[j] : 0.f;
   v.set(f);
 }
-// V floats as pairs for packed arithmetic.
-template <typename T, int V>
-__device__ __forceinline__ void pairs(const Vec<T, V>& v, uint64_t (&p)[V / 2]) {
-  float f[V];
-  v.get(f);
-#pragma unroll
-  for (int j = 0; j < V / 2; ++j) p[j] = pack_f32x2(f[2 * j], f[2 * j + 1]);
-}
-
 // The backward.  A CTA takes every gridDim.x-th tile of rows: one row for all its threads, or, of narrow rows, some for each of
 // its warps.  Tiles are contiguous in memory and come by bulk copies into a ring of stages, so that several are in flight
 // whatever the arithmetic waits for (31041 x 4096 bf16 with d_total: 346 us with loads where the values are used, 253 with the
 // next row's in registers, @NB@ so).  For the sums over tokens a thread keeps its columns [k V, (k + 1) V) throughout; of dx it
-// writes window k of each row (the same columns where rows are aligned).  partial: [gridDim.x][2][hidden].
+// writes window k of each row (the same columns where rows are aligned).  partial: [gridDim.x][2][part_pitch].
+// A part's rows of sums start at 16 bytes.
+__host__ __device__ constexpr int part_pitch(int hidden) { return (hidden + 3) / 4 * 4; }
+
 struct BwdShape {
   int32_t rows, stages;                   // rows of a tile; tiles in flight
   int32_t staged;                         // tensors that come by the ring: x, d_out and, where there is room, d_total
@@ -183,12 +180,12 @@ struct BwdShape {
 constexpr uint32_t kWeightPad = 64;       // zeros in front of the weight and behind it
 
 template <typename XT, typename WT, int NV, bool kWarp, bool kRagged>
-__global__ void __launch_bounds__(bwd_threads<XT, NV, kWarp>())
+__global__ void __launch_bounds__(bwd_threads<XT, NV, kWarp>(), 1)
 norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* stats, const XT* d_total, int64_t n_tokens,
                 int32_t hidden, int32_t rms, XT* dx, float* partial, BwdShape shape, int32_t* status) {
-  constexpr int V = 16 / int(sizeof(XT)), kE = int(sizeof(XT));
+  constexpr int V = 16 / int(sizeof(XT)), kE = int(sizeof(XT)), kW = int(sizeof(WT));
   constexpr bool kKeep = !kRagged && NV * V <= 16;
-  extern __shared__ uint8_t smem_raw[];        // [stages][2 or 3 tensors][slot], weight, [2][hidden] sums (over the stages, at the end)
+  extern __shared__ uint8_t smem_raw[];        // [stages][2 or 3 tensors][slot], weight;  at the end the warps' sums
   __shared__ float s_part[4][32];
   __shared__ uint64_t s_bar[8];
   __shared__ int s_abort;
@@ -197,6 +194,7 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
   const uint32_t base = (smem_u32(smem_raw) + 15u) & ~15u, n_tensors = uint32_t(shape.staged);
   uint8_t* ring = smem_raw + (base - smem_u32(smem_raw));
   uint8_t* s_weight = ring + uint32_t(shape.stages) * n_tensors * shape.slot_bytes + kWeightPad;
+  const uint32_t sw = base + uint32_t(shape.stages) * n_tensors * shape.slot_bytes + kWeightPad;
   const WaitCtx wctx{&s_abort, status, kWaitLimitClocks};
   const int64_t all = n_tokens * hidden, tile_elems = int64_t(shape.rows) * hidden, n_tiles = (n_tokens + shape.rows - 1) / shape.rows;
 
@@ -225,19 +223,19 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
       if (n_tensors == 3) bulk_load(to + 2 * shape.slot_bytes, d_total + first, n, bar);
       return;
     }
-    const int64_t end = min(all, first + tile_elems), to = min(all & ~int64_t(V - 1), (end + V - 1) & ~int64_t(V - 1));
-    const uint32_t bytes = to > from ? uint32_t(to - from) * kE : 0u, bar = smem_u32(&s_bar[stage]);
-    for (uint32_t t = 0; t < n_tensors; ++t) {
-      const XT* src = t == 0 ? x : t == 1 ? d_out : d_total;
-      XT* slot = reinterpret_cast<XT*>(ring + (uint32_t(stage) * n_tensors + t) * shape.slot_bytes);
-      for (int64_t e = max(to, from); e < end; ++e) slot[e - from] = src[e];
-    }
-    mbar_expect_tx(bar, n_tensors * bytes);
-    if (bytes)
+    const int64_t end = min(all, first + tile_elems), last = all & ~int64_t(V - 1), to = min(last, (end + V - 1) & ~int64_t(V - 1));
+    const uint32_t bytes = uint32_t(to - from) * kE, bar = smem_u32(&s_bar[stage]), at = base + uint32_t(stage) * n_tensors * shape.slot_bytes;
+    if (end > last)
       for (uint32_t t = 0; t < n_tensors; ++t) {
         const XT* src = t == 0 ? x : t == 1 ? d_out : d_total;
-        bulk_load(base + (uint32_t(stage) * n_tensors + t) * shape.slot_bytes, src + from, bytes, bar);
+        XT* slot = reinterpret_cast<XT*>(ring + (uint32_t(stage) * n_tensors + t) * shape.slot_bytes);
+        for (int64_t e = max(last, from); e < end; ++e) slot[e - from] = src[e];
       }
+    mbar_expect_tx(bar, n_tensors * bytes);
+    if (bytes == 0) return;
+    bulk_load(at, x + from, bytes, bar);
+    bulk_load(at + shape.slot_bytes, d_out + from, bytes, bar);
+    if (n_tensors == 3) bulk_load(at + 2 * shape.slot_bytes, d_total + from, bytes, bar);
   };
   int64_t asked = blockIdx.x;     // the next tile to request, and how many have been (thread 0's)
   int n_asked = 0;
@@ -245,11 +243,11 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
     for (int s = 0; s < shape.stages && asked < n_tiles; ++s, asked += gridDim.x, ++n_asked) request(asked, s);
   __syncthreads();
 
-  uint64_t dw[NV][V / 2], db[NV][V / 2];
+  float dw[NV][V], db[NV][V];
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int j = 0; j < V / 2; ++j) dw[i][j] = db[i][j] = 0;
+    for (int j = 0; j < V; ++j) dw[i][j] = db[i][j] = 0.f;
   const float inv = 1.0f / float(hidden);
   int stage = 0, turn = 0, slot = 0, before = -1;     // before: the stage that the last tile was in
   float next_mean = 0.f, next_rstd = 0.f;             // of the row after this one
@@ -262,53 +260,46 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
   fetch_stats(int64_t(blockIdx.x) * shape.rows + first_r);
   for (int64_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
     mbar_wait(smem_u32(&s_bar[stage]), turn & 1, wctx);
-    const uint8_t* tx = ring + uint32_t(stage) * n_tensors * shape.slot_bytes;
+    const uint32_t tx = base + uint32_t(stage) * n_tensors * shape.slot_bytes;
     const int64_t row0 = tile * shape.rows;
     const int n_rows = int(min(int64_t(shape.rows), n_tokens - row0));
     const int lead = kRagged ? int(row0 * hidden & (V - 1)) : 0;      // elements in front of the tile in its slot
     for (int r = first_r; r < n_rows; r += kWarp ? kRowsPerCta : 1, slot ^= 1) {
       const int64_t row = row0 + r, at = row * hidden;
       const int o = lead + r * hidden, a = kRagged ? o & (V - 1) : 0;
-      const XT *sx = reinterpret_cast<const XT*>(tx) + o, *sg = reinterpret_cast<const XT*>(tx + shape.slot_bytes) + o;
-      const XT* sd = reinterpret_cast<const XT*>(tx + 2 * shape.slot_bytes) + o;
+      const uint32_t sx = tx + uint32_t(o * kE), sg = sx + shape.slot_bytes, sd = sg + shape.slot_bytes;
       const float mean = next_mean, rstd = next_rstd;
       fetch_stats(kWarp && r + kRowsPerCta < n_rows ? row + kRowsPerCta : (tile + gridDim.x) * shape.rows + first_r);
-      // u = x rstd - mean rstd, in pairs
-      const uint64_t r2 = pack_f32x2(rstd, rstd), m2 = pack_f32x2(-mean * rstd, -mean * rstd);
-      uint64_t sum_u = 0, sum_1 = 0;
-      uint64_t ku[kKeep ? NV : 1][V / 2], kg[kKeep ? NV : 1][V / 2];     // u and g w, where there are registers for them
+      const float shift = -mean * rstd;         // u = x rstd + shift
+      float sum[2] = {0.f, 0.f};
+      float ku[kKeep ? NV : 1][V], kg[kKeep ? NV : 1][V];     // u and g w, where there are registers for them
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int col = (i * group + tid) * V;
         if (col >= hidden) continue;
-        Vec<XT, V> px = shared_vec<XT, kRagged>(sx + col, a), pg = shared_vec<XT, kRagged>(sg + col, a);
+        Vec<XT, V> px = shared_vec<XT, V, kRagged>(sx + col * kE, a), pg = shared_vec<XT, V, kRagged>(sg + col * kE, a);
         if (kRagged && col + V > hidden) {    // what follows the row
           zero_behind(px, hidden - col);
           zero_behind(pg, hidden - col);
         }
-        uint64_t u[V / 2], g[V / 2], wp[V / 2];
-        pairs(px, u);
-        pairs(pg, g);
-        pairs(load_vec<WT, V>(reinterpret_cast<const WT*>(s_weight) + col), wp);
+        float u[V], g[V], w[V];
+        px.get(u);
+        pg.get(g);
+        shared_vec<WT, V, false>(sw + col * kW, 0).get(w);
 #pragma unroll
-        for (int j = 0; j < V / 2; ++j) {
-          u[j] = fma_f32x2(u[j], r2, m2);
-          dw[i][j] = fma_f32x2(g[j], u[j], dw[i][j]);
-          db[i][j] = add_f32x2(db[i][j], g[j]);
-          g[j] = mul_f32x2(g[j], wp[j]);
-          sum_u = fma_f32x2(g[j], u[j], sum_u);
-          sum_1 = add_f32x2(sum_1, g[j]);
+        for (int j = 0; j < V; ++j) {
+          u[j] = u[j] * rstd + shift;
+          dw[i][j] += g[j] * u[j];
+          db[i][j] += g[j];
+          g[j] *= w[j];
+          sum[0] += g[j] * u[j];
+          sum[1] += g[j];
           if (kKeep) {
             ku[kKeep ? i : 0][j] = u[j];
             kg[kKeep ? i : 0][j] = g[j];
           }
         }
       }
-      float sum[2], odd[2];
-      unpack_f32x2(sum_u, sum[0], odd[0]);
-      unpack_f32x2(sum_1, sum[1], odd[1]);
-      sum[0] += odd[0];
-      sum[1] += odd[1];
       row_sum<kWarp>(sum, s_part, slot);
       // (a row for all threads: they have left the tile before this one)
       if (!kWarp && before >= 0 && threadIdx.x == 0 && asked < n_tiles && !s_abort) {
@@ -318,51 +309,39 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
       }
       // dx = (g w - u c_u - c_1) rstd + d_total
       const float c_u = -sum[0] * inv * rstd, c_1 = rms ? 0.f : -sum[1] * inv * rstd;
-      const uint64_t cu2 = pack_f32x2(c_u, c_u), c12 = pack_f32x2(c_1, c_1);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int col = (i * group + tid) * V - a;
         if (col >= hidden) continue;
-        uint64_t u[V / 2], g[V / 2], wp[V / 2], t[V / 2];
-        const WT* sw = reinterpret_cast<const WT*>(s_weight) + col;
+        float u[V], g[V], d[V];
         if (kKeep) {
 #pragma unroll
-          for (int j = 0; j < V / 2; ++j) { u[j] = ku[kKeep ? i : 0][j]; g[j] = kg[kKeep ? i : 0][j]; }
+          for (int j = 0; j < V; ++j) { u[j] = ku[kKeep ? i : 0][j]; g[j] = kg[kKeep ? i : 0][j]; }
         } else {
-          pairs(load_vec<XT, V>(sx + col), u);
-          pairs(load_vec<XT, V>(sg + col), g);
-        }
-        if (kKeep) {
-        } else if (kRagged) {
-          constexpr int kPer = 16 / int(sizeof(WT)), P = V / kPer;      // the weights from column -a on: k elements into their vectors
-          const int k = -a & (kPer - 1);
-          const uint4* q = reinterpret_cast<const uint4*>(sw - k);
-          uint4 w4[P];
+          float w[V];
+          shared_vec<XT, V, false>(sx + col * kE, 0).get(u);
+          shared_vec<XT, V, false>(sg + col * kE, 0).get(g);
+          shared_vec<WT, V, kRagged>(sw + col * kW, -a & (16 / kW - 1)).get(w);
 #pragma unroll
-          for (int n = 0; n < P; ++n) w4[n] = shift_pair<int(sizeof(WT))>(q[n], q[n + 1], k);
-          Vec<WT, V> v;
-          memcpy(&v, w4, sizeof(w4));
-          pairs(v, wp);
-        } else {
-          pairs(load_vec<WT, V>(sw), wp);
+          for (int j = 0; j < V; ++j) {
+            u[j] = u[j] * rstd + shift;
+            g[j] *= w[j];
+          }
         }
+#pragma unroll
+        for (int j = 0; j < V; ++j) d[j] = g[j] * rstd + (u[j] * c_u + c_1);
         if (d_total) {
+          float t[V];
           if (n_tensors == 3) {
-            pairs(load_vec<XT, V>(sd + col), t);
+            shared_vec<XT, V, false>(sd + col * kE, 0).get(t);
           } else {
             const uint4 q = load_window(d_total, at + col, all);
             Vec<XT, V> v;
             memcpy(&v, &q, 16);
-            pairs(v, t);
+            v.get(t);
           }
-        }
-        float d[V];
 #pragma unroll
-        for (int j = 0; j < V / 2; ++j) {
-          const uint64_t un = kKeep ? u[j] : fma_f32x2(u[j], r2, m2), gw = kKeep ? g[j] : mul_f32x2(g[j], wp[j]);
-          uint64_t v = fma_f32x2(gw, r2, fma_f32x2(un, cu2, c12));
-          if (d_total) v = add_f32x2(v, t[j]);
-          unpack_f32x2(v, d[2 * j], d[2 * j + 1]);
+          for (int j = 0; j < V; ++j) d[j] += t[j];
         }
         store_window(dx, at + col, d, -col, hidden - col);
       }
@@ -385,27 +364,30 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
       while (!mbar_try_wait(smem_u32(&s_bar[q % shape.stages]), (q / shape.stages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
   }
   __syncthreads();
-  float* mine_dw = partial + int64_t(blockIdx.x) * 2 * hidden;
-  float* s_sum = reinterpret_cast<float*>(ring);
-  for (int k = 0; k < (kWarp ? kRowsPerCta : 1); ++k) {     // the warps' rows are added in the warps' order
-    if (!kWarp || k == warp) {
+  // The sums of a CTA's warps, each in a place of its own over the ring, are added in the warps' order.
+  const int pitch = part_pitch(hidden);
+  float* mine_dw = partial + int64_t(blockIdx.x) * 2 * pitch;
+  float* to = kWarp ? reinterpret_cast<float*>(ring) + warp * 2 * pitch : mine_dw;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int col = (i * group + tid) * V;
+  for (int i = 0; i < NV; ++i) {
+    const int col = (i * group + tid) * V;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          if (col + j >= hidden) continue;
-          float e[2], f[2];
-          unpack_f32x2(dw[i][j / 2], e[0], e[1]);
-          unpack_f32x2(db[i][j / 2], f[0], f[1]);
-          s_sum[col + j] = (k ? s_sum[col + j] : 0.f) + e[j & 1];
-          s_sum[hidden + col + j] = (k ? s_sum[hidden + col + j] : 0.f) + f[j & 1];
-        }
-      }
+    for (int j = 0; j < V; j += 4) {
+      if (col + j >= pitch) continue;
+      *reinterpret_cast<float4*>(to + col + j) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
+      *reinterpret_cast<float4*>(to + pitch + col + j) = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
     }
-    __syncthreads();
   }
-  for (int c = threadIdx.x; c < 2 * hidden; c += blockDim.x) mine_dw[c] = s_sum[c];
+  if (kWarp) {
+    __syncthreads();
+    const float* sums = reinterpret_cast<const float*>(ring);
+    for (int c = threadIdx.x; c < 2 * pitch; c += blockDim.x) {
+      float v = 0.f;
+#pragma unroll
+      for (int k = 0; k < kRowsPerCta; ++k) v += sums[k * 2 * pitch + c];
+      mine_dw[c] = v;
+    }
+  }
 }
 
 // dw (blockIdx.y = 0) and db (1): the parts of all CTAs, added in a fixed order.
@@ -417,17 +399,18 @@ norm_sum_kernel(const float* partial, int32_t n_parts, int32_t hidden, WT* dweig
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
   behind_wait();
   behind_go();
+  const int pitch = part_pitch(hidden);
   float v = 0.f;
   if (col < hidden) {
     int p = part;
     for (; p + 7 * kSumRows < n_parts; p += 8 * kSumRows) {
       float w[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = partial[(int64_t(p + k * kSumRows) * 2 + blockIdx.y) * hidden + col];
+      for (int k = 0; k < 8; ++k) w[k] = partial[(int64_t(p + k * kSumRows) * 2 + blockIdx.y) * pitch + col];
 #pragma unroll
       for (int k = 0; k < 8; ++k) v += w[k];
     }
-    for (; p < n_parts; p += kSumRows) v += partial[(int64_t(p) * 2 + blockIdx.y) * hidden + col];
+    for (; p < n_parts; p += kSumRows) v += partial[(int64_t(p) * 2 + blockIdx.y) * pitch + col];
   }
   s[part][lane] = v;
   __syncthreads();
@@ -461,7 +444,7 @@ Division divide_bwd(int32_t hidden, int elem_bytes) {
 }
 
 // CTAs of the backward for an SM: 512 threads of 128 registers.
-int ctas_per_sm(const Division& d) { return d.threads == 32 ? 2 : std::max(1, std::min(4, 512 / d.threads)); }
+int ctas_per_sm(const Division& d) { return d.threads == 32 ? 2 : std::max(1, std::min(8, 512 / d.threads)); }
 // Rows of a tile: one, or 8 for each of a CTA's warps, fewer where all tiles would not fill the SMs, and 8 KB of a tensor at most.
 int tile_rows(const Division& d, int64_t n_tokens, int32_t hidden, int elem_bytes) {
   if (d.threads != 32) return 1;
@@ -470,7 +453,9 @@ int tile_rows(const Division& d, int64_t n_tokens, int32_t hidden, int elem_byte
   return rows;
 }
 int64_t part_count(const Division& d, int64_t n_tokens, int rows) {
-  return std::max<int64_t>(1, std::min<int64_t>((n_tokens + rows - 1) / rows, int64_t(kSmCount) * ctas_per_sm(d)));
+  const int64_t tiles = std::max<int64_t>(1, (n_tokens + rows - 1) / rows), most = int64_t(kSmCount) * ctas_per_sm(d);
+  const int64_t each = (tiles + most - 1) / most;      // and no more than it takes for the busiest one's number of tiles
+  return (tiles + each - 1) / each;
 }
 
 template <typename F>
@@ -536,7 +521,8 @@ struct Backward {
     shape.staged = d_total && 3 * shape.slot_bytes <= room ? 3 : 2;
     const uint32_t stage = uint32_t(shape.staged) * shape.slot_bytes;
     shape.stages = int(std::max(1u, std::min(8u, std::min(room / stage, 1 + 98304 / stage))));
-    const uint32_t smem = std::max(shape.stages * stage, uint32_t(hidden) * 8) + shape.w_bytes + 16;
+    const uint32_t sums = kWarp ? uint32_t(kRowsPerCta * 2 * 4 * part_pitch(hidden)) : 0u;
+    const uint32_t smem = std::max(shape.stages * stage + shape.w_bytes, sums) + 16;
     const int64_t parts = part_count(d, n_tokens, shape.rows);
     auto kernel = norm_bwd_kernel<XT, WT, NV, kWarp, kRagged>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return PSA_ERR_CUDA;
@@ -594,7 +580,7 @@ extern "C" size_t psa_norm_bwd_workspace_bytes(int64_t n_tokens, int32_t hidden)
     const psa::Division d = psa::divide_bwd(hidden, e);
     parts = std::max(parts, size_t(psa::part_count(d, n_tokens, psa::tile_rows(d, n_tokens, hidden, e))));
   }
-  return parts * 2 * size_t(hidden) * 4;
+  return parts * 2 * size_t(psa::part_pitch(hidden)) * 4;
 }
 
 extern "C" psa_status_t psa_norm_bwd(const void* d_out, const void* x, const void* weight, const float* stats,
