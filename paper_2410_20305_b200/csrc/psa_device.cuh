@@ -412,13 +412,10 @@ __device__ __forceinline__ void umma_commit_pair_w(uint32_t bar, uint32_t leader
       : "memory");
 }
 
-// Adds eight floats of a CTA of the cluster (address from cluster_map).
-__device__ __forceinline__ void add_cluster8(uint32_t addr, float (&x)[8]) {
-  float v[8];
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr) : "memory");
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(addr + 16u) : "memory");
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] += v[i];
+__device__ __forceinline__ uint4 ld_cluster_v4(uint32_t cluster_addr) {   // (address from cluster_map)
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(cluster_addr) : "memory");
+  return v;
 }
 
 // Warpgroup register reallocation (all four warps of an aligned warpgroup must execute it).

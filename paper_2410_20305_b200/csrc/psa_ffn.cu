@@ -15,6 +15,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "psa.h"
 #include "psa_device.cuh"
@@ -176,8 +177,28 @@ __device__ __forceinline__ void finish8(const ProductList& list, const Product& 
   }
 }
 
+// The sums of eight elements over a cluster's CTAs, in their order.  All reads are on their way before the first is needed: one
+// after the other, a trip to another SM each, they took more time than the product (19 us of which @PARTS@ were left at 100 x 1024 x 2816).
+__device__ __forceinline__ void add_parts(uint32_t from, int splits, float (&x)[8]) {
+  uint4 v[8][2];
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+    if (s < splits) {
+      const uint32_t addr = cluster_map(from, uint32_t(s));
+      v[s][0] = ld_cluster_v4(addr);
+      v[s][1] = ld_cluster_v4(addr + 16);
+    }
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+    if (s < splits) {
+      const uint32_t w[8] = {v[s][0].x, v[s][0].y, v[s][0].z, v[s][0].w, v[s][1].x, v[s][1].y, v[s][1].z, v[s][1].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] += __uint_as_float(w[i]);
+    }
+}
+
 template <int EPI>
-__global__ void __launch_bounds__(kSmallThreads)
+__global__ void __launch_bounds__(kSmallThreads, 2)
 ffn_small_kernel(const __grid_constant__ ProductList list) {
   constexpr int kBN = kSmallBN;
   constexpr int kTileN = EPI == kEpiGate ? kBN / 2 : kBN;      // features per tile
@@ -337,11 +358,9 @@ ffn_small_kernel(const __grid_constant__ ProductList list) {
       uint4 g, u;
       load_gate(at.m0 + r, col, g, u);
       float x[8] = {}, y[8] = {};
-      for (int s = 0; s < splits; ++s) {
-        const uint32_t from = cluster_map(base + uint32_t(r * kPartPitch + c) * 4, uint32_t(s));
-        add_cluster8(from, x);
-        if (EPI == kEpiGate) add_cluster8(from + kTileN * 4, y);
-      }
+      const uint32_t from = base + uint32_t(r * kPartPitch + c) * 4;
+      add_parts(from, splits, x);
+      if (EPI == kEpiGate) add_parts(from + kTileN * 4, splits, y);
       finish8<EPI>(list, p, at.sel, at.m0 + r, col, x, y, g, u);
     }
     cluster_arrive();
@@ -717,17 +736,70 @@ psa_status_t launch(void (*kernel)(Params...), int64_t grid, unsigned threads, u
   return check_last_cuda_error("psa_ffn launch");
 }
 
+// Estimates in us that choose between the two kernels and the parts of K, fitted to both at 36 sizes (16 to 2500 tokens,
+// 512 x 1408 to 4096 x 14336, L2 cold; most within 15 %).  A pair's stage takes 0.37 with all SMs at work, 0.31 with few, the
+// end of a tile 2.4 and more where it is not hidden behind the next tile's stages.  A stage of a CTA alone takes 0.38 (0.25 with
+// few tokens), of an SM's two CTAs together 0.56; the parts of a split K cross between the SMs of their cluster at 1 TB/s
+// (2816 features, K = 1024, 128 tokens in 8 parts: 23 MB, 45 us instead of 16).  Where they differ most: 1815 x 2048,
+// K = 5632: 40 us by pairs, 53 without; 129 tokens, dX = 1024, K = 2 x 2816: 36 by pairs, 22 in 4 parts of K.
+double dram_us(const Wanted* w, int n, int epilogue) {
+  double bytes = 0;
+  for (int i = 0; i < n; ++i)
+    bytes += 2.0 * (double(w[i].M) * w[i].K * w[i].k_pairs + double(w[i].K) * w[i].N * (w[i].b[1].p ? 2 : 1) +
+                    double(w[i].M) * w[i].N * w[i].n_outputs * (epilogue == kEpiOut ? 1 : 3));
+  return bytes / 6.0e6;
+}
+double pairs_us(const Wanted* w, int n, int epilogue) {
+  const int tile_n = epilogue == kEpiGate ? kBigBN / 2 : kBigBN;
+  const double clusters = kSmCount / 2;
+  double sum = 0, longest = 0, tiles = 0;
+  for (int i = 0; i < n; ++i) tiles += double(tiles_of(w[i], kBigBM, tile_n));
+  const double stage = tiles <= clusters / 2 ? 0.31 : 0.37;
+  for (int i = 0; i < n; ++i) {
+    const double stages = double(stages_of(w[i])), end = epilogue == kEpiGate ? 7.5 : epilogue == kEpiGateBwd ? 14 : 2.4 + 0.2 * stages;
+    const double each = std::max(stage * stages, end);
+    sum += each * double(tiles_of(w[i], kBigBM, tile_n));
+    longest = std::max(longest, each);
+  }
+  const double work = n == 1 ? std::ceil(tiles / clusters) * longest : std::max(longest, sum / clusters + longest / 2);
+  return 9 + (epilogue == kEpiOut ? 0 : 4) + std::max(work, dram_us(w, n, epilogue));
+}
+double small_us(const Wanted* w, int n, int epilogue, int splits) {
+  const int tile_n = epilogue == kEpiGate ? kSmallBN / 2 : kSmallBN;
+  const double sms = kSmCount;
+  double work = 0, join = 0, longest = 0;
+  for (int i = 0; i < n; ++i) {
+    const bool few = w[i].M <= 64;
+    const double stages = std::ceil(double(stages_of(w[i])) / splits), tiles = double(tiles_of(w[i], kSmallBM, tile_n));
+    const double alone = std::max((few ? 0.25 : 0.38) * stages, 3.0), both = std::max((few ? 0.36 : 0.56) * stages, 6.0);   // a CTA, two of an SM
+    const double ctas = tiles * splits, waves = std::floor(ctas / (2 * sms)), rest = ctas - waves * 2 * sms, second = std::max(0.0, rest / sms - 1);
+    // what a tile's end adds where one CTA does all of it
+    const double end_alone = splits > 1 || epilogue == kEpiOut ? 0 : epilogue == kEpiGate ? 4 : 7, end_both = end_alone == 7 ? 24 : end_alone;
+    if (n == 1)
+      work = waves * (both + end_both) + (rest > 0 ? alone + end_alone + second * (both - alone + end_both - end_alone) : 0);
+    else
+      work += ctas / (2 * sms) * both;
+    longest = std::max(longest, alone);
+    join += tiles * (splits - 1) * double(std::min<int64_t>(w[i].M, kSmallBM)) * (4 * kSmallBN) / 1.0e6;
+  }
+  return 10 + (splits > 1 ? 2 : 0) + join + std::max({n == 1 ? work : work + longest / 2, longest, dram_us(w, n, epilogue)});
+}
+int best_splits(const Wanted* w, int n, int epilogue) {
+  int best = 1;
+  for (int s = 2; s <= 8; s *= 2)
+    if (small_us(w, n, epilogue, s) < small_us(w, n, epilogue, best)) best = s;
+  return best;
+}
+double best_us(const Wanted* w, int n, int epilogue) {
+  return std::min(pairs_us(w, n, epilogue), small_us(w, n, epilogue, best_splits(w, n, epilogue)));
+}
+
 // Products that do not depend on one another, in one launch.
 template <int EPI>
 psa_status_t run(const Wanted* wanted, int n, ProductList list, cudaStream_t stream) {
-  int64_t big = 0, small = 0, longest = 0;
   constexpr int kBigN = EPI == kEpiGate ? kBigBN / 2 : kBigBN, kSmallN = EPI == kEpiGate ? kSmallBN / 2 : kSmallBN;
-  for (int i = 0; i < n; ++i) {
-    big += tiles_of(wanted[i], kBigBM, kBigN);
-    small += tiles_of(wanted[i], kSmallBM, kSmallN);
-    longest = std::max(longest, stages_of(wanted[i]));
-  }
-  const bool pairs = big >= 40 && wanted[0].M > kSmallBM;
+  list.splits = best_splits(wanted, n, EPI);
+  const bool pairs = pairs_us(wanted, n, EPI) < small_us(wanted, n, EPI, list.splits);
   const int edge_m = pairs ? kBigBM : kSmallBM, edge_n = pairs ? kBigN : kSmallN;
   list.n_products = n;
   list.a_rows = pairs || n > 1 || wanted[0].a[0].mn_major ? 128 : small_rows(wanted[0].M);
@@ -757,7 +829,6 @@ psa_status_t run(const Wanted* wanted, int n, ProductList list, cudaStream_t str
   }
   if (first > 0x7fffffff / 8) return PSA_ERR_UNSUPPORTED;
   list.n_work = int32_t(first);
-  list.splits = 1;
   if (pairs) {
     const Wanted& w = wanted[0];
     if (EPI != kEpiOut && !matrix_map(&list.store_h, list.h, w.M, w.N, 32, EPI == kEpiGateBwd ? 32 : 64)) return PSA_ERR_CUDA;
@@ -765,7 +836,6 @@ psa_status_t run(const Wanted* wanted, int n, ProductList list, cudaStream_t str
       return PSA_ERR_CUDA;
     return launch(ffn_big_kernel<EPI>, 2 * std::min<int64_t>(first, kSmCount / 2), kBigThreads, kBigSmem, 0, stream, list);
   }
-  while (list.splits < 8 && 2 * list.splits * small <= 2 * kSmCount && longest >= 8 * list.splits) list.splits *= 2;
   return launch(ffn_small_kernel<EPI>, first * list.splits, kSmallThreads, kSmallSmem, list.splits, stream, list);
 }
 
@@ -863,5 +933,8 @@ extern "C" psa_status_t psa_ffn_bwd(const void* d_out, const void* x, const void
       {hidden, ffn, n_tokens, {{x, true}}, {{d_gate, true}, {d_up, true}}, {bf(dw_gate), bf(dw_up)}, 1, 2, false},
       // dWd = H^T dY
       {ffn, hidden, n_tokens, {{h, true}}, {{d_out, true}}, {bf(dw_down)}, 1, 1, true}};
-  return run<kEpiOut>(last, 3, list, st);
+  // One launch, unless dX, with its long K in few tiles, does better alone (less 4 us: the second starts behind the first).
+  if (best_us(last, 3, kEpiOut) <= best_us(last, 1, kEpiOut) + best_us(last + 1, 2, kEpiOut) - 4) return run<kEpiOut>(last, 3, list, st);
+  const psa_status_t first = run<kEpiOut>(last, 1, list, st);
+  return first != PSA_OK ? first : run<kEpiOut>(last + 1, 2, list, st);
 }
