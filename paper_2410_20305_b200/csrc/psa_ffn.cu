@@ -178,7 +178,7 @@ __device__ __forceinline__ void finish8(const ProductList& list, const Product& 
 }
 
 // The sums of eight elements over a cluster's CTAs, in their order.  All reads are on their way before the first is needed: one
-// after the other, a trip to another SM each, they took more time than the product (19 us of which @PARTS@ were left at 100 x 1024 x 2816).
+// after the other, a trip to another SM each, they took more time than the product at a hundred tokens.
 __device__ __forceinline__ void add_parts(uint32_t from, int splits, float (&x)[8]) {
   uint4 v[8][2];
 #pragma unroll

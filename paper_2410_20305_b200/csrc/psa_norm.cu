@@ -167,7 +167,7 @@ __device__ __forceinline__ void zero_behind(Vec<T, V>& v, int n) {
 // The backward.  A CTA takes every gridDim.x-th tile of rows: one row for all its threads, or, of narrow rows, some for each of
 // its warps.  Tiles are contiguous in memory and come by bulk copies into a ring of stages, so that several are in flight
 // whatever the arithmetic waits for (31041 x 4096 bf16 with d_total: 346 us with loads where the values are used, 253 with the
-// next row's in registers, @NB@ so).  For the sums over tokens a thread keeps its columns [k V, (k + 1) V) throughout; of dx it
+// next row's in registers, 187 so).  For the sums over tokens a thread keeps its columns [k V, (k + 1) V) throughout; of dx it
 // writes window k of each row (the same columns where rows are aligned).  partial: [gridDim.x][2][part_pitch].
 // A part's rows of sums start at 16 bytes.
 __host__ __device__ constexpr int part_pitch(int hidden) { return (hidden + 3) / 4 * 4; }
