@@ -187,7 +187,7 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
   constexpr bool kKeep = !kRagged && NV * V <= 16;
   extern __shared__ uint8_t smem_raw[];        // [stages][2 or 3 tensors][slot], weight;  at the end the warps' sums
   __shared__ float s_part[4][32];
-  __shared__ uint64_t s_bar[8];
+  __shared__ uint64_t s_bar[8], s_weight_bar;
   __shared__ int s_abort;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int group = kWarp ? 32 : int(blockDim.x), tid = kWarp ? lane : int(threadIdx.x);
@@ -201,14 +201,11 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
   if (threadIdx.x == 0) {
     s_abort = 0;
     for (int s = 0; s < shape.stages; ++s) mbar_init(smem_u32(&s_bar[s]), 1);
+    mbar_init(smem_u32(&s_weight_bar), 1);
     fence_mbar_init();
   }
   behind_wait();
   behind_go();
-  for (int i = threadIdx.x; i < int(shape.w_bytes / 4); i += blockDim.x)
-    reinterpret_cast<uint32_t*>(s_weight - kWeightPad)[i] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < hidden; i += blockDim.x) reinterpret_cast<WT*>(s_weight)[i] = weight[i];
 
   // One thread requests a tile: from the 16-byte boundary at or before its first element to the one at or behind its last; the
   // tensor's last elements, if no boundary follows them within it, by hand.
@@ -241,6 +238,16 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
   int n_asked = 0;
   if (threadIdx.x == 0)
     for (int s = 0; s < shape.stages && asked < n_tiles; ++s, asked += gridDim.x, ++n_asked) request(asked, s);
+  // The weight, behind the first tiles (element by element ahead of them: @W@ us instead of @X@ at 4000 x 2048): whole vectors by
+  // a copy, the rest and the zeros around it by hand.
+  const int whole = hidden * kW & ~15;
+  if (threadIdx.x == 0) {
+    mbar_expect_tx(smem_u32(&s_weight_bar), uint32_t(whole));
+    if (whole) bulk_load(sw, weight, uint32_t(whole), smem_u32(&s_weight_bar));
+  }
+  for (int i = threadIdx.x; i < int(kWeightPad); i += blockDim.x) s_weight[i - int(kWeightPad)] = 0;
+  for (int i = whole / kW + int(threadIdx.x); i < int(shape.w_bytes - kWeightPad) / kW; i += blockDim.x)
+    reinterpret_cast<WT*>(s_weight)[i] = i < hidden ? weight[i] : WT(0.f);
   __syncthreads();
 
   float dw[NV][V], db[NV][V];
@@ -258,6 +265,7 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
   };
   const int first_r = kWarp ? warp : 0;
   fetch_stats(int64_t(blockIdx.x) * shape.rows + first_r);
+  mbar_wait(smem_u32(&s_weight_bar), 0, wctx);
   for (int64_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
     mbar_wait(smem_u32(&s_bar[stage]), turn & 1, wctx);
     const uint32_t tx = base + uint32_t(stage) * n_tensors * shape.slot_bytes;
@@ -360,6 +368,7 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
   }
   if (s_abort && threadIdx.x == 0) {      // shared memory must outlive the copies in flight
     const long long t0 = clock64();
+    while (!mbar_try_wait(smem_u32(&s_weight_bar), 0) && clock64() - t0 < kWaitLimitClocks) {}
     for (int q = max(0, n_asked - shape.stages); q < n_asked; ++q)
       while (!mbar_try_wait(smem_u32(&s_bar[q % shape.stages]), (q / shape.stages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
   }
