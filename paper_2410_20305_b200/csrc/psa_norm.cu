@@ -238,7 +238,7 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
   int n_asked = 0;
   if (threadIdx.x == 0)
     for (int s = 0; s < shape.stages && asked < n_tiles; ++s, asked += gridDim.x, ++n_asked) request(asked, s);
-  // The weight, behind the first tiles (element by element ahead of them: @W@ us instead of @X@ at 4000 x 2048): whole vectors by
+  // The weight, behind the first tiles (32.7 us instead of 38.0 element by element ahead of them at 4000 x 2048 fp32): whole vectors by
   // a copy, the rest and the zeros around it by hand.
   const int whole = hidden * kW & ~15;
   if (threadIdx.x == 0) {
@@ -529,7 +529,7 @@ struct Backward {
     const uint32_t room = 224 * 1024 / ctas_per_sm(d) - 1024 - shape.w_bytes;
     shape.staged = d_total && 3 * shape.slot_bytes <= room ? 3 : 2;
     const uint32_t stage = uint32_t(shape.staged) * shape.slot_bytes;
-    shape.stages = int(std::max(1u, std::min(8u, std::min(room / stage, 1 + 98304 / stage))));
+    shape.stages = int(std::max(1u, std::min(8u, std::min(room / stage, 1 + 196608 / uint32_t(ctas_per_sm(d)) / stage))));
     const uint32_t sums = kWarp ? uint32_t(kRowsPerCta * 2 * 4 * part_pitch(hidden)) : 0u;
     const uint32_t smem = std::max(shape.stages * stage + shape.w_bytes, sums) + 16;
     const int64_t parts = part_count(d, n_tokens, shape.rows);
