@@ -28,9 +28,16 @@ constexpr int kMaxHidden = 16384;
 constexpr int kRowsPerCta = 8;      // rows of a CTA where a warp holds a row
 
 // The most threads that divide() and divide_bwd() below give a CTA.
-template <typename XT, int NV, bool kWarp>
+template <typename XT, int NV, bool kWarp, bool kRagged>
 constexpr int max_threads() {
-  return kWarp ? 32 * kRowsPerCta : NV < 4 ? 256 : std::min(1024, kMaxHidden / (16 / int(sizeof(XT)) * NV) + 32);
+  return kWarp ? 32 * kRowsPerCta : NV == 1 && kRagged ? 544 : NV < 4 ? 256 : std::min(1024, kMaxHidden / (16 / int(sizeof(XT)) * NV) + 32);
+}
+// The forward's CTAs take several rows each; an SM then holds 1024 threads of them.
+template <int NV, bool kWarp>
+__host__ __device__ constexpr bool holds() { return NV == 1 && !kWarp; }
+template <typename XT, int NV, bool kWarp, bool kRagged>
+constexpr int fwd_ctas() {
+  return holds<NV, kWarp>() ? 1088 / max_threads<XT, NV, kWarp, kRagged>() : 1;
 }
 template <typename XT, int NV, bool kWarp>
 constexpr int bwd_threads() {
@@ -52,93 +59,131 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*s_part)[32], int 
 }
 
 // A thread's columns in a row that starts `a` elements behind an aligned one: window k holds the columns [k V - a, (k + 1) V - a).
+// `stride` rows lie between the rows that a warp or CTA takes, a multiple of V where it takes several: `a`, and with it every
+// column of a thread, is the same in all of them.  Where a thread has one or two windows (kHold) it keeps its weights in
+// registers and requests the next row ahead of the sums of this one; with a CTA for each row these kernels were bound by
+// instructions, the weights' shift among them (5465 x 1237 bf16 with residual: 20.7 us, so 16.8; 4000 x 4095 35.6 and 27.7).
 template <typename XT, typename WT, int NV, bool kWarp, bool kRagged>
-__global__ void __launch_bounds__(max_threads<XT, NV, kWarp>())
-norm_kernel(const XT* x, const XT* residual, const WT* weight, const WT* bias, int64_t n_tokens, int32_t hidden, float eps,
-            int32_t rms, XT* out, XT* total, float* stats) {
+__global__ void __launch_bounds__(max_threads<XT, NV, kWarp, kRagged>(), fwd_ctas<XT, NV, kWarp, kRagged>())
+norm_kernel(const XT* x, const XT* residual, const WT* weight, const WT* bias, int64_t n_tokens, int64_t stride, int32_t hidden,
+            float eps, int32_t rms, XT* out, XT* total, float* stats) {
   constexpr int V = 16 / int(sizeof(XT));
+  constexpr bool kHold = holds<NV, kWarp>();
   using Weight = Span<WT, V, kRagged>;
   __shared__ float s_part[4][32];
   const int group = kWarp ? 32 : int(blockDim.x), tid = kWarp ? int(threadIdx.x) & 31 : int(threadIdx.x);
-  const int64_t row = kWarp ? int64_t(blockIdx.x) * kRowsPerCta + (threadIdx.x >> 5) : int64_t(blockIdx.x);
+  int64_t row = kWarp ? int64_t(blockIdx.x) * kRowsPerCta + (threadIdx.x >> 5) : int64_t(blockIdx.x);
   behind_wait();
   behind_go();
   if (kWarp && row >= n_tokens) return;
-  const int64_t at = row * hidden, all = n_tokens * hidden;
-  const int a = kRagged ? int(at & (V - 1)) : 0;
+  const int64_t all = n_tokens * hidden;
+  const int a = kRagged ? int(row * hidden & (V - 1)) : 0;
+  // (A division by the width costs the kernels that instructions bind 1 us of 13 and 8 of 62 at 4000 x 7001; the others hide it,
+  // and lost 7 us of 160 at 31041 x 4096 with the registers that the reciprocal takes.)
+  const float inv = 1.0f / float(hidden);
+  auto mean_of = [&](float v) { return kHold || kRagged ? v * inv : v / float(hidden); };
   uint4 rx[NV], rr[NV];
+  auto fetch = [&](int64_t at) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int col = (i * group + tid) * V - a;
-    if (col >= hidden) continue;
-    rx[i] = kRagged ? load_window(x, at + col, all) : *reinterpret_cast<const uint4*>(x + at + col);
-    if (residual) rr[i] = kRagged ? load_window(residual, at + col, all) : *reinterpret_cast<const uint4*>(residual + at + col);
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * group + tid) * V - a;
+      if (col >= hidden) continue;
+      rx[i] = kRagged ? load_window(x, at + col, all) : *reinterpret_cast<const uint4*>(x + at + col);
+      if (residual) rr[i] = kRagged ? load_window(residual, at + col, all) : *reinterpret_cast<const uint4*>(residual + at + col);
+    }
+  };
+  fetch(row * hidden);
+  Vec<WT, V> hw[kHold ? NV : 1], hb[kHold ? NV : 1];
+  if (kHold) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * group + tid) * V - a;
+      if (col >= hidden) continue;
+      Weight v;
+      v.load(weight, col, hidden);
+      hw[kHold ? i : 0] = v.at(col);
+      if (!bias) continue;
+      v.load(bias, col, hidden);
+      hb[kHold ? i : 0] = v.at(col);
+    }
   }
-  float s[NV][V], sum[1] = {0.f};
+  for (int slot = 0;; slot ^= 1) {
+    const int64_t at = row * hidden;
+    float s[NV][V], sum[1] = {0.f};
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int col = (i * group + tid) * V - a;
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * group + tid) * V - a;
 #pragma unroll
-    for (int j = 0; j < V; ++j) s[i][j] = 0.f;
-    if (col >= hidden) continue;
-    Vec<XT, V> v;
-    memcpy(&v, &rx[i], 16);
-    v.get(s[i]);
-    if (residual) {
-      float r[V];
-      memcpy(&v, &rr[i], 16);
-      v.get(r);
-#pragma unroll
-      for (int j = 0; j < V; ++j) s[i][j] += r[j];
-      v.set(s[i]);     // what is normalised is what the residual stream holds
+      for (int j = 0; j < V; ++j) s[i][j] = 0.f;
+      if (col >= hidden) continue;
+      Vec<XT, V> v;
+      memcpy(&v, &rx[i], 16);
       v.get(s[i]);
-      store_window(total, at + col, s[i], -col, hidden - col);
+      if (residual) {
+        float r[V];
+        memcpy(&v, &rr[i], 16);
+        v.get(r);
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[i][j] += r[j];
+        v.set(s[i]);     // what is normalised is what the residual stream holds
+        v.get(s[i]);
+        store_window(total, at + col, s[i], -col, hidden - col);
+      }
+      if (kRagged && (col < 0 || col + V > hidden))
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[i][j] = col + j >= 0 && col + j < hidden ? s[i][j] : 0.f;
+      if (!rms)
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[0] += s[i][j];
     }
-    if (kRagged && (col < 0 || col + V > hidden))
-#pragma unroll
-      for (int j = 0; j < V; ++j) s[i][j] = col + j >= 0 && col + j < hidden ? s[i][j] : 0.f;
-    if (!rms)
-#pragma unroll
-      for (int j = 0; j < V; ++j) sum[0] += s[i][j];
-  }
-  float mean = 0.f;
-  if (!rms) {
-    row_sum<kWarp>(sum, s_part, 0);
-    mean = sum[0] / float(hidden);
-  }
-  float sq[1] = {0.f};
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int col = (i * group + tid) * V - a;
-    if (col >= hidden) continue;
-    if (kRagged && (col < 0 || col + V > hidden)) {
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (col + j >= 0 && col + j < hidden) sq[0] += (s[i][j] - mean) * (s[i][j] - mean);
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) sq[0] += (s[i][j] - mean) * (s[i][j] - mean);
+    const int64_t next = row + stride;
+    if (kHold && next < n_tokens) fetch(next * hidden);
+    float mean = 0.f;
+    if (!rms) {
+      row_sum<kWarp>(sum, s_part, 0);
+      mean = mean_of(sum[0]);
     }
-  }
-  row_sum<kWarp>(sq, s_part, 1);
-  const float rstd = 1.0f / sqrtf(sq[0] / float(hidden) + eps);
-  if (tid == 0) {
-    stats[row] = mean;
-    stats[n_tokens + row] = rstd;
-  }
+    float sq[1] = {0.f};
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int col = (i * group + tid) * V - a;
-    if (col >= hidden) continue;
-    Weight ww, wb;
-    float w[V], b[V], y[V];
-    ww.load(weight, col, hidden);
-    if (bias) wb.load(bias, col, hidden);
-    ww.at(col).get(w);
-    wb.at(col).get(b);
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * group + tid) * V - a;
+      if (col >= hidden) continue;
+      if (kRagged && (col < 0 || col + V > hidden)) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) y[j] = (s[i][j] - mean) * rstd * w[j] + (bias ? b[j] : 0.f);
-    store_window(out, at + col, y, -col, hidden - col);
+        for (int j = 0; j < V; ++j)
+          if (col + j >= 0 && col + j < hidden) sq[0] += (s[i][j] - mean) * (s[i][j] - mean);
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) sq[0] += (s[i][j] - mean) * (s[i][j] - mean);
+      }
+    }
+    row_sum<kWarp>(sq, s_part, rms ? slot : 1);      // (a place that nobody still reads)
+    const float rstd = 1.0f / sqrtf(mean_of(sq[0]) + eps);
+    if (tid == 0) {
+      stats[row] = mean;
+      stats[n_tokens + row] = rstd;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = (i * group + tid) * V - a;
+      if (col >= hidden) continue;
+      float w[V], b[V], y[V];
+      if (kHold) {
+        hw[kHold ? i : 0].get(w);
+        hb[kHold ? i : 0].get(b);
+      } else {
+        Weight ww, wb;
+        ww.load(weight, col, hidden);
+        if (bias) wb.load(bias, col, hidden);
+        ww.at(col).get(w);
+        wb.at(col).get(b);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) y[j] = (s[i][j] - mean) * rstd * w[j] + (bias ? b[j] : 0.f);
+      store_window(out, at + col, y, -col, hidden - col);
+    }
+    if (!kHold || next >= n_tokens) return;
+    row = next;
   }
 }
 
@@ -441,7 +486,7 @@ int vectors(int32_t hidden, int elem_bytes) {
 Division divide(int32_t hidden, int elem_bytes) {
   const int n = vectors(hidden, elem_bytes);
   if (n <= 128) return {n <= 32 ? 1 : n <= 64 ? 2 : 4, 32};
-  const int nv = n <= 256 ? 1 : n <= 512 ? 2 : n <= 4096 ? 4 : 8;
+  const int nv = n <= (hidden * elem_bytes % 16 ? 544 : 256) ? 1 : n <= 512 ? 2 : n <= 4096 ? 4 : 8;
   return {nv, ((n + nv - 1) / nv + 31) / 32 * 32};
 }
 // The backward: a warp a row of up to 1024 columns, else 16 columns a thread for up to 512 threads, else 32.
@@ -494,10 +539,12 @@ struct Forward {
   }
   template <int NV, bool kWarp, bool kRagged>
   psa_status_t go() {
-    const int64_t grid = kWarp ? (n_tokens + kRowsPerCta - 1) / kRowsPerCta : n_tokens;
+    int64_t grid = kWarp ? (n_tokens + kRowsPerCta - 1) / kRowsPerCta : n_tokens;
+    if (holds<NV, kWarp>()) grid = std::min<int64_t>(grid, kSmCount * (1088 / threads) & ~7);      // (a multiple of V)
+    const int64_t stride = kWarp ? grid * kRowsPerCta : grid;
     launch_behind(true, norm_kernel<XT, WT, NV, kWarp, kRagged>, dim3(unsigned(grid)), kWarp ? 32 * kRowsPerCta : threads, 0, stream,
         static_cast<const XT*>(x), static_cast<const XT*>(residual), static_cast<const WT*>(weight), static_cast<const WT*>(bias),
-        n_tokens, hidden, eps, rms, static_cast<XT*>(out), static_cast<XT*>(total), stats);
+        n_tokens, stride, hidden, eps, rms, static_cast<XT*>(out), static_cast<XT*>(total), stats);
     return check_last_cuda_error("psa_norm launch");
   }
 };

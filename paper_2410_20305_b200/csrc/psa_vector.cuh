@@ -92,6 +92,19 @@ __device__ __forceinline__ uint4 shift_pair(const uint4& lo, const uint4& hi, in
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// One window: the aligned vector at element `first`, elements behind the tensor's end as zeros.
+template <typename T>
+__device__ __forceinline__ uint4 load_window(const T* p, int64_t first, int64_t all) {
+  constexpr int W = 16 / int(sizeof(T));
+  if (first + W <= all) return *reinterpret_cast<const uint4*>(p + first);
+  T v[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) v[j] = first + j < all ? p[first + j] : T(0.f);
+  uint4 r;
+  memcpy(&r, v, 16);
+  return r;
+}
+
 // V elements (a multiple of 16 bytes) from element `first` on of a tensor of `all` elements; those outside it read as zeros.
 // kAny: from any element on, of which some may lie outside; else from a multiple of V within the tensor.
 template <typename T, int V, bool kAny>
@@ -105,17 +118,10 @@ struct Span {
       return;
     }
     const int64_t q = first & ~int64_t(W - 1);
-    if (q >= 0 && q + V + W <= all) {
 #pragma unroll
-      for (int k = 0; k <= P; ++k) r[kAny ? k : 0] = *reinterpret_cast<const uint4*>(p + q + k * W);
-    } else {
-#pragma unroll
-      for (int k = 0; k <= P; ++k) {
-        T v[W];
-#pragma unroll
-        for (int j = 0; j < W; ++j) v[j] = q + k * W + j >= 0 && q + k * W + j < all ? p[q + k * W + j] : T(0.f);
-        memcpy(&r[kAny ? k : 0], v, 16);
-      }
+    for (int k = 0; k <= P; ++k) {
+      const int64_t at = q + k * W;
+      r[kAny ? k : 0] = at < 0 || at >= all ? make_uint4(0, 0, 0, 0) : load_window(p, at, all);
     }
   }
   __device__ __forceinline__ Vec<T, V> at(int64_t first) const {
@@ -127,18 +133,6 @@ struct Span {
     return v;
   }
 };
-// One window: the aligned vector at element `first`, elements behind the tensor's end as zeros.
-template <typename T>
-__device__ __forceinline__ uint4 load_window(const T* p, int64_t first, int64_t all) {
-  constexpr int W = 16 / int(sizeof(T));
-  if (first + W <= all) return *reinterpret_cast<const uint4*>(p + first);
-  T v[W];
-#pragma unroll
-  for (int j = 0; j < W; ++j) v[j] = first + j < all ? p[first + j] : T(0.f);
-  uint4 r;
-  memcpy(&r, v, 16);
-  return r;
-}
 // Writes the elements [lo, hi) of V (a multiple of 16 bytes) that start at the aligned element `first`.
 template <typename T, int V>
 __device__ __forceinline__ void store_window(T* p, int64_t first, const float (&f)[V], int lo, int hi) {
