@@ -445,11 +445,12 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
 }
 
 // dw (blockIdx.y = 0) and db (1): the parts of all CTAs, added in a fixed order.
-constexpr int kSumRows = 16;
-template <typename WT>
-__global__ void __launch_bounds__(32 * kSumRows)
+// 16 warps for the parts of up to two CTAs an SM, 32 for more (592 parts at 5465 x 1237: 33.3 us for the whole backward with 16,
+// 28.8 with 32; 148 at 4000 x 8192: 57.5 and 59.8).
+template <typename WT, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps)
 norm_sum_kernel(const float* partial, int32_t n_parts, int32_t hidden, WT* dweight, WT* dbias) {
-  __shared__ float s[kSumRows][33];
+  __shared__ float s[kWarps][33];
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
   behind_wait();
   behind_go();
@@ -457,19 +458,19 @@ norm_sum_kernel(const float* partial, int32_t n_parts, int32_t hidden, WT* dweig
   float v = 0.f;
   if (col < hidden) {
     int p = part;
-    for (; p + 7 * kSumRows < n_parts; p += 8 * kSumRows) {
+    for (; p + 7 * kWarps < n_parts; p += 8 * kWarps) {
       float w[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = partial[(int64_t(p + k * kSumRows) * 2 + blockIdx.y) * pitch + col];
+      for (int k = 0; k < 8; ++k) w[k] = partial[(int64_t(p + k * kWarps) * 2 + blockIdx.y) * pitch + col];
 #pragma unroll
       for (int k = 0; k < 8; ++k) v += w[k];
     }
-    for (; p < n_parts; p += kSumRows) v += partial[(int64_t(p) * 2 + blockIdx.y) * pitch + col];
+    for (; p < n_parts; p += kWarps) v += partial[(int64_t(p) * 2 + blockIdx.y) * pitch + col];
   }
   s[part][lane] = v;
   __syncthreads();
   if (part == 0 && col < hidden) {
-    for (int p = 1; p < kSumRows; ++p) v += s[p][lane];
+    for (int p = 1; p < kWarps; ++p) v += s[p][lane];
     set_element((blockIdx.y ? dbias : dweight) + col, v);
   }
 }
@@ -585,7 +586,8 @@ struct Backward {
     launch_behind(true, kernel, dim3(unsigned(parts)), kWarp ? 32 * kRowsPerCta : d.threads, smem, stream,
                   static_cast<const XT*>(d_out), static_cast<const XT*>(x), static_cast<const WT*>(weight), stats,
                   static_cast<const XT*>(d_total), n_tokens, hidden, rms, static_cast<XT*>(dx), partial, shape, status);
-    launch_behind(true, norm_sum_kernel<WT>, dim3(unsigned((hidden + 31) / 32), dbias ? 2 : 1), 32 * kSumRows, 0, stream, partial,
+    const bool many = parts > 2 * kSmCount;
+    launch_behind(true, many ? norm_sum_kernel<WT, 32> : norm_sum_kernel<WT, 16>, dim3(unsigned((hidden + 31) / 32), dbias ? 2 : 1), many ? 1024 : 512, 0, stream, partial,
                   int32_t(parts), hidden, static_cast<WT*>(dweight), static_cast<WT*>(dbias));
     return check_last_cuda_error("psa_norm_bwd launch");
   }
