@@ -141,3 +141,15 @@ def test_a_bad_row_beside_rows_that_share_its_vectors(D):
     dx2, _, _ = B.psa_norm_bwd(g2, x2, w, stats2, with_bias=True)
     assert torch.equal(out[~bad], clean[~bad]) and torch.equal(dx2[~bad], dx[~bad])
     assert out[bad].isnan().all() and dx2[bad].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("V,D", [(701, 4099), (35, 9001), (100, 2305)])
+def test_ranges_of_absent_ids_in_wide_rows_that_start_anywhere(V, D, dtype):
+    ids = torch.tensor([0, 1, 7, 15, 16, 33, V - 2], dtype=torch.int32, device="cuda")
+    d_out = torch.empty((7, D), device="cuda").normal_().to(BF)
+    padded = torch.full((V + 1, D), 5.0, dtype=dtype, device="cuda")
+    B.psa_embed_bwd(d_out, ids, V, dtable=padded[:V])
+    want = torch.zeros((V, D), dtype=dtype, device="cuda")
+    want[ids.long()] = d_out.to(dtype)
+    assert torch.equal(padded[:V], want) and (padded[V:] == 5).all()
