@@ -10,6 +10,9 @@
 //     an element and writes H (and, for a backward pass, G and U) from registers;
 //     dH is never written: its tile meets G and U in registers and leaves as dG, dU and H;
 //     dX sums over two pairs of operands, one after the other; dWg and dWu are two outputs of one launch.
+// Rounded to bf16, once each: what enters a product (H, dG, dU), as tcgen05.mma takes bf16, and G and U where a backward keeps
+// them (in fp32 they would be 4 T F bytes more to write and to read; their part of a gradient's error is no larger than dG's own:
+// in all 0.0035 of the gradient in the 2-norm, 0.0017 with only the result rounded).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
