@@ -159,18 +159,18 @@ embed_index_kernel(const int32_t* ids, int32_t n_tokens, int32_t vocab, int32_t 
 }
 
 // ---------------------------------------------------------------- sums
-// blockIdx.x < n_runs: the sorted tokens [r * kRun, (r + 1) * kRun).  An id that lies within the run is written; the part of
+// blockIdx.x < n_runs: the sorted tokens [r * run, (r + 1) * run).  An id that lies within the run is written; the part of
 // one that began in an earlier run goes to slot 0 of the run, of one that only goes on in the next run to slot 1.
 // The other CTAs clear the rows of ids that do not occur (dense gradients only).  Where rows start anywhere and take several
 // slices, neighbouring ones are cleared as one range: row by row, their ends made it 288 us instead of 194 at 4000 tokens of
 // 128256 x 4095, while at one slice (50257 x 1002) rows took 81 and ranges 86.  (Clearing all rows beside the index took longer, 90
 // there: here it fills the time in which the sums wait for their rows.)  blockIdx.y: a slice of the columns.
-constexpr int kRun = 32, kZeroRows = 16;
+constexpr int kZeroRows = 16;
 
 // A thread holds one window of V columns: of the row of the table that it adds to, so that what it writes is aligned.
 template <typename XT, typename GT, bool kRagged>
 __global__ void __launch_bounds__(kThreads)
-embed_sum_kernel(const XT* d_out, const int32_t* start, const int32_t* count, const int32_t* order, const int32_t* sorted_id, int32_t n_runs,
+embed_sum_kernel(const XT* d_out, const int32_t* start, const int32_t* count, const int32_t* order, const int32_t* sorted_id, int32_t run, int32_t n_runs,
                  int64_t n_tokens, int32_t vocab, int32_t hidden, int32_t windows, float scale, int32_t accumulate, GT* dtable,
                  float* partial) {
   constexpr int V = 16 / int(sizeof(XT)), W = 16 / int(sizeof(GT)), kUnroll = kRagged ? 4 : 8;     // rows in flight
@@ -203,7 +203,7 @@ embed_sum_kernel(const XT* d_out, const int32_t* start, const int32_t* count, co
     }
     return;
   }
-  const int n_valid = start[vocab], first = int(blockIdx.x) * kRun, n = min(kRun, n_valid - first);
+  const int n_valid = start[vocab], first = int(blockIdx.x) * run, n = min(run, n_valid - first);
   if (n <= 0) return;
   // Lane l holds the run's l-th token and its id; `ends`: the next token's id is another one.
   const int mine = first + lane;
@@ -267,19 +267,19 @@ constexpr int kJoinWarps = 8;
 
 template <typename GT, int V, bool kRagged>
 __global__ void __launch_bounds__(32 * kJoinWarps)
-embed_join_kernel(const int32_t* start, const int32_t* count, const int32_t* sorted_id, int32_t vocab, int32_t hidden, int32_t windows, float scale,
+embed_join_kernel(const int32_t* start, const int32_t* count, const int32_t* sorted_id, int32_t length, int32_t vocab, int32_t hidden, int32_t windows, float scale,
                   int32_t accumulate, const float* partial, GT* dtable) {
   constexpr int W = 16 / int(sizeof(GT));
   __shared__ float s_sum[kJoinWarps][V][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = int(blockIdx.y) * 32 + lane;
-  const int run = blockIdx.x, last = run * kRun + kRun - 1;
+  const int run = blockIdx.x, last = run * length + length - 1;
   behind_wait();
   behind_go();
   if (last >= start[vocab]) return;
   const int id = sorted_id[last], from = start[id], to = from + count[id];
-  if (from < run * kRun || to <= last + 1) return;
+  if (from < run * length || to <= last + 1) return;
   const int64_t row = int64_t(id) * hidden;
-  const int col = k * V - (kRagged ? int(row & (W - 1)) : 0), n = (to - 1) / kRun - run + 1;
+  const int col = k * V - (kRagged ? int(row & (W - 1)) : 0), n = (to - 1) / length - run + 1;
   const bool live = k < windows && col < hidden;
   float acc[V] = {};
   if (live) {
@@ -314,6 +314,11 @@ embed_join_kernel(const int32_t* start, const int32_t* count, const int32_t* sor
 constexpr int64_t kMaxVocab = 1 << 24, kMaxTokens = 1 << 24;
 constexpr int kMaxEmbed = 1 << 20;
 
+// Tokens of a run: a run's rows are read one batch behind the other, so shorter runs end sooner where there are few (16 and 32: 15.9
+// and 20.5 us at 567 tokens x 94, 12.4 and 15.1 at 2192 x 56, 24.5 and 25.5 at 7965 x 1024), and cost more parts' sums where there
+// are many (35.3 and 33.6 at 16215 x 1024, 89 and 82 at 31041 x 1002).
+int run_length(int64_t T, int64_t hidden) { return T * hidden <= 1 << 23 ? 16 : 32; }
+
 size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
 
 struct EmbedWorkspace {
@@ -329,7 +334,7 @@ EmbedWorkspace workspace_layout(int64_t T, int64_t vocab, int64_t hidden) {
   w.sorted_id = at;
   at += aligned(size_t(T) * 4);
   w.partial = at;
-  w.total = at + size_t((T + kRun - 1) / kRun) * 2 * size_t(hidden / 8 + 2) * 8 * 4;
+  w.total = at + size_t((T + run_length(T, hidden) - 1) / run_length(T, hidden)) * 2 * size_t(hidden / 8 + 2) * 8 * 4;
   return w;
 }
 
@@ -367,7 +372,7 @@ psa_status_t embed_bwd(const void* d_out, const int32_t* ids, int64_t n_tokens, 
     return PSA_ERR_CUDA;
   launch_behind(true, embed_index_kernel, dim3(unsigned(ctas)), kIndexThreads, size_t(32) * bins * 4, stream, ids,
                 int32_t(n_tokens), int32_t(vocab), bins, ints(w.start), ints(w.count), ints(w.order), ints(w.sorted_id), status);
-  const int n_runs = int((n_tokens + kRun - 1) / kRun);
+  const int run = run_length(n_tokens, hidden), n_runs = int((n_tokens + run - 1) / run);
   const int windows = windows_of(hidden, V, 16 / int(sizeof(GT)));
   const unsigned slices = unsigned((windows + kThreads - 1) / kThreads);
   const unsigned threads = unsigned((windows + int(slices) * 32 - 1) / (int(slices) * 32)) * 32;     // even slices of whole warps
@@ -375,11 +380,11 @@ psa_status_t embed_bwd(const void* d_out, const int32_t* ids, int64_t n_tokens, 
   float* partial = reinterpret_cast<float*>(ws + w.partial);
   if (n_runs + zero > 0)
     launch_behind(true, embed_sum_kernel<XT, GT, kRagged>, dim3(unsigned(n_runs) + zero, slices), threads, 0, stream,
-                  static_cast<const XT*>(d_out), ints(w.start), ints(w.count), ints(w.order), ints(w.sorted_id), n_runs, n_tokens, int32_t(vocab),
+                  static_cast<const XT*>(d_out), ints(w.start), ints(w.count), ints(w.order), ints(w.sorted_id), run, n_runs, n_tokens, int32_t(vocab),
                   hidden, windows, scale, accumulate, static_cast<GT*>(dtable), partial);
   if (n_runs > 1)
     launch_behind(true, embed_join_kernel<GT, V, kRagged>, dim3(unsigned(n_runs), unsigned((windows + 31) / 32)), 32 * kJoinWarps, 0, stream, ints(w.start),
-                  ints(w.count), ints(w.sorted_id), int32_t(vocab), hidden, windows, scale, accumulate, partial, static_cast<GT*>(dtable));
+                  ints(w.count), ints(w.sorted_id), run, int32_t(vocab), hidden, windows, scale, accumulate, partial, static_cast<GT*>(dtable));
   return check_last_cuda_error("psa_embed_bwd launch");
 }
 

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2410_20305_b200 import binding as B
+from test_gpu_embed import check_bwd as check_embed_bwd
 from test_gpu_ffn import test_whole_numbers_are_exact as whole_numbers_are_exact
 
 pytestmark = pytest.mark.gpu
@@ -153,3 +154,10 @@ def test_ranges_of_absent_ids_in_wide_rows_that_start_anywhere(V, D, dtype):
     # (V - 2 is 33 again in one case: the fp32 sum of two values, in either order, rounded once more)
     want = torch.zeros((V, D), device="cuda").index_add_(0, ids.long(), d_out.float()).to(dtype)
     assert torch.equal(padded[:V], want) and (padded[V:] == 5).all()
+
+
+# (runs of 32 sorted tokens; test_gpu_embed's tensors are short enough for runs of 16)
+@pytest.mark.parametrize("kind", ["bf16", "mixed", "f32"])
+@pytest.mark.parametrize("T,V,D,how", [(9000, 3000, 1001, "text"), (20000, 64, 424, "any"), (8400, 5, 1024, "one")])
+def test_gradient_in_long_runs(T, V, D, how, kind):
+    check_embed_bwd(T, V, D, kind, how, accumulate=D == 424, seed=T)
