@@ -26,6 +26,7 @@ using namespace dev;
 constexpr int kSmCount = 148;
 constexpr int kMaxHidden = 16384;
 constexpr int kRowsPerCta = 8;      // rows of a CTA where a warp holds a row
+constexpr int kMaxGroups = 8;       // of the backward
 
 // The most threads that divide() and divide_bwd() below give a CTA.
 template <typename XT, int NV, bool kWarp, bool kRagged>
@@ -44,16 +45,16 @@ constexpr int bwd_threads() {
   return kWarp ? 32 * kRowsPerCta : NV * 16 / int(sizeof(XT)) < 32 ? 512 : 544;
 }
 
-// Sum over the threads that share a row: a warp (kWarp) or the CTA.  `slot` alternates, so that one barrier is enough.
-template <bool kWarp, int N>
-__device__ __forceinline__ void row_sum(float (&v)[N], float (*s_part)[32], int slot) {
+// Sum over the threads that share a row: a warp (kWarp) or `n_warps`, for which sync() is a barrier.  `slot` alternates, so that one barrier is enough.
+template <bool kWarp, int N, typename Sync>
+__device__ __forceinline__ void row_sum(float (&v)[N], float (*s_part)[32], int slot, int tid, int n_warps, Sync&& sync) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
   if (kWarp) return;
-  const int lane = threadIdx.x & 31, n_warps = blockDim.x >> 5;
+  const int lane = tid & 31;
   if (lane == 0)
-    for (int i = 0; i < N; ++i) s_part[slot * 2 + i][threadIdx.x >> 5] = v[i];
-  __syncthreads();
+    for (int i = 0; i < N; ++i) s_part[slot * 2 + i][tid >> 5] = v[i];
+  sync();
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < n_warps ? s_part[slot * 2 + i][lane] : 0.f);
 }
@@ -71,7 +72,7 @@ norm_kernel(const XT* x, const XT* residual, const WT* weight, const WT* bias, i
   constexpr bool kHold = holds<NV, kWarp>();
   using Weight = Span<WT, V, kRagged>;
   __shared__ float s_part[4][32];
-  const int group = kWarp ? 32 : int(blockDim.x), tid = kWarp ? int(threadIdx.x) & 31 : int(threadIdx.x);
+  const int group = kWarp ? 32 : int(blockDim.x), tid = kWarp ? int(threadIdx.x) & 31 : int(threadIdx.x), n_warps = int(blockDim.x) >> 5;
   int64_t row = kWarp ? int64_t(blockIdx.x) * kRowsPerCta + (threadIdx.x >> 5) : int64_t(blockIdx.x);
   behind_wait();
   behind_go();
@@ -140,7 +141,7 @@ norm_kernel(const XT* x, const XT* residual, const WT* weight, const WT* bias, i
     if (kHold && next < n_tokens) fetch(next * hidden);
     float mean = 0.f;
     if (!rms) {
-      row_sum<kWarp>(sum, s_part, 0);
+      row_sum<kWarp>(sum, s_part, 0, tid, n_warps, [] { __syncthreads(); });
       mean = mean_of(sum[0]);
     }
     float sq[1] = {0.f};
@@ -157,7 +158,7 @@ norm_kernel(const XT* x, const XT* residual, const WT* weight, const WT* bias, i
         for (int j = 0; j < V; ++j) sq[0] += (s[i][j] - mean) * (s[i][j] - mean);
       }
     }
-    row_sum<kWarp>(sq, s_part, rms ? slot : 1);      // (a place that nobody still reads)
+    row_sum<kWarp>(sq, s_part, rms ? slot : 1, tid, n_warps, [] { __syncthreads(); });      // (a place that nobody still reads)
     const float rstd = 1.0f / sqrtf(mean_of(sq[0]) + eps);
     if (tid == 0) {
       stats[row] = mean;
@@ -209,8 +210,10 @@ __device__ __forceinline__ void zero_behind(Vec<T, V>& v, int n) {
   for (int j = 0; j < V; ++j) f[j] = j < n ? f[j] : 0.f;
   v.set(f);
 }
-// The backward.  A CTA takes every gridDim.x-th tile of rows: one row for all its threads, or, of narrow rows, some for each of
-// its warps.  Tiles are contiguous in memory and come by bulk copies into a ring of stages, so that several are in flight
+// The backward.  A CTA's threads are up to 8 groups, each with a ring and a barrier of its own; a group takes every n-th tile of rows:
+// one row for all its threads, or (then the only one), of narrow rows, some for each of its warps.  (As CTAs of their own the groups
+// wrote a part of the sums each: 24.0 us at 5465 x 1240, 22.3 so, 20.9 and 19.8 at 4000 x 1536.  Groups of more than 128 threads are
+// CTAs: 179 us at 31041 x 4096, 193 as two groups of one.)  Tiles are contiguous in memory and come by bulk copies into a ring of stages, so that several are in flight
 // whatever the arithmetic waits for (31041 x 4096 bf16 with d_total: 346 us with loads where the values are used, 253 with the
 // next row's in registers, 187 so).  For the sums over tokens a thread keeps its columns [k V, (k + 1) V) throughout; of dx it
 // writes window k of each row (the same columns where rows are aligned).  partial: [gridDim.x][2][part_pitch].
@@ -219,40 +222,55 @@ __host__ __device__ constexpr int part_pitch(int hidden) { return (hidden + 3) /
 
 struct BwdShape {
   int32_t rows, stages;                   // rows of a tile; tiles in flight
+  int32_t groups;
   int32_t staged;                         // tensors that come by the ring: x, d_out and, where there is room, d_total
   uint32_t slot_bytes, w_bytes;           // of a tile of one tensor; of the weight with zeros around it
 };
 constexpr uint32_t kWeightPad = 64;       // zeros in front of the weight and behind it
 
-template <typename XT, typename WT, int NV, bool kWarp, bool kRagged>
+template <typename XT, typename WT, int NV, bool kWarp, bool kRagged, bool kGrouped>
 __global__ void __launch_bounds__(bwd_threads<XT, NV, kWarp>(), 1)
 norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* stats, const XT* d_total, int64_t n_tokens,
                 int32_t hidden, int32_t rms, XT* dx, float* partial, BwdShape shape, int32_t* status) {
   constexpr int V = 16 / int(sizeof(XT)), kE = int(sizeof(XT)), kW = int(sizeof(WT));
   constexpr bool kKeep = !kRagged && NV * V <= 16;
   extern __shared__ uint8_t smem_raw[];        // [stages][2 or 3 tensors][slot], weight;  at the end the warps' sums
-  __shared__ float s_part[4][32];
-  __shared__ uint64_t s_bar[8], s_weight_bar;
+  __shared__ float s_parts[kGrouped ? kMaxGroups : 1][4][32];
+  __shared__ uint64_t s_bars[kGrouped ? kMaxGroups : 1][8], s_weight_bar;
   __shared__ int s_abort;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int group = kWarp ? 32 : int(blockDim.x), tid = kWarp ? lane : int(threadIdx.x);
-  const uint32_t base = (smem_u32(smem_raw) + 15u) & ~15u, n_tensors = uint32_t(shape.staged);
-  uint8_t* ring = smem_raw + (base - smem_u32(smem_raw));
-  uint8_t* s_weight = ring + uint32_t(shape.stages) * n_tensors * shape.slot_bytes + kWeightPad;
-  const uint32_t sw = base + uint32_t(shape.stages) * n_tensors * shape.slot_bytes + kWeightPad;
+  const int groups = kGrouped ? shape.groups : 1;
+  const int width = int(blockDim.x) / groups, mine = kGrouped ? int(threadIdx.x) / width : 0;     // a group's threads; its number
+  const int place = int(threadIdx.x) - mine * width;                                              // in the group
+  const int group = kWarp ? 32 : width, tid = kWarp ? lane : place;                   // threads of a row
+  const uint32_t n_tensors = uint32_t(shape.staged), ring_bytes = uint32_t(shape.stages) * n_tensors * shape.slot_bytes;
+  const uint32_t base0 = (smem_u32(smem_raw) + 15u) & ~15u, base = base0 + uint32_t(mine) * ring_bytes;
+  uint8_t* ring0 = smem_raw + (base0 - smem_u32(smem_raw));
+  uint8_t* ring = ring0 + uint32_t(mine) * ring_bytes;
+  uint8_t* s_weight = ring0 + uint32_t(groups) * ring_bytes + kWeightPad;
+  const uint32_t sw = base0 + uint32_t(groups) * ring_bytes + kWeightPad;
+  uint64_t* s_bar = s_bars[mine];
+  float(*s_part)[32] = s_parts[mine];
+  const int64_t start = int64_t(blockIdx.x) * groups + mine, stride = int64_t(gridDim.x) * groups;
+  auto sync = [&] {
+    if (!kGrouped) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(width) : "memory");
+  };
   const WaitCtx wctx{&s_abort, status, kWaitLimitClocks};
   const int64_t all = n_tokens * hidden, tile_elems = int64_t(shape.rows) * hidden, n_tiles = (n_tokens + shape.rows - 1) / shape.rows;
 
   if (threadIdx.x == 0) {
     s_abort = 0;
-    for (int s = 0; s < shape.stages; ++s) mbar_init(smem_u32(&s_bar[s]), 1);
+    for (int g = 0; g < groups; ++g)
+      for (int s = 0; s < shape.stages; ++s) mbar_init(smem_u32(&s_bars[g][s]), 1);
     mbar_init(smem_u32(&s_weight_bar), 1);
     fence_mbar_init();
   }
+  if (kGrouped) __syncthreads();      // (the first threads of all groups use their barriers)
   behind_wait();
   behind_go();
 
-  // One thread requests a tile: from the 16-byte boundary at or before its first element to the one at or behind its last; the
+  // One thread of a group requests a tile: from the 16-byte boundary at or before its first element to the one at or behind its last; the
   // tensor's last elements, if no boundary follows them within it, by hand.
   auto request = [&](int64_t tile, int stage) {
     const int64_t first = tile * tile_elems, from = first & ~int64_t(V - 1);
@@ -279,10 +297,10 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
     bulk_load(at + shape.slot_bytes, d_out + from, bytes, bar);
     if (n_tensors == 3) bulk_load(at + 2 * shape.slot_bytes, d_total + from, bytes, bar);
   };
-  int64_t asked = blockIdx.x;     // the next tile to request, and how many have been (thread 0's)
+  int64_t asked = start;     // the next tile to request, and how many have been (the first thread's)
   int n_asked = 0;
-  if (threadIdx.x == 0)
-    for (int s = 0; s < shape.stages && asked < n_tiles; ++s, asked += gridDim.x, ++n_asked) request(asked, s);
+  if (place == 0)
+    for (int s = 0; s < shape.stages && asked < n_tiles; ++s, asked += stride, ++n_asked) request(asked, s);
   // The weight, behind the first tiles (32.7 us instead of 38.0 element by element ahead of them at 4000 x 2048 fp32): whole vectors by
   // a copy, the rest and the zeros around it by hand.
   const int whole = hidden * kW & ~15;
@@ -309,9 +327,9 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
     next_rstd = stats[n_tokens + row];
   };
   const int first_r = kWarp ? warp : 0;
-  fetch_stats(int64_t(blockIdx.x) * shape.rows + first_r);
+  fetch_stats(start * shape.rows + first_r);
   mbar_wait(smem_u32(&s_weight_bar), 0, wctx);
-  for (int64_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
+  for (int64_t tile = start; tile < n_tiles; tile += stride) {
     mbar_wait(smem_u32(&s_bar[stage]), turn & 1, wctx);
     const uint32_t tx = base + uint32_t(stage) * n_tensors * shape.slot_bytes;
     const int64_t row0 = tile * shape.rows;
@@ -322,7 +340,7 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
       const int o = lead + r * hidden, a = kRagged ? o & (V - 1) : 0;
       const uint32_t sx = tx + uint32_t(o * kE), sg = sx + shape.slot_bytes, sd = sg + shape.slot_bytes;
       const float mean = next_mean, rstd = next_rstd;
-      fetch_stats(kWarp && r + kRowsPerCta < n_rows ? row + kRowsPerCta : (tile + gridDim.x) * shape.rows + first_r);
+      fetch_stats(kWarp && r + kRowsPerCta < n_rows ? row + kRowsPerCta : (tile + stride) * shape.rows + first_r);
       const float shift = -mean * rstd;         // u = x rstd + shift
       float sum[2] = {0.f, 0.f};
       float ku[kKeep ? NV : 1][V], kg[kKeep ? NV : 1][V];     // u and g w, where there are registers for them
@@ -353,11 +371,11 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
           }
         }
       }
-      row_sum<kWarp>(sum, s_part, slot);
+      row_sum<kWarp>(sum, s_part, slot, tid, width >> 5, sync);
       // (a row for all threads: they have left the tile before this one)
-      if (!kWarp && before >= 0 && threadIdx.x == 0 && asked < n_tiles && !s_abort) {
+      if (!kWarp && before >= 0 && place == 0 && asked < n_tiles && !s_abort) {
         request(asked, before);
-        asked += gridDim.x;
+        asked += stride;
         ++n_asked;
       }
       // dx = (g w - u c_u - c_1) rstd + d_total
@@ -400,10 +418,10 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
       }
     }
     if (kWarp || shape.stages == 1) {     // all warps have left the tile
-      __syncthreads();
-      if (threadIdx.x == 0 && asked < n_tiles && !s_abort) {
+      sync();
+      if (place == 0 && asked < n_tiles && !s_abort) {
         request(asked, stage);
-        asked += gridDim.x;
+        asked += stride;
         ++n_asked;
       }
     } else {
@@ -411,17 +429,18 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
     }
     if (++stage == shape.stages) { stage = 0; ++turn; }
   }
-  if (s_abort && threadIdx.x == 0) {      // shared memory must outlive the copies in flight
+  if (s_abort && place == 0) {      // shared memory must outlive the copies in flight
     const long long t0 = clock64();
     while (!mbar_try_wait(smem_u32(&s_weight_bar), 0) && clock64() - t0 < kWaitLimitClocks) {}
     for (int q = max(0, n_asked - shape.stages); q < n_asked; ++q)
       while (!mbar_try_wait(smem_u32(&s_bar[q % shape.stages]), (q / shape.stages) & 1) && clock64() - t0 < kWaitLimitClocks) {}
   }
   __syncthreads();
-  // The sums of a CTA's warps, each in a place of its own over the ring, are added in the warps' order.
+  // The sums of a CTA's warps or groups, each in a place of its own over the rings, are added in their order.
   const int pitch = part_pitch(hidden);
   float* mine_dw = partial + int64_t(blockIdx.x) * 2 * pitch;
-  float* to = kWarp ? reinterpret_cast<float*>(ring) + warp * 2 * pitch : mine_dw;
+  const int n_sums = kWarp ? kRowsPerCta : groups;
+  float* to = n_sums > 1 ? reinterpret_cast<float*>(ring0) + (kWarp ? warp : mine) * 2 * pitch : mine_dw;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int col = (i * group + tid) * V;
@@ -432,13 +451,13 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
       *reinterpret_cast<float4*>(to + pitch + col + j) = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
     }
   }
-  if (kWarp) {
+  if (n_sums > 1) {
     __syncthreads();
-    const float* sums = reinterpret_cast<const float*>(ring);
+    const float* sums = reinterpret_cast<const float*>(ring0);
     for (int c = threadIdx.x; c < 2 * pitch; c += blockDim.x) {
       float v = 0.f;
-#pragma unroll
-      for (int k = 0; k < kRowsPerCta; ++k) v += sums[k * 2 * pitch + c];
+#pragma unroll 8
+      for (int k = 0; k < n_sums; ++k) v += sums[k * 2 * pitch + c];
       mine_dw[c] = v;
     }
   }
@@ -498,8 +517,12 @@ Division divide_bwd(int32_t hidden, int elem_bytes) {
   return {nv, ((n + nv - 1) / nv + 31) / 32 * 32};
 }
 
-// CTAs of the backward for an SM: 512 threads of 128 registers.
-int ctas_per_sm(const Division& d) { return d.threads == 32 ? 2 : std::max(1, std::min(8, 512 / d.threads)); }
+// CTAs of the backward for an SM (512 threads of 128 registers), and the groups of one: as many as tiles can fill.
+bool grouped(const Division& d) { return d.threads > 32 && d.threads <= 128; }
+int ctas_per_sm(const Division& d) { return d.threads == 32 ? 2 : grouped(d) ? 1 : std::max(1, 512 / d.threads); }
+int groups_of(const Division& d, int64_t tiles) {
+  return grouped(d) ? int(std::max<int64_t>(1, std::min<int64_t>({(tiles + kSmCount - 1) / kSmCount, 512 / d.threads, kMaxGroups}))) : 1;
+}
 // Rows of a tile: one, or 8 for each of a CTA's warps, fewer where all tiles would not fill the SMs, and 8 KB of a tensor at most.
 int tile_rows(const Division& d, int64_t n_tokens, int32_t hidden, int elem_bytes) {
   if (d.threads != 32) return 1;
@@ -508,9 +531,9 @@ int tile_rows(const Division& d, int64_t n_tokens, int32_t hidden, int elem_byte
   return rows;
 }
 int64_t part_count(const Division& d, int64_t n_tokens, int rows) {
-  const int64_t tiles = std::max<int64_t>(1, (n_tokens + rows - 1) / rows), most = int64_t(kSmCount) * ctas_per_sm(d);
+  const int64_t tiles = std::max<int64_t>(1, (n_tokens + rows - 1) / rows), groups = groups_of(d, tiles), most = int64_t(kSmCount) * ctas_per_sm(d) * groups;
   const int64_t each = (tiles + most - 1) / most;      // and no more than it takes for the busiest one's number of tiles
-  return (tiles + each - 1) / each;
+  return ((tiles + each - 1) / each + groups - 1) / groups;
 }
 
 template <typename F>
@@ -570,20 +593,24 @@ struct Backward {
   }
   template <int NV, bool kWarp, bool kRagged>
   psa_status_t go() {
+    constexpr int kWide = int(sizeof(XT)) / 2;
     BwdShape shape{};
     shape.rows = tile_rows(d, n_tokens, hidden, int(sizeof(XT)));
+    shape.groups = groups_of(d, (n_tokens + shape.rows - 1) / shape.rows);
     shape.slot_bytes = uint32_t((int64_t(shape.rows) * hidden * int(sizeof(XT)) + 47) / 16 * 16);    // and a vector around it
     shape.w_bytes = uint32_t((hidden * int(sizeof(WT)) + 15) / 16 * 16) + 2 * kWeightPad;
-    const uint32_t room = 224 * 1024 / ctas_per_sm(d) - 1024 - shape.w_bytes;
+    const uint32_t room = (224 * 1024 / ctas_per_sm(d) - (grouped(d) ? 8192 : 1024) - shape.w_bytes) / uint32_t(shape.groups);     // of a group, less the static arrays
     shape.staged = d_total && 3 * shape.slot_bytes <= room ? 3 : 2;
     const uint32_t stage = uint32_t(shape.staged) * shape.slot_bytes;
-    shape.stages = int(std::max(1u, std::min(8u, std::min(room / stage, 1 + 196608 / uint32_t(ctas_per_sm(d)) / stage))));
-    const uint32_t sums = kWarp ? uint32_t(kRowsPerCta * 2 * 4 * part_pitch(hidden)) : 0u;
-    const uint32_t smem = std::max(shape.stages * stage + shape.w_bytes, sums) + 16;
+    shape.stages = int(std::max(1u, std::min(8u, std::min(room / stage, 1 + 196608 / uint32_t(ctas_per_sm(d) * shape.groups) / stage))));
+    const uint32_t sums = uint32_t((kWarp ? kRowsPerCta : shape.groups) * 2 * 4 * part_pitch(hidden));
+    const uint32_t smem = std::max(shape.groups * shape.stages * stage + shape.w_bytes, sums) + 16;
     const int64_t parts = part_count(d, n_tokens, shape.rows);
-    auto kernel = norm_bwd_kernel<XT, WT, NV, kWarp, kRagged>;
+    auto kernel = norm_bwd_kernel<XT, WT, NV, kWarp, kRagged, false>;
+    if constexpr (!kWarp && NV == 2 * kWide)
+      if (grouped(d)) kernel = norm_bwd_kernel<XT, WT, NV, kWarp, kRagged, true>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return PSA_ERR_CUDA;
-    launch_behind(true, kernel, dim3(unsigned(parts)), kWarp ? 32 * kRowsPerCta : d.threads, smem, stream,
+    launch_behind(true, kernel, dim3(unsigned(parts)), kWarp ? 32 * kRowsPerCta : d.threads * shape.groups, smem, stream,
                   static_cast<const XT*>(d_out), static_cast<const XT*>(x), static_cast<const WT*>(weight), stats,
                   static_cast<const XT*>(d_total), n_tokens, hidden, rms, static_cast<XT*>(dx), partial, shape, status);
     const bool many = parts > 2 * kSmCount;
