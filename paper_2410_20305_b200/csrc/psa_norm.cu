@@ -212,10 +212,10 @@ __device__ __forceinline__ void zero_behind(Vec<T, V>& v, int n) {
 }
 // The backward.  A CTA's threads are up to 8 groups, each with a ring and a barrier of its own; a group takes every n-th tile of rows:
 // one row for all its threads, or (then the only one), of narrow rows, some for each of its warps.  (As CTAs of their own the groups
-// wrote a part of the sums each: 24.0 us at 5465 x 1240, 22.3 so, 20.9 and 19.8 at 4000 x 1536.  Groups of more than 128 threads are
-// CTAs: 179 us at 31041 x 4096, 193 as two groups of one.)  Tiles are contiguous in memory and come by bulk copies into a ring of stages, so that several are in flight
-// whatever the arithmetic waits for (31041 x 4096 bf16 with d_total: 346 us with loads where the values are used, 253 with the
-// next row's in registers, 187 so).  For the sums over tokens a thread keeps its columns [k V, (k + 1) V) throughout; of dx it
+// wrote a part of the sums each: 24.0 us at 5465 x 1240, 22.3 so, 20.9 and 19.8 at 4000 x 1536.  Two groups of
+// more threads are two CTAs: 179 us at 31041 x 4096, 193 as one.)  Tiles are contiguous in memory and come by bulk copies into a ring
+// of stages, so that several are in flight whatever the arithmetic waits for (31041 x 4096 bf16 with d_total: 346 us with loads where
+// the values are used, 253 with the next row's in registers, 187 so at first).  For the sums over tokens a thread keeps its columns [k V, (k + 1) V) throughout; of dx it
 // writes window k of each row (the same columns where rows are aligned).  partial: [gridDim.x][2][part_pitch].
 // A part's rows of sums start at 16 bytes.
 __host__ __device__ constexpr int part_pitch(int hidden) { return (hidden + 3) / 4 * 4; }
@@ -464,12 +464,12 @@ norm_bwd_kernel(const XT* d_out, const XT* x, const WT* weight, const float* sta
 }
 
 // dw (blockIdx.y = 0) and db (1): the parts of all CTAs, added in a fixed order.
-// 16 warps for the parts of up to two CTAs an SM, 32 for more (592 parts at 5465 x 1237: 33.3 us for the whole backward with 16,
-// 28.8 with 32; 148 at 4000 x 8192: 57.5 and 59.8).
-template <typename WT, int kWarps>
-__global__ void __launch_bounds__(32 * kWarps)
+// (32 warps are faster from 400 parts on, of which there are none: two CTAs of the backward an SM at most.)
+constexpr int kSumWarps = 16;
+template <typename WT>
+__global__ void __launch_bounds__(32 * kSumWarps)
 norm_sum_kernel(const float* partial, int32_t n_parts, int32_t hidden, WT* dweight, WT* dbias) {
-  __shared__ float s[kWarps][33];
+  __shared__ float s[kSumWarps][33];
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
   behind_wait();
   behind_go();
@@ -477,19 +477,19 @@ norm_sum_kernel(const float* partial, int32_t n_parts, int32_t hidden, WT* dweig
   float v = 0.f;
   if (col < hidden) {
     int p = part;
-    for (; p + 7 * kWarps < n_parts; p += 8 * kWarps) {
+    for (; p + 7 * kSumWarps < n_parts; p += 8 * kSumWarps) {
       float w[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w[k] = partial[(int64_t(p + k * kWarps) * 2 + blockIdx.y) * pitch + col];
+      for (int k = 0; k < 8; ++k) w[k] = partial[(int64_t(p + k * kSumWarps) * 2 + blockIdx.y) * pitch + col];
 #pragma unroll
       for (int k = 0; k < 8; ++k) v += w[k];
     }
-    for (; p < n_parts; p += kWarps) v += partial[(int64_t(p) * 2 + blockIdx.y) * pitch + col];
+    for (; p < n_parts; p += kSumWarps) v += partial[(int64_t(p) * 2 + blockIdx.y) * pitch + col];
   }
   s[part][lane] = v;
   __syncthreads();
   if (part == 0 && col < hidden) {
-    for (int p = 1; p < kWarps; ++p) v += s[p][lane];
+    for (int p = 1; p < kSumWarps; ++p) v += s[p][lane];
     set_element((blockIdx.y ? dbias : dweight) + col, v);
   }
 }
@@ -518,7 +518,7 @@ Division divide_bwd(int32_t hidden, int elem_bytes) {
 }
 
 // CTAs of the backward for an SM (512 threads of 128 registers), and the groups of one: as many as tiles can fill.
-bool grouped(const Division& d) { return d.threads > 32 && d.threads <= 128; }
+bool grouped(const Division& d) { return d.threads > 32 && d.threads <= 160; }
 int ctas_per_sm(const Division& d) { return d.threads == 32 ? 2 : grouped(d) ? 1 : std::max(1, 512 / d.threads); }
 int groups_of(const Division& d, int64_t tiles) {
   return grouped(d) ? int(std::max<int64_t>(1, std::min<int64_t>({(tiles + kSmCount - 1) / kSmCount, 512 / d.threads, kMaxGroups}))) : 1;
@@ -613,8 +613,7 @@ struct Backward {
     launch_behind(true, kernel, dim3(unsigned(parts)), kWarp ? 32 * kRowsPerCta : d.threads * shape.groups, smem, stream,
                   static_cast<const XT*>(d_out), static_cast<const XT*>(x), static_cast<const WT*>(weight), stats,
                   static_cast<const XT*>(d_total), n_tokens, hidden, rms, static_cast<XT*>(dx), partial, shape, status);
-    const bool many = parts > 2 * kSmCount;
-    launch_behind(true, many ? norm_sum_kernel<WT, 32> : norm_sum_kernel<WT, 16>, dim3(unsigned((hidden + 31) / 32), dbias ? 2 : 1), many ? 1024 : 512, 0, stream, partial,
+    launch_behind(true, norm_sum_kernel<WT>, dim3(unsigned((hidden + 31) / 32), dbias ? 2 : 1), 32 * kSumWarps, 0, stream, partial,
                   int32_t(parts), hidden, static_cast<WT*>(dweight), static_cast<WT*>(dbias));
     return check_last_cuda_error("psa_norm_bwd launch");
   }
