@@ -571,7 +571,7 @@ psa_status_t psa_embed_bwd(const void* d_out, const int32_t* token_ids, int32_t 
  *   hidden, ffn  multiples of 8, at most 2^20
  *   out          device bf16 [n_tokens, hidden] (out)
  *   gate, up     device bf16 [n_tokens, ffn] (out): G and U for psa_ffn_bwd; both NULL where there is no backward
- *   workspace    device scratch of psa_ffn_workspace_bytes(.., backward = 0) bytes, 256-byte aligned
+ *   workspace    device scratch of psa_ffn_workspace_bytes(.., backward = 0) bytes, 16-byte aligned
  *   device_status  device int32 or NULL; PSA_DEVSTAT_WAIT_EXPIRED is ORed in as by psa_fwd
  * Outputs must not overlap inputs or one another.  n_tokens = 0 is a no-op.
  * Errors: INVALID_ARG, UNSUPPORTED (sizes), ALIGNMENT (16 bytes), CUDA.
@@ -588,7 +588,7 @@ psa_status_t psa_ffn(const void* x, const void* w_gate, const void* w_up, const 
  * with fp32 sums; dG, dU and H (formed again from G and U) are rounded to bf16 between the products.
  *   d_out        device bf16 [n_tokens, hidden]      gate, up  as written by psa_ffn
  *   dx, dw_gate, dw_up, dw_down   device bf16 (out), shaped as x and the weights
- *   workspace    device scratch of psa_ffn_workspace_bytes(.., backward = 1) bytes, 256-byte aligned
+ *   workspace    device scratch of psa_ffn_workspace_bytes(.., backward = 1) bytes, 16-byte aligned
  * No atomics: the same inputs give the same bits.  n_tokens = 0 writes zeros to the weights' gradients.
  * Errors and the rest: as psa_ffn.
  */
