@@ -609,7 +609,10 @@ struct Backward {
     auto kernel = norm_bwd_kernel<XT, WT, NV, kWarp, kRagged, false>;
     if constexpr (!kWarp && NV == 2 * kWide)
       if (grouped(d)) kernel = norm_bwd_kernel<XT, WT, NV, kWarp, kRagged, true>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return PSA_ERR_CUDA;
+    // (The limit is the kernel's, for all host threads: the same in every call, or a call could lower it under another one's launch.)
+    const int limit = 227 * 1024 - (grouped(d) ? 8192 : 1024);      // of an SM's 228 KB, less the CTA's own and the static arrays
+    if (smem > uint32_t(limit)) return PSA_ERR_UNSUPPORTED;         // (no shape asks for more)
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, limit) != cudaSuccess) return PSA_ERR_CUDA;
     launch_behind(true, kernel, dim3(unsigned(parts)), kWarp ? 32 * kRowsPerCta : d.threads * shape.groups, smem, stream,
                   static_cast<const XT*>(d_out), static_cast<const XT*>(x), static_cast<const WT*>(weight), stats,
                   static_cast<const XT*>(d_total), n_tokens, hidden, rms, static_cast<XT*>(dx), partial, shape, status);

@@ -1,0 +1,74 @@
+"""What the decoder's operators ask of the CUDA runtime, checked without a GPU: their host code, compiled against stand-ins
+for the two calls that launch a kernel and set its limit of shared memory, which write down what they are given."""
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2410_20305_b200", "csrc")
+
+STANDINS = r"""
+#include <cuda_runtime.h>
+#include <cstdio>
+#include <map>
+#include <set>
+std::map<const void*, std::set<int>> limits;      // of a kernel: what its limit of shared memory was set to
+std::map<const void*, size_t> most;               // the most that a launch asked for
+int launches = 0, fails_from = 1 << 30;           // launches so far; the first one that is refused
+extern "C" cudaError_t recorded_limit(const void* kernel, cudaFuncAttribute, int bytes) {
+  limits[kernel].insert(bytes);
+  return cudaSuccess;
+}
+extern "C" cudaError_t recorded_launch(const cudaLaunchConfig_t* config, const void* kernel, void**) {
+  if (config->dynamicSmemBytes > most[kernel]) most[kernel] = config->dynamicSmemBytes;
+  return ++launches >= fails_from ? cudaErrorLaunchOutOfResources : cudaSuccess;
+}
+#include "%s"
+namespace psa {
+psa_status_t check_last_cuda_error(const char*) { return launches >= fails_from ? PSA_ERR_CUDA : PSA_OK; }
+}  // namespace psa
+void* const P = reinterpret_cast<void*>(4096);
+#define FLOATS reinterpret_cast<float*>(4096)
+#define INTS reinterpret_cast<int*>(4096)
+int main() {
+%s
+  return 0;
+}
+"""
+
+
+def run(tmp_path, source, body):
+    """The output of a program that has `source`'s host code with the stand-ins, and `body` as its main function."""
+    (tmp_path / "host.cu").write_text(STANDINS % (source, body))
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    # (no machine code for the kernels: nothing here runs them)
+    done = subprocess.run([nvcc, "-std=c++17", "-gencode", "arch=compute_100a,code=compute_100a", "-DcudaLaunchKernelExC=recorded_launch",
+                           "-DcudaFuncSetAttribute=recorded_limit", "-I", CSRC, "-I", os.path.join(ROOT, "include"), "-o",
+                           str(tmp_path / "host"), str(tmp_path / "host.cu")], capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr
+    done = subprocess.run([str(tmp_path / "host")], capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr
+    return done.stdout
+
+
+def test_a_kernels_limit_of_shared_memory_does_not_depend_on_the_call(tmp_path):
+    """The limit belongs to the kernel, not to the call, and host threads share it: one that lowered it between another
+    one's setting and launch would have that launch refused."""
+    out = run(tmp_path, "psa_norm.cu", r"""
+  for (int hidden = 1; hidden <= 16384; ++hidden)
+    for (long long tokens : {1LL, 300LL, 5000LL, 200000LL})
+      for (int types = 0; types < 3; ++types)
+        for (void* d_total : {(void*)nullptr, P}) {
+          const int x = types == 2 ? PSA_DTYPE_F32 : PSA_DTYPE_BF16, w = types == 0 ? PSA_DTYPE_BF16 : PSA_DTYPE_F32;
+          if (psa_norm_bwd(P, P, P, FLOATS, d_total, x, w, tokens, hidden, 0, P, P, P, P, nullptr, nullptr) != PSA_OK) return 1;
+        }
+  for (auto& l : limits) {
+    printf("%zu %zu", l.second.size(), most[l.first]);
+    for (int bytes : l.second) printf(" %d", bytes);
+    printf("\n");
+  }""")
+    kernels = [[int(v) for v in line.split()] for line in out.splitlines()]
+    assert len(kernels) >= 12
+    for n, most, *values in kernels:
+        assert n == 1 and most <= values[0] <= 227 * 1024, (n, most, values[:5])
