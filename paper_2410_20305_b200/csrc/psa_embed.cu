@@ -372,18 +372,22 @@ psa_status_t embed_bwd(const void* d_out, const int32_t* ids, int64_t n_tokens, 
   const int bins = int((vocab + ctas - 1) / ctas);
   if (cudaFuncSetAttribute(embed_index_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 32 * kMaxBins * 4) != cudaSuccess)
     return PSA_ERR_CUDA;
-  launch_behind(true, embed_index_kernel, dim3(unsigned(ctas)), kIndexThreads, size_t(32) * bins * 4, stream, ids,
-                int32_t(n_tokens), int32_t(vocab), bins, ints(w.start), ints(w.count), ints(w.order), ints(w.sorted_id), status);
+  // (The sums take token numbers and ids from the index, so nothing is launched behind a refused launch.)
+  if (launch_behind(true, embed_index_kernel, dim3(unsigned(ctas)), kIndexThreads, size_t(32) * bins * 4, stream, ids,
+                    int32_t(n_tokens), int32_t(vocab), bins, ints(w.start), ints(w.count), ints(w.order), ints(w.sorted_id),
+                    status) != cudaSuccess)
+    return failed_launch("psa_embed_bwd launch");
   const int run = run_length(n_tokens, hidden), n_runs = int((n_tokens + run - 1) / run);
   const int windows = windows_of(hidden, V, 16 / int(sizeof(GT)));
   const unsigned slices = unsigned((windows + kThreads - 1) / kThreads);
   const unsigned threads = unsigned((windows + int(slices) * 32 - 1) / (int(slices) * 32)) * 32;     // even slices of whole warps
   const unsigned zero = accumulate ? 0u : unsigned((vocab + kZeroRows - 1) / kZeroRows);
   float* partial = reinterpret_cast<float*>(ws + w.partial);
-  if (n_runs + zero > 0)
-    launch_behind(true, embed_sum_kernel<XT, GT, kRagged>, dim3(unsigned(n_runs) + zero, slices), threads, 0, stream,
-                  static_cast<const XT*>(d_out), ints(w.start), ints(w.count), ints(w.order), ints(w.sorted_id), run, n_runs, n_tokens, int32_t(vocab),
-                  hidden, windows, scale, accumulate, static_cast<GT*>(dtable), partial);
+  if (n_runs + zero > 0 &&
+      launch_behind(true, embed_sum_kernel<XT, GT, kRagged>, dim3(unsigned(n_runs) + zero, slices), threads, 0, stream,
+                    static_cast<const XT*>(d_out), ints(w.start), ints(w.count), ints(w.order), ints(w.sorted_id), run, n_runs, n_tokens, int32_t(vocab),
+                    hidden, windows, scale, accumulate, static_cast<GT*>(dtable), partial) != cudaSuccess)
+    return failed_launch("psa_embed_bwd launch");
   if (n_runs > 1)
     launch_behind(true, embed_join_kernel<GT, V, kRagged>, dim3(unsigned(n_runs), unsigned((windows + 31) / 32)), 32 * kJoinWarps, 0, stream, ints(w.start),
                   ints(w.count), ints(w.sorted_id), run, int32_t(vocab), hidden, windows, scale, accumulate, partial, static_cast<GT*>(dtable));

@@ -102,6 +102,11 @@ bool plan_on_current_device(const psa_plan_t* plan);
 // Returns PSA_OK if no CUDA error is pending, else PSA_ERR_CUDA; with PSA_DEBUG set in the
 // environment the CUDA error string is written to stderr.
 psa_status_t check_last_cuda_error(const char* where);
+// After a launch that was refused: the error is reported as above, and a call's further launches are left out.
+inline psa_status_t failed_launch(const char* where) {
+  check_last_cuda_error(where);
+  return PSA_ERR_CUDA;
+}
 
 // Optional event pairs recorded around one kernel (see psa_profile_events).
 struct ProfileEvents { void* start; void* stop; };

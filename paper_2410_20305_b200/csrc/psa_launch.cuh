@@ -19,9 +19,10 @@ namespace psa {
 __device__ __forceinline__ void behind_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void behind_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// Returns the launch's error, so that a caller whose next kernel takes addresses from this one's results can leave it out.
 template <typename... Params, typename... Args>
-void launch_behind(bool behind, void (*kernel)(Params...), dim3 grid, unsigned block, size_t smem, cudaStream_t stream,
-                   Args&&... args) {
+cudaError_t launch_behind(bool behind, void (*kernel)(Params...), dim3 grid, unsigned block, size_t smem, cudaStream_t stream,
+                          Args&&... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(block);
@@ -32,7 +33,7 @@ void launch_behind(bool behind, void (*kernel)(Params...), dim3 grid, unsigned b
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = behind ? 1 : 0;
-  cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);   // (converts as a launch with <<<>>> does)
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);   // (converts as a launch with <<<>>> does)
 }
 
 }  // namespace psa

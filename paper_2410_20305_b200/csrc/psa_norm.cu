@@ -613,9 +613,11 @@ struct Backward {
     const int limit = 227 * 1024 - (grouped(d) ? 8192 : 1024);      // of an SM's 228 KB, less the CTA's own and the static arrays
     if (smem > uint32_t(limit)) return PSA_ERR_UNSUPPORTED;         // (no shape asks for more)
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, limit) != cudaSuccess) return PSA_ERR_CUDA;
-    launch_behind(true, kernel, dim3(unsigned(parts)), kWarp ? 32 * kRowsPerCta : d.threads * shape.groups, smem, stream,
-                  static_cast<const XT*>(d_out), static_cast<const XT*>(x), static_cast<const WT*>(weight), stats,
-                  static_cast<const XT*>(d_total), n_tokens, hidden, rms, static_cast<XT*>(dx), partial, shape, status);
+    if (launch_behind(true, kernel, dim3(unsigned(parts)), kWarp ? 32 * kRowsPerCta : d.threads * shape.groups, smem, stream,
+                      static_cast<const XT*>(d_out), static_cast<const XT*>(x), static_cast<const WT*>(weight), stats,
+                      static_cast<const XT*>(d_total), n_tokens, hidden, rms, static_cast<XT*>(dx), partial, shape,
+                      status) != cudaSuccess)
+      return failed_launch("psa_norm_bwd launch");      // (no sums of parts that are not written)
     launch_behind(true, norm_sum_kernel<WT>, dim3(unsigned((hidden + 31) / 32), dbias ? 2 : 1), 32 * kSumWarps, 0, stream, partial,
                   int32_t(parts), hidden, static_cast<WT*>(dweight), static_cast<WT*>(dbias));
     return check_last_cuda_error("psa_norm_bwd launch");

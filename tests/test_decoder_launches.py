@@ -72,3 +72,18 @@ def test_a_kernels_limit_of_shared_memory_does_not_depend_on_the_call(tmp_path):
     assert len(kernels) >= 12
     for n, most, *values in kernels:
         assert n == 1 and most <= values[0] <= 227 * 1024, (n, most, values[:5])
+
+
+@pytest.mark.parametrize("source,call,n", [
+    ("psa_embed.cu", "psa_embed_bwd(P, INTS, PSA_DTYPE_BF16, PSA_DTYPE_BF16, 1000, 500, 72, 1.0f, 0, P, P, nullptr, nullptr)", 3),
+    ("psa_norm.cu", "psa_norm_bwd(P, P, P, FLOATS, P, PSA_DTYPE_BF16, PSA_DTYPE_BF16, 1000, 72, 0, P, P, P, P, nullptr, nullptr)", 2)])
+def test_nothing_is_launched_behind_a_refused_launch(tmp_path, source, call, n):
+    """The sums of the embedding's gradient take token numbers and ids as addresses from what the launch before them wrote."""
+    out = run(tmp_path, source, r"""
+  for (int first = 1; first <= %d; ++first) {
+    launches = 0;
+    fails_from = first;
+    const int rc = %s;
+    printf("%%d %%d\n", rc == PSA_ERR_CUDA, launches);
+  }""" % (n + 1, call))
+    assert out.split("\n")[:-1] == ["1 %d" % k for k in range(1, n + 1)] + ["0 %d" % n]
