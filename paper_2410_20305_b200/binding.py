@@ -12,6 +12,10 @@ dpo_logp without stream=, out= and scratch=, dpo_logp_bwd without stream= and
 with dlogits=, psa_rope without stream= and with out=, the normalisation, the
 embedding and the feed-forward block without stream= and outputs of their own.
 Results and refusals are the same.
+
+A call with stream= runs on that stream, and what it allocates belongs to it;
+results are also kept for the stream that is current at the call.  Ordering
+their use behind the call is the caller's.
 """
 from __future__ import annotations
 
@@ -190,18 +194,41 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _call_stream(device, stream):
+    """The torch stream for the handle of a call, None where it is the current one."""
+    import torch
+    if stream is None or int(stream) == _stream(None):
+        return None
+    # handles 0 and 1 both name the default stream
+    return torch.cuda.default_stream(device) if int(stream) in (0, 1) else torch.cuda.ExternalStream(int(stream), device=device)
+
+
 def _temporary(n, dtype, device, stream):
     """A device buffer that the library uses on `stream` and that the caller drops on return.  torch gives a freed
     block to the next tensor of the stream that the block was allocated on, so it is allocated on the stream of the
     call: whoever owns it before or after has its work ordered against the call's.  (A graph captured by other means
     than torch's has no pool that keeps such a block: there the caller passes the buffer.)"""
     import torch
-    if stream is None or int(stream) == _stream(None):
+    own = _call_stream(device, stream)
+    if own is None:
         return torch.empty(n, dtype=dtype, device=device)
-    # handles 0 and 1 both name the default stream
-    own = torch.cuda.default_stream(device) if int(stream) in (0, 1) else torch.cuda.ExternalStream(int(stream), device=device)
     with torch.cuda.stream(own):
         return torch.empty(n, dtype=dtype, device=device)
+
+
+def _result(like, stream, make=None):
+    """A result that the caller left to the call: make(), or a tensor as `like`.  It is allocated on the stream of the call, as
+    _temporary is: from the current stream's blocks it could get one that the current stream's work still uses.  Where that
+    is another stream than the current one, which the caller goes on with, torch keeps the block from the next tensor until
+    the current stream has done what it had to do when the result was dropped."""
+    import torch
+    own = _call_stream(like.device, stream) if stream is not None and like.is_cuda else None
+    if own is None:
+        return torch.empty_like(like) if make is None else make()
+    with torch.cuda.stream(own):
+        t = torch.empty_like(like) if make is None else make()
+    t.record_stream(torch.cuda.current_stream(t.device))
+    return t
 
 
 def _want(t, name, shape, dtype, cuda=True, placement=True):
@@ -348,9 +375,9 @@ def psa_fwd(plan: Plan, q, k, v, o=None, lse=None, status=None, stream=None):
     import torch
     T = plan.total_tokens
     if o is None:
-        o = torch.empty_like(q)
+        o = _result(q, stream)
     if lse is None:
-        lse = torch.empty((plan.n_q_heads, T), dtype=torch.float32, device=q.device)
+        lse = _result(q, stream, lambda: torch.empty((plan.n_q_heads, T), dtype=torch.float32, device=q.device))
     fast = _fast(stream)
     if fast:
         code = fast.fwd(plan._key, q, k, v, o, lse, status)
@@ -368,11 +395,11 @@ def psa_bwd(plan: Plan, d_o, q, k, v, o, lse, dq=None, dk=None, dv=None, workspa
     """Returns (dq [T,Hq,d], dk, dv [T,Hkv,d]) bf16."""
     import torch
     if dq is None:
-        dq = torch.empty_like(q)
+        dq = _result(q, stream)
     if dk is None:
-        dk = torch.empty_like(k)
+        dk = _result(k, stream)
     if dv is None:
-        dv = torch.empty_like(v)
+        dv = _result(v, stream)
     fast = _fast(stream) if workspace is not None else None
     if fast:
         code = fast.bwd(False, plan._key, d_o, q, k, v, o, lse, dq, dk, dv, workspace, status)
@@ -395,7 +422,7 @@ def psa_bwd_f32(plan: Plan, d_o, q, k, v, o, lse, dq=None, dk=None, dv=None, wor
     """psa_bwd with fp32 gradient outputs: returns (dq [T,Hq,d], dk, dv [T,Hkv,d]) fp32, the
     kernels' fp32 accumulators written out without the final rounding to bf16."""
     import torch
-    f32 = lambda t: torch.empty(t.shape, dtype=torch.float32, device=t.device)
+    f32 = lambda t: _result(t, stream, lambda: torch.empty(t.shape, dtype=torch.float32, device=t.device))
     dq = f32(q) if dq is None else dq
     dk = f32(k) if dk is None else dk
     dv = f32(v) if dv is None else dv
@@ -463,7 +490,7 @@ def dpo_logp(logits, targets, segment_ids, n_segments, fork_rows=None, fork_targ
     else:
         fork_rows = fork_targets = fork_segments = None
     if out is None:
-        out = torch.empty(n_segments, dtype=torch.float32, device=logits.device)
+        out = _result(logits, stream, lambda: torch.empty(n_segments, dtype=torch.float32, device=logits.device))
     if scratch is None:
         scratch = _temporary(max(n_segments, 0) + 1, torch.float64, logits.device, stream)
     else:
@@ -544,8 +571,8 @@ def dpo_loss(policy_logps, ref_logps, beta, stream=None):
     assert ref_logps.shape == policy_logps.shape and ref_logps.dtype == torch.float32 and ref_logps.is_contiguous()
     _want_flat(ref_logps, "ref_logps", torch.float32, policy_logps.numel())
     n = policy_logps.numel() // 2
-    loss = torch.empty(1, dtype=torch.float32, device=policy_logps.device)
-    coef = torch.empty(2 * n, dtype=torch.float32, device=policy_logps.device)
+    loss, coef = (_result(policy_logps, stream, lambda m=m: torch.empty(m, dtype=torch.float32, device=policy_logps.device))
+                  for m in (1, 2 * n))
     _check("dpo_loss", load_library().dpo_loss(_ptr(policy_logps), _ptr(ref_logps), n, float(beta), _ptr(loss),
                                               _ptr(coef), _stream(stream)))
     return loss, coef
@@ -567,8 +594,8 @@ def simpo_loss(policy_logps, lengths, beta, gamma, status=None, stream=None):
     _want_flat(lengths, "lengths", torch.int32, policy_logps.numel())
     _want_status(status)
     n = policy_logps.numel() // 2
-    loss = torch.empty(1, dtype=torch.float32, device=policy_logps.device)
-    coef = torch.empty(2 * n, dtype=torch.float32, device=policy_logps.device)
+    loss, coef = (_result(policy_logps, stream, lambda m=m: torch.empty(m, dtype=torch.float32, device=policy_logps.device))
+                  for m in (1, 2 * n))
     _check("simpo_loss", load_library().simpo_loss(_ptr(policy_logps), _ptr(lengths), n, float(beta),
                                                   float(gamma), _ptr(loss), _ptr(coef), _ptr(status),
                                                   _stream(stream)))
@@ -591,8 +618,8 @@ def orpo_loss(policy_logps, lengths, lam, status=None, stream=None):
     _want_flat(lengths, "lengths", torch.int32, policy_logps.numel())
     _want_status(status)
     n = policy_logps.numel() // 2
-    loss = torch.empty(1, dtype=torch.float32, device=policy_logps.device)
-    coef = torch.empty(2 * n, dtype=torch.float32, device=policy_logps.device)
+    loss, coef = (_result(policy_logps, stream, lambda m=m: torch.empty(m, dtype=torch.float32, device=policy_logps.device))
+                  for m in (1, 2 * n))
     _check("orpo_loss", load_library().orpo_loss(_ptr(policy_logps), _ptr(lengths), n, float(lam), _ptr(loss),
                                                 _ptr(coef), _ptr(status), _stream(stream)))
     return loss, coef
@@ -617,7 +644,8 @@ def dpo_logp_bwd(logits, targets, segment_ids, coef, fork_rows=None, fork_target
         fork_rows = fork_targets = fork_segments = None
     assert coef.is_cuda and coef.dtype == torch.float32 and coef.is_contiguous()
     if dlogits is None:
-        dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=logits.device)
+        dlogits = _result(logits, stream, lambda: torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype,
+                                                                      device=logits.device))
     assert dlogits.dtype == logits.dtype and dlogits.stride() == logits.stride()
     if not dlogits.is_cuda or dlogits.shape[0] < n_rows or dlogits.shape[1] < vocab:
         raise ValueError("dlogits: a CUDA tensor of the logits' shape is needed")
@@ -716,7 +744,7 @@ def psa_rope(x, position_ids, rope_theta=10000.0, out=None, stream=None):
     assert x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous() and x.dim() == 3
     assert position_ids.is_cuda and position_ids.dtype == torch.int32 and position_ids.numel() == x.shape[0]
     if out is None:
-        out = torch.empty_like(x)
+        out = _result(x, stream)
     _want_flat(out, "out", torch.bfloat16, x.numel())
     _check("psa_rope", load_library().psa_rope(_ptr(x), _ptr(out), _ptr(position_ids), x.shape[0], x.shape[1],
                                               x.shape[2], float(rope_theta), _stream(stream)))
@@ -801,11 +829,12 @@ def psa_norm(x, weight, bias=None, eps=1e-5, rms=False, residual=None, out=None,
     elif total is not None:
         raise ValueError("total: there is none without residual")
     _want_given(given)
-    out = torch.empty_like(x) if out is None else out
-    stats = torch.empty((2, T), dtype=torch.float32, device=x.device) if stats is None else stats
+    out = _result(x, stream) if out is None else out
+    if stats is None:
+        stats = _result(x, stream, lambda: torch.empty((2, T), dtype=torch.float32, device=x.device))
     outputs = [("out", out, (T, D), x.dtype), ("stats", stats, (2, T), torch.float32)]
     if residual is not None:
-        total = torch.empty_like(x) if total is None else total
+        total = _result(x, stream) if total is None else total
         outputs.append(("total", total, (T, D), x.dtype))
     _want_given(outputs)
     _want_in_place([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given], {"out": ("x", "residual"),
@@ -845,11 +874,11 @@ def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=Fal
         raise ValueError("dbias: the root-mean-square form has no bias")
     _want_given(given)
     _want_status(status)
-    dx = torch.empty_like(x) if dx is None else dx
-    dweight = torch.empty_like(weight) if dweight is None else dweight
+    dx = _result(x, stream) if dx is None else dx
+    dweight = _result(weight, stream) if dweight is None else dweight
     outputs = [("dx", dx, (T, D), x.dtype), ("dweight", dweight, (D,), weight.dtype)]
     if with_bias or dbias is not None:
-        dbias = torch.empty_like(weight) if dbias is None else dbias
+        dbias = _result(weight, stream) if dbias is None else dbias
         outputs.append(("dbias", dbias, (D,), weight.dtype))
     _want_given(outputs)
     _want_in_place([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given], {"dx": ("d_out", "d_total", "x")})
@@ -879,7 +908,8 @@ def psa_embed(token_ids, table, scale=1.0, out=None, status=None, stream=None):
     T, (V, D) = token_ids.shape[0], table.shape
     _want_given([("token_ids", token_ids, (T,), torch.int32), ("table", table, (V, D), table.dtype)])
     _want_status(status)
-    out = torch.empty((T, D), dtype=table.dtype, device=table.device) if out is None else out
+    if out is None:
+        out = _result(table, stream, lambda: torch.empty((T, D), dtype=table.dtype, device=table.device))
     _want_given([("out", out, (T, D), table.dtype)])
     _want_apart([("out", out)], [("token_ids", token_ids), ("table", table)])
     _check("psa_embed", load_library().psa_embed(_ptr(token_ids), _ptr(table), dtype, T, V, D, float(scale), _ptr(out),
@@ -909,7 +939,7 @@ def psa_embed_bwd(d_out, token_ids, vocab, scale=1.0, dtable=None, dtype=None, a
     _want_given([("d_out", d_out, (T, D), d_out.dtype), ("token_ids", token_ids, (T,), torch.int32)])
     _want_status(status)
     if dtable is None:
-        dtable = torch.empty((V, D), dtype=dtype or d_out.dtype, device=d_out.device)
+        dtable = _result(d_out, stream, lambda: torch.empty((V, D), dtype=dtype or d_out.dtype, device=d_out.device))
     grad = _dtype_code(dtable, "dtable")
     if (dtype is not None and dtable.dtype != dtype) or (code == PSA_DTYPE_F32 and grad != PSA_DTYPE_F32):
         raise ValueError("dtable: dtype %s does not fit" % dtable.dtype)
@@ -950,10 +980,10 @@ def psa_ffn(x, w_gate, w_up, w_down, save=True, out=None, gate=None, up=None, wo
     T, D, F, given = _want_ffn(x, w_gate, w_up, w_down)
     _want_given(given)
     _want_status(status)
-    out = torch.empty_like(x) if out is None else out
+    out = _result(x, stream) if out is None else out
     outputs = [("out", out, (T, D), torch.bfloat16)]
     if save:
-        new = lambda: torch.empty((T, F), dtype=torch.bfloat16, device=x.device)  # noqa: E731
+        new = lambda: _result(x, stream, lambda: torch.empty((T, F), dtype=torch.bfloat16, device=x.device))  # noqa: E731
         gate, up = new() if gate is None else gate, new() if up is None else up
         outputs += [("gate", gate, (T, F), torch.bfloat16), ("up", up, (T, F), torch.bfloat16)]
     elif gate is not None or up is not None:
@@ -985,7 +1015,7 @@ def psa_ffn_bwd(d_out, x, w_gate, w_up, w_down, saved, dx=None, dw_gate=None, dw
     given += [("d_out", d_out, (T, D), torch.bfloat16), ("gate", gate, (T, F), torch.bfloat16), ("up", up, (T, F), torch.bfloat16)]
     _want_given(given)
     _want_status(status)
-    dx, dw_gate, dw_up, dw_down = (torch.empty_like(like) if t is None else t
+    dx, dw_gate, dw_up, dw_down = (_result(like, stream) if t is None else t
                                    for t, like in ((dx, x), (dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down)))
     outputs = [("dx", dx, (T, D), torch.bfloat16), ("dw_gate", dw_gate, (D, F), torch.bfloat16),
                ("dw_up", dw_up, (D, F), torch.bfloat16), ("dw_down", dw_down, (F, D), torch.bfloat16)]
