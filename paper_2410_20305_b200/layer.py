@@ -15,9 +15,10 @@ from . import binding as B
 class AttentionLayer:
     """Holds a plan, the position ids and the scratch of one pack; `forward` and `backward`
     run the layer for bf16 CUDA inputs x [T, hidden] and weights wq [hidden, Hq d],
-    wk, wv [hidden, Hkv d], wo [Hq d, hidden]."""
+    wk, wv [hidden, Hkv d], wo [Hq d, hidden].  `status` (optional): the int32 CUDA word in which
+    psa_fwd and psa_bwd report a wait that gave up."""
 
-    def __init__(self, pack_lengths, n_q_heads, n_kv_heads, head_dim, device, rope_theta=10000.0):
+    def __init__(self, pack_lengths, n_q_heads, n_kv_heads, head_dim, device, rope_theta=10000.0, status=None):
         import torch
         cu, P, C, R = pack_lengths
         self.plan = B.psa_plan(cu, P, C, R, n_q_heads, n_kv_heads, head_dim)
@@ -25,6 +26,7 @@ class AttentionLayer:
         self.neg = -self.pos
         self.ws = torch.empty(max(self.plan.bwd_workspace_bytes, 256), dtype=torch.uint8, device=device)
         self.theta = float(rope_theta)
+        self.status = status
         self.Hq, self.Hkv, self.d = n_q_heads, n_kv_heads, head_dim
 
     def forward(self, x, wq, wk, wv, wo):
@@ -34,7 +36,7 @@ class AttentionLayer:
         v = (x @ wv).view(T, self.Hkv, self.d)
         B.psa_rope(q, self.pos, self.theta, out=q)
         B.psa_rope(k, self.pos, self.theta, out=k)
-        o, lse = B.psa_fwd(self.plan, q, k, v)
+        o, lse = B.psa_fwd(self.plan, q, k, v, status=self.status)
         out = o.view(T, self.Hq * self.d) @ wo
         return out, (q, k, v, o, lse)
 
@@ -44,7 +46,7 @@ class AttentionLayer:
         T = x.shape[0]
         d_o = (d_out @ wo.t()).view(T, self.Hq, self.d)
         dwo = o.view(T, self.Hq * self.d).t() @ d_out
-        dq, dk, dv = B.psa_bwd(self.plan, d_o, q, k, v, o, lse, workspace=self.ws)
+        dq, dk, dv = B.psa_bwd(self.plan, d_o, q, k, v, o, lse, workspace=self.ws, status=self.status)
         # the gradient of a rotation is the inverse rotation
         B.psa_rope(dq, self.neg, self.theta, out=dq)
         B.psa_rope(dk, self.neg, self.theta, out=dk)
@@ -62,12 +64,14 @@ class DecoderLayer:
     w_down [ffn, hidden], all bf16.
 
     A layer takes the residual stream x and what is still to be added to it (`delta`, the feed-forward output of the layer
-    before; None in the first one): the addition is part of its first norm, as that of the attention's output is of its second."""
+    before; None in the first one): the addition is part of its first norm, as that of the attention's output is of its second.
+    `status` (optional): the int32 CUDA word in which all its calls report a wait that gave up."""
 
     KEYS = ("norm1", "wq", "wk", "wv", "wo", "norm2", "w_gate", "w_up", "w_down")
 
-    def __init__(self, pack_lengths, n_q_heads, n_kv_heads, head_dim, device, rope_theta=10000.0, eps=1e-5):
-        self.attention = AttentionLayer(pack_lengths, n_q_heads, n_kv_heads, head_dim, device, rope_theta)
+    def __init__(self, pack_lengths, n_q_heads, n_kv_heads, head_dim, device, rope_theta=10000.0, eps=1e-5, status=None):
+        self.attention = AttentionLayer(pack_lengths, n_q_heads, n_kv_heads, head_dim, device, rope_theta, status)
+        self.status = status
         self.eps = float(eps)
 
     def forward(self, x, w, delta=None):
@@ -78,7 +82,7 @@ class DecoderLayer:
             a, stats1, x = B.psa_norm(x, w["norm1"], eps=self.eps, rms=True, residual=delta)
         attn, saved = self.attention.forward(a, w["wq"], w["wk"], w["wv"], w["wo"])
         b, stats2, mid = B.psa_norm(attn, w["norm2"], eps=self.eps, rms=True, residual=x)
-        out, gate_up = B.psa_ffn(b, w["w_gate"], w["w_up"], w["w_down"])
+        out, gate_up = B.psa_ffn(b, w["w_gate"], w["w_up"], w["w_down"], status=self.status)
         return mid, out, (x, a, stats1, saved, mid, b, stats2, gate_up)
 
     def backward(self, d_stream, d_delta, w, saved):
@@ -86,8 +90,9 @@ class DecoderLayer:
         gradients).  Where the layer's output is their sum, both are the gradient of the output."""
         x, a, stats1, attn_saved, mid, b, stats2, gate_up = saved
         g = {}
-        db, g["w_gate"], g["w_up"], g["w_down"] = B.psa_ffn_bwd(d_delta, b, w["w_gate"], w["w_up"], w["w_down"], gate_up)
-        d_mid, g["norm2"], _ = B.psa_norm_bwd(db, mid, w["norm2"], stats2, rms=True, d_total=d_stream)
+        db, g["w_gate"], g["w_up"], g["w_down"] = B.psa_ffn_bwd(d_delta, b, w["w_gate"], w["w_up"], w["w_down"], gate_up,
+                                                                          status=self.status)
+        d_mid, g["norm2"], _ = B.psa_norm_bwd(db, mid, w["norm2"], stats2, rms=True, d_total=d_stream, status=self.status)
         da, g["wq"], g["wk"], g["wv"], g["wo"] = self.attention.backward(a, w["wq"], w["wk"], w["wv"], w["wo"], attn_saved, d_mid)
-        dx, g["norm1"], _ = B.psa_norm_bwd(da, x, w["norm1"], stats1, rms=True, d_total=d_mid)
+        dx, g["norm1"], _ = B.psa_norm_bwd(da, x, w["norm1"], stats1, rms=True, d_total=d_mid, status=self.status)
         return dx, g
