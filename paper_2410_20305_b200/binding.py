@@ -173,6 +173,12 @@ def _check(fn, code):
         raise PsaError(fn, code, load_library().psa_status_string(code).decode())
 
 
+def _want_widths(fn, *widths):
+    """Raises the library's refusal (status 3) for a width that its 32-bit argument would cut off."""
+    if max(widths) > 0x7fffffff:
+        _check(fn, 3)
+
+
 def _i32(a):
     if type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous:
         return a
@@ -746,6 +752,7 @@ def psa_rope(x, position_ids, rope_theta=10000.0, out=None, stream=None):
     if out is None:
         out = _result(x, stream)
     _want_flat(out, "out", torch.bfloat16, x.numel())
+    _want_widths("psa_rope", x.shape[1], x.shape[2])
     _check("psa_rope", load_library().psa_rope(_ptr(x), _ptr(out), _ptr(position_ids), x.shape[0], x.shape[1],
                                               x.shape[2], float(rope_theta), _stream(stream)))
     return out
@@ -829,6 +836,7 @@ def psa_norm(x, weight, bias=None, eps=1e-5, rms=False, residual=None, out=None,
     elif total is not None:
         raise ValueError("total: there is none without residual")
     _want_given(given)
+    _want_widths("psa_norm", D)
     out = _result(x, stream) if out is None else out
     if stats is None:
         stats = _result(x, stream, lambda: torch.empty((2, T), dtype=torch.float32, device=x.device))
@@ -874,6 +882,7 @@ def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=Fal
         raise ValueError("dbias: the root-mean-square form has no bias")
     _want_given(given)
     _want_status(status)
+    _want_widths("psa_norm_bwd", D)
     dx = _result(x, stream) if dx is None else dx
     dweight = _result(weight, stream) if dweight is None else dweight
     outputs = [("dx", dx, (T, D), x.dtype), ("dweight", dweight, (D,), weight.dtype)]
@@ -908,6 +917,7 @@ def psa_embed(token_ids, table, scale=1.0, out=None, status=None, stream=None):
     T, (V, D) = token_ids.shape[0], table.shape
     _want_given([("token_ids", token_ids, (T,), torch.int32), ("table", table, (V, D), table.dtype)])
     _want_status(status)
+    _want_widths("psa_embed", D)
     if out is None:
         out = _result(table, stream, lambda: torch.empty((T, D), dtype=table.dtype, device=table.device))
     _want_given([("out", out, (T, D), table.dtype)])
@@ -938,6 +948,7 @@ def psa_embed_bwd(d_out, token_ids, vocab, scale=1.0, dtable=None, dtype=None, a
     code = _dtype_code(d_out, "d_out")
     _want_given([("d_out", d_out, (T, D), d_out.dtype), ("token_ids", token_ids, (T,), torch.int32)])
     _want_status(status)
+    _want_widths("psa_embed_bwd", D)
     if dtable is None:
         dtable = _result(d_out, stream, lambda: torch.empty((V, D), dtype=dtype or d_out.dtype, device=d_out.device))
     grad = _dtype_code(dtable, "dtable")
@@ -980,6 +991,7 @@ def psa_ffn(x, w_gate, w_up, w_down, save=True, out=None, gate=None, up=None, wo
     T, D, F, given = _want_ffn(x, w_gate, w_up, w_down)
     _want_given(given)
     _want_status(status)
+    _want_widths("psa_ffn", D, F)
     out = _result(x, stream) if out is None else out
     outputs = [("out", out, (T, D), torch.bfloat16)]
     if save:
@@ -1015,6 +1027,7 @@ def psa_ffn_bwd(d_out, x, w_gate, w_up, w_down, saved, dx=None, dw_gate=None, dw
     given += [("d_out", d_out, (T, D), torch.bfloat16), ("gate", gate, (T, F), torch.bfloat16), ("up", up, (T, F), torch.bfloat16)]
     _want_given(given)
     _want_status(status)
+    _want_widths("psa_ffn_bwd", D, F)
     dx, dw_gate, dw_up, dw_down = (_result(like, stream) if t is None else t
                                    for t, like in ((dx, x), (dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down)))
     outputs = [("dx", dx, (T, D), torch.bfloat16), ("dw_gate", dw_gate, (D, F), torch.bfloat16),
