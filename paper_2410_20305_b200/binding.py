@@ -770,6 +770,14 @@ def _want_given(given):
         raise ValueError("tensors on %s: all have to be on the current device" % ", ".join(sorted(map(str, devices))))
 
 
+def _want_status_here(status):
+    """_want_status, and the word lies on the current device: kernels that run there add to it."""
+    import torch
+    _want_status(status)
+    if status is not None and status.numel() and status.device.type == "cuda" and status.device.index != torch.cuda.current_device():
+        raise ValueError("status: on %s, the call runs on the current device" % status.device)
+
+
 def _want_apart(outputs, inputs):
     """Raises ValueError where an output, a (name, tensor), shares memory with an input or with another output."""
     span = lambda t: (t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())  # noqa: E731
@@ -881,7 +889,7 @@ def psa_norm_bwd(d_out, x, weight, stats, rms=False, d_total=None, with_bias=Fal
     if rms and (with_bias or dbias is not None):
         raise ValueError("dbias: the root-mean-square form has no bias")
     _want_given(given)
-    _want_status(status)
+    _want_status_here(status)
     _want_widths("psa_norm_bwd", D)
     dx = _result(x, stream) if dx is None else dx
     dweight = _result(weight, stream) if dweight is None else dweight
@@ -916,7 +924,7 @@ def psa_embed(token_ids, table, scale=1.0, out=None, status=None, stream=None):
     dtype = _dtype_code(table, "table")
     T, (V, D) = token_ids.shape[0], table.shape
     _want_given([("token_ids", token_ids, (T,), torch.int32), ("table", table, (V, D), table.dtype)])
-    _want_status(status)
+    _want_status_here(status)
     _want_widths("psa_embed", D)
     if out is None:
         out = _result(table, stream, lambda: torch.empty((T, D), dtype=table.dtype, device=table.device))
@@ -947,7 +955,7 @@ def psa_embed_bwd(d_out, token_ids, vocab, scale=1.0, dtable=None, dtype=None, a
     T, D, V = d_out.shape[0], d_out.shape[1], int(vocab)
     code = _dtype_code(d_out, "d_out")
     _want_given([("d_out", d_out, (T, D), d_out.dtype), ("token_ids", token_ids, (T,), torch.int32)])
-    _want_status(status)
+    _want_status_here(status)
     _want_widths("psa_embed_bwd", D)
     if dtable is None:
         dtable = _result(d_out, stream, lambda: torch.empty((V, D), dtype=dtype or d_out.dtype, device=d_out.device))
@@ -990,7 +998,7 @@ def psa_ffn(x, w_gate, w_up, w_down, save=True, out=None, gate=None, up=None, wo
     import torch
     T, D, F, given = _want_ffn(x, w_gate, w_up, w_down)
     _want_given(given)
-    _want_status(status)
+    _want_status_here(status)
     _want_widths("psa_ffn", D, F)
     out = _result(x, stream) if out is None else out
     outputs = [("out", out, (T, D), torch.bfloat16)]
@@ -1026,7 +1034,7 @@ def psa_ffn_bwd(d_out, x, w_gate, w_up, w_down, saved, dx=None, dw_gate=None, dw
     gate, up = saved
     given += [("d_out", d_out, (T, D), torch.bfloat16), ("gate", gate, (T, F), torch.bfloat16), ("up", up, (T, F), torch.bfloat16)]
     _want_given(given)
-    _want_status(status)
+    _want_status_here(status)
     _want_widths("psa_ffn_bwd", D, F)
     dx, dw_gate, dw_up, dw_down = (_result(like, stream) if t is None else t
                                    for t, like in ((dx, x), (dw_gate, w_gate), (dw_up, w_up), (dw_down, w_down)))

@@ -372,6 +372,12 @@ bool take_optional(PyObject* o, at::ScalarType type, at::IntArrayRef shape, void
   if (t) *p = t->data_ptr();
   return t != nullptr;
 }
+// As take_status; a word on another device is binding.py's to refuse.
+bool take_status_here(PyObject* o, void** p) {
+  if (!take_status(o, p)) return false;
+  const at::Tensor* t = o == Py_None ? nullptr : plain(o);
+  return !t || t->numel() == 0 || here(*t);
+}
 bool take_bool(PyObject* o, bool* v) {
   *v = o == Py_True;
   return PyBool_Check(o);
@@ -453,7 +459,7 @@ PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     bool rms, with_bias;
     void *d_out, *stats, *d_total, *word;
     at::Tensor ws;
-    if (n != 9 || !take_status(a[8], &word) || !modes_off() || !take_norm(a[1], a[2], &m) || !take_bool(a[4], &rms) || !take_bool(a[6], &with_bias) ||
+    if (n != 9 || !take_status_here(a[8], &word) || !modes_off() || !take_norm(a[1], a[2], &m) || !take_bool(a[4], &rms) || !take_bool(a[6], &with_bias) ||
         a[0] == Py_None || !take_optional(a[0], m.x->scalar_type(), {m.T, m.hidden}, &d_out) || a[3] == Py_None ||
         !take_optional(a[3], at::kFloat, {2, m.T}, &stats) ||
         !take_optional(a[5], m.x->scalar_type(), {m.T, m.hidden}, &d_total) || (rms && with_bias) ||
@@ -479,7 +485,7 @@ PyObject* embed(PyObject*, PyObject* const* a, Py_ssize_t n) {
     float scale;
     void* st;
     int32_t dtype;
-    if (n != 4 || !modes_off() || !take_float(a[2], &scale) || !take_status(a[3], &st)) return none();
+    if (n != 4 || !modes_off() || !take_float(a[2], &scale) || !take_status_here(a[3], &st)) return none();
     const at::Tensor *ids = plain(a[0]), *table = plain(a[1]);
     if (!ids || !table || ids->dim() != 1 || ids->scalar_type() != at::kInt || !ids->is_contiguous() || !here(*ids) ||
         table->dim() != 2 || !table->is_contiguous() || !here(*table) || !take_dtype(*table, &dtype) ||
@@ -507,7 +513,7 @@ PyObject* embed_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t dtype;
     at::Tensor ws;
     if (n != 7 || !modes_off() || !take_int(a[2], &V) || !take_float(a[3], &scale) || !take_bool(a[4], &f32) ||
-        !take_status(a[6], &st))
+        !take_status_here(a[6], &st))
       return none();
     const at::Tensor *d = plain(a[0]), *ids = plain(a[1]);
     if (!d || d->dim() != 2 || !d->is_contiguous() || !here(*d) || !take_dtype(*d, &dtype) || d->size(1) > INT32_MAX || V <= 0 ||
@@ -555,7 +561,7 @@ PyObject* ffn(PyObject*, PyObject* const* a, Py_ssize_t n) {
     bool save;
     void* st;
     at::Tensor ws, gate, up;
-    if (n != 7 || !modes_off() || !take_ffn(a[0], a + 1, &f) || !take_bool(a[4], &save) || !take_status(a[6], &st) ||
+    if (n != 7 || !modes_off() || !take_ffn(a[0], a + 1, &f) || !take_bool(a[4], &save) || !take_status_here(a[6], &st) ||
         !take_workspace(a[5], g_lib.ffn_bytes(f.T, int32_t(f.D), int32_t(f.F), 0), *f.x, &ws))
       return none();
     at::Tensor out = make({f.T, f.D}, at::kBFloat16, *f.x);
@@ -583,7 +589,7 @@ PyObject* ffn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const auto b = at::kBFloat16;
     if (n != 9 || !modes_off() || !take_ffn(a[1], a + 2, &f) || a[0] == Py_None || a[5] == Py_None || a[6] == Py_None ||
         !take_optional(a[0], b, {f.T, f.D}, &d_out) || !take_optional(a[5], b, {f.T, f.F}, &gate) ||
-        !take_optional(a[6], b, {f.T, f.F}, &up) || !take_status(a[8], &st) ||
+        !take_optional(a[6], b, {f.T, f.F}, &up) || !take_status_here(a[8], &st) ||
         !take_workspace(a[7], g_lib.ffn_bytes(f.T, int32_t(f.D), int32_t(f.F), 1), *f.x, &ws))
       return none();
     at::Tensor dx = make({f.T, f.D}, b, *f.x), dg = make({f.D, f.F}, b, *f.x), du = make({f.D, f.F}, b, *f.x),
