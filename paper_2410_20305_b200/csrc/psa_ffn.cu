@@ -61,7 +61,7 @@ struct Product {
   int32_t n_outputs;           // outputs side by side
   int32_t first;               // the product's first tile in the launch
   int32_t a_mn, b_mn;          // which way the operands lie
-  int32_t early;               // B is not written by the kernel before this one, nor is that kernel's end awaited for it
+  int32_t early;               // B may be loaded before behind_wait(): see Wanted::early
 };
 struct ProductList {
   ProductMaps maps[kMaxProducts];
@@ -711,6 +711,8 @@ struct Wanted {
   Matrix a[2], b[2];
   __nv_bfloat16* out[2];
   int k_pairs, n_outputs;
+  // B may be loaded while the kernel before this one runs.  Only where that kernel is one of the same call, which waits before it
+  // lets this one start (so what came before the call is complete), and writes no B of this one.
   bool early;
 };
 

@@ -6,9 +6,12 @@
 // 2. Whatever the kernel before it may still read or write is touched only after behind_wait(), and is not declared
 //    `const T* __restrict__`: that says that nobody writes there while the kernel runs, and the compiler may load it early.
 // 3. A kernel that touches anything of others before its behind_wait() (dpo_logp_kernel the logits and labels,
-//    psa_bwd_kernel the plan and the tiles of Q, K, V, dO) is launched behind one that calls behind_wait() ahead of
-//    behind_go(): all that came before is complete by then.  psa_bwd_kernel calls behind_go() first, so only kernels that
-//    wait before they read (psa_fwd_kernel, psa_bwd_delta_kernel, psa_bwd_convert_kernel and those of the loss) may follow it.
+//    psa_bwd_kernel the plan and the tiles of Q, K, V, dO, ffn_small_kernel the B operand of a product that is marked
+//    `early`) is launched behind one that calls behind_wait() ahead of behind_go() and does not write it: all that came
+//    before is complete by then.  (An `early` product is never a call's first; the one before it is of the same call.)
+//    psa_bwd_kernel calls behind_go() first, so only kernels that wait before they read may follow it: psa_fwd_kernel,
+//    psa_bwd_delta_kernel, psa_bwd_convert_kernel, those of the loss, of the normalisation and of the embedding, and the
+//    first of the feed-forward block.
 #pragma once
 #include <cuda_runtime.h>
 
