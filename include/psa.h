@@ -499,12 +499,14 @@ psa_status_t dpo_logp_bwd(const void* logits, int32_t logits_dtype, int64_t n_ro
  *   x, residual  device [n_tokens, hidden] of `dtype`; residual may be NULL
  *   weight, bias device [hidden] of `weight_dtype`; bias may be NULL, and is NULL if rms
  *   dtype, weight_dtype   PSA_DTYPE_BF16 with either type of weights, or PSA_DTYPE_F32 with fp32 weights
- *   hidden       1 to 16384 (any: rows that are no multiple of 16 bytes are read element by element)
+ *   hidden       1 to 16384, any width
  *   rms          0: layer norm, else the root-mean-square form
  *   out          device [n_tokens, hidden] of `dtype` (out); may be x or residual
  *   total        device [n_tokens, hidden] of `dtype` (out): s; given where residual is, may be x or residual
  *   stats        device fp32 [2, n_tokens] (out): m of every row, then r of every row, for psa_norm_bwd
- * A row with a NaN or an infinity gives NaN in that row alone.  n_tokens = 0 is a no-op.
+ * A row with a NaN gives NaN in all of that row, one with an infinity too; in the RMS form r = 0 there, so that the infinite
+ * elements give NaN and the others 0.  No other row changes.  Squares are fp32: r = 0 where their sum passes 2^128.
+ * n_tokens = 0 is a no-op.
  * Errors: INVALID_ARG, UNSUPPORTED (hidden, n_tokens >= 2^31), ALIGNMENT (16 bytes), CUDA.
  */
 psa_status_t psa_norm(const void* x, const void* residual, const void* weight, const void* bias,
@@ -547,11 +549,13 @@ psa_status_t psa_embed(const int32_t* token_ids, const void* table, int32_t dtyp
 
 /*
  * psa_embed_bwd -- gradient of psa_embed's table: dtable[v] = scale * sum over t with token_ids[t] = v of d_out[t],
- * in fp32 and always in the tokens' order.
+ * in fp32 and in an order that the ids and the sizes fix: the same inputs give the same bits.  (Tokens are sorted by id, those of
+ * one id in their order, and added in runs of 16 or 32 sorted tokens; the sums of an id that spreads over several runs are added by
+ * eight warps, every eighth of them each, and the eight sums in the warps' order.)
  *   d_out       device [n_tokens, hidden] of `dtype`
  *   dtable      device [vocab, hidden] of `grad_dtype` (PSA_DTYPE_F32, or bf16 where d_out is bf16)
  *   accumulate  0: dtable is overwritten, with zeros in the rows of ids that do not occur;
- *               else the gradient is added to what dtable holds, and other rows are neither read nor written
+ *               else the gradient is added to what dtable holds, and the rows of other ids are left as they are
  *   workspace   device scratch of psa_embed_bwd_workspace_bytes() bytes, 16-byte aligned
  *   device_status  as for psa_embed; a bad id adds nothing
  * Errors and limits: as psa_embed.

@@ -939,7 +939,7 @@ def psa_embed_bwd(d_out, token_ids, vocab, scale=1.0, dtable=None, dtype=None, a
                   stream=None):
     """Gradient [vocab, hidden] of psa_embed's table for d_out [T, hidden] (bf16 or fp32), in d_out's type, or in fp32 with
     dtype=torch.float32 or an fp32 `dtable`.  With accumulate=True it is added to `dtable`, where only the rows of ids that
-    occur are touched.  Sums are fp32 and in the tokens' order."""
+    occur change.  Sums are fp32, in an order that the ids and the sizes fix: the same inputs give the same bits."""
     import torch
     fast = _fast(stream) if dtable is None and not accumulate and dtype in (None, torch.float32) else None
     if fast:

@@ -1,9 +1,9 @@
 // psa_embed / psa_embed_bwd: token embedding and the gradient of its table,
 //     y[t] = scale * table[id[t]],        dtable[v] = scale * sum over t with id[t] = v of dy[t].
 // Both are bound by HBM: the forward writes T rows, the backward reads T rows and writes the table's V rows once, zeros
-// included.  The backward's sums are fp32 and taken in the tokens' order, whatever the order in which CTAs run: the tokens are
-// sorted by id first (stably), a CTA adds a fixed run of the sorted tokens, and an id whose tokens spread over several runs
-// has the runs' sums added in their order.
+// included.  The backward's sums are fp32 and in an order that the ids and the sizes fix, whatever the order in which CTAs run: the
+// tokens are sorted by id first (stably), a CTA adds a fixed run of the sorted tokens in their order, and an id whose tokens
+// spread over several runs has the runs' sums added by eight warps, every eighth of them each, and those of the warps in order.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
