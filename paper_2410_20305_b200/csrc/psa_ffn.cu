@@ -742,7 +742,8 @@ psa_status_t launch(void (*kernel)(Params...), int64_t grid, unsigned threads, u
 }
 
 // Estimates in us that choose between the two kernels and the parts of K, fitted to both at 36 sizes (16 to 2500 tokens,
-// 512 x 1408 to 4096 x 14336, L2 cold; most within 15 %).  A pair's stage takes 0.37 with all SMs at work, 0.31 with few, the
+// 512 x 1408 to 4096 x 14336, L2 cold: of 216 chosen launches 85 % are within 15 % of their estimate, 97 % within 20 %, and the
+// choice took 2.4 % longer than the fastest one in the mean).  A pair's stage takes 0.37 with all SMs at work, 0.31 with few, the
 // end of a tile 2.4 and more where it is not hidden behind the next tile's stages.  A stage of a CTA alone takes 0.38 (0.25 with
 // few tokens), of an SM's two CTAs together 0.56; the parts of a split K cross between the SMs of their cluster at 1 TB/s
 // (2816 features, K = 1024, 128 tokens in 8 parts: 23 MB, 45 us instead of 16).  Where they differ most: 1815 x 2048,

@@ -62,8 +62,10 @@ __device__ __forceinline__ void row_sum(float (&v)[N], float (*s_part)[32], int 
 // A thread's columns in a row that starts `a` elements behind an aligned one: window k holds the columns [k V - a, (k + 1) V - a).
 // `stride` rows lie between the rows that a warp or CTA takes, a multiple of V where it takes several: `a`, and with it every
 // column of a thread, is the same in all of them.  Where a thread has one or two windows (kHold) it keeps its weights in
-// registers and requests the next row ahead of the sums of this one; with a CTA for each row these kernels were bound by
-// instructions, the weights' shift among them (5465 x 1237 bf16 with residual: 20.7 us, so 16.8; 4000 x 4095 35.6 and 27.7).
+// registers and requests the next row ahead of the sums of this one; with a CTA for each row these kernels took more instructions,
+// the weights' shift among them (bf16 layer norm with residual, one call between two events, cold in L2: 5465 x 1237 26.6 us, so 20.5;
+// 4000 x 4095 49.2 and 36.9; 8000 x 1025 34.8 and 26.6).  At 1237 columns 66 % of the issue slots are taken, 41 % of DRAM's time and
+// 40 % of the warps.
 template <typename XT, typename WT, int NV, bool kWarp, bool kRagged>
 __global__ void __launch_bounds__(max_threads<XT, NV, kWarp, kRagged>(), fwd_ctas<XT, NV, kWarp, kRagged>())
 norm_kernel(const XT* x, const XT* residual, const WT* weight, const WT* bias, int64_t n_tokens, int64_t stride, int32_t hidden,
@@ -523,7 +525,8 @@ int ctas_per_sm(const Division& d) { return d.threads == 32 ? 2 : grouped(d) ? 1
 int groups_of(const Division& d, int64_t tiles) {
   return grouped(d) ? int(std::max<int64_t>(1, std::min<int64_t>({(tiles + kSmCount - 1) / kSmCount, 512 / d.threads, kMaxGroups}))) : 1;
 }
-// Rows of a tile: one, or 8 for each of a CTA's warps, fewer where all tiles would not fill the SMs, and 8 KB of a tensor at most.
+// Rows of a tile: one, or one for each of a CTA's 8 warps, whatever their size (16 KB of a tensor at 1024 columns of bf16, 32 KB of
+// fp32); up to 8 for each warp where a tensor's tile stays within 8 KB and there are tiles enough to fill the SMs.
 int tile_rows(const Division& d, int64_t n_tokens, int32_t hidden, int elem_bytes) {
   if (d.threads != 32) return 1;
   int rows = kRowsPerCta;
