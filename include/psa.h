@@ -51,9 +51,9 @@ typedef enum {
 
 /* Bits of the word a kernel ORs into `device_status` (device int32, may be NULL). */
 #define PSA_DEVSTAT_WAIT_EXPIRED 1 /* a bounded barrier wait gave up; outputs are invalid    */
-#define PSA_DEVSTAT_BAD_TARGET   2 /* dpo_logp: a scored target id was outside [0, vocab);
+#define PSA_DEVSTAT_BAD_TARGET   2 /* dpo_logp, dpo_linear_logp: a scored target id was outside [0, vocab);
                                       psa_embed, psa_embed_bwd: a token id was             */
-#define PSA_DEVSTAT_BAD_SEGMENT  4 /* dpo_logp: a segment id was >= n_segments               */
+#define PSA_DEVSTAT_BAD_SEGMENT  4 /* dpo_logp, dpo_linear_logp: a segment id was >= n_segments */
 #define PSA_DEVSTAT_OUT_OF_BOUNDS 8 /* debug library only (libpsa_debug.so): a thread's own global
                                        index fell outside its tensor; the access was skipped     */
 
@@ -490,6 +490,54 @@ psa_status_t dpo_logp_bwd(const void* logits, int32_t logits_dtype, int64_t n_ro
                           const int32_t* fork_rows, const int32_t* fork_targets,
                           const int32_t* fork_segments, int32_t n_forks, int32_t n_segments,
                           const float* coef, void* dlogits, int32_t* device_status, void* stream);
+
+/*
+ * dpo_linear_logp -- dpo_logp straight from the hidden states and the output table: the logits
+ *     z[t][v] = scale * sum_c hidden[t][c] * table[v][c]
+ * are formed tile by tile, in fp32, and not kept.
+ *   out[g] = sum over scored (row t, label y) with response id g of  z[t][y] - log sum_v exp(z[t][v])
+ *   lse[t] = log sum_v exp(z[t][v]) of every row that scores a label, 0 of the others
+ *   hidden        device bf16 [n_rows, width]      table  device bf16 [vocab, width] (as psa_embed's)
+ *   width         a multiple of 8, at most 2^20;  n_rows, n_forks, n_segments and vocab at most 2^24
+ *   scale         positive and finite
+ *   targets, segment_ids, fork_rows, fork_targets, fork_segments, n_forks, n_segments   as for dpo_logp; a row may be
+ *                 named by any number of forks
+ *   out           device fp32 [n_segments] (out)   lse    device fp32 [n_rows] (out)
+ *   workspace     device scratch of dpo_linear_logp_workspace_bytes(.., backward = 0) bytes, 16-byte aligned
+ *   device_status device int32 or NULL: BAD_TARGET and BAD_SEGMENT as by dpo_logp, WAIT_EXPIRED as by psa_fwd
+ * The sums of the responses do not depend on the order of their terms: the same inputs give the same bits.  A term below
+ * -2^38 counts as -2^38, one that rounding has put above 0 as 0.  A row whose logits are not all finite has no
+ * log-probability: its term and lse are NaN.  Outputs must not overlap inputs or one another.
+ * Errors: INVALID_ARG, UNSUPPORTED (sizes), ALIGNMENT (hidden, table, workspace: 16 bytes), CUDA.
+ */
+size_t dpo_linear_logp_workspace_bytes(int64_t n_rows, int32_t n_forks, int32_t n_segments, int64_t vocab,
+                                       int32_t width, int32_t backward);
+psa_status_t dpo_linear_logp(const void* hidden, const void* table, int64_t n_rows, int64_t vocab, int32_t width,
+                             float scale, const int32_t* targets, const int32_t* segment_ids,
+                             const int32_t* fork_rows, const int32_t* fork_targets,
+                             const int32_t* fork_segments, int32_t n_forks, int32_t n_segments, float* out,
+                             float* lse, void* workspace, int32_t* device_status, void* stream);
+
+/*
+ * dpo_linear_logp_bwd -- gradient of sum_g coef[g] * out[g] with respect to hidden and table:
+ *     dz[t][v] = scale * sum over the labels (t, y, g) of coef[g] * (1[v == y] - exp(z[t][v] - lse[t])),
+ *     d_hidden = dz table,   d_table = dz^T hidden,
+ * with fp32 sums; the logits are formed again, in pieces of the vocabulary, and dz of a piece, rounded to bf16 for the two
+ * products, takes 1 GiB of the workspace at most (or 256 columns of the vocabulary, where those are more).
+ *   coef          device fp32 [n_segments], e.g. from dpo_loss
+ *   lse           device fp32 [n_rows] as written by dpo_linear_logp
+ *   d_hidden      device bf16 [n_rows, width] (out): zeros in rows that score nothing
+ *   d_table       device bf16 [vocab, width] (out), or NULL where it is not wanted
+ *   workspace     device scratch of dpo_linear_logp_workspace_bytes(.., backward = 1) bytes, 16-byte aligned
+ * No atomics on floats: the same inputs give the same bits.
+ * Errors and the rest: as dpo_linear_logp (d_hidden, d_table: 16 bytes).
+ */
+psa_status_t dpo_linear_logp_bwd(const float* coef, const void* hidden, const void* table, const float* lse,
+                                 int64_t n_rows, int64_t vocab, int32_t width, float scale,
+                                 const int32_t* targets, const int32_t* segment_ids, const int32_t* fork_rows,
+                                 const int32_t* fork_targets, const int32_t* fork_segments, int32_t n_forks,
+                                 int32_t n_segments, void* d_hidden, void* d_table, void* workspace,
+                                 int32_t* device_status, void* stream);
 
 /*
  * psa_norm -- normalisation of every token's row of hidden values, with the residual add in front of it (the step

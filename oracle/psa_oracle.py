@@ -618,3 +618,34 @@ def ffn_bwd(d_out, x, w_gate, w_up, w_down):
     dh = d_out @ w_down.T
     d_gate, d_up = dh * up * (s + gate * s * (1.0 - s)), dh * gate * s
     return d_gate @ w_gate.T + d_up @ w_up.T, x.T @ d_gate, x.T @ d_up, h.T @ d_out
+
+
+# ------------------------------------------------------------------ log-probabilities from hidden states
+def linear_logp(hidden, table, targets, segment_ids, n_segments, fork_rows=(), fork_targets=(), fork_segments=(), scale=1.0):
+    """dpo_logp of the logits scale * hidden @ table.T, and log sum exp of the logits of every row that scores a valid label (0 of
+    the others): (out, lse).  A label whose target or response is out of range counts as absent, a fork that names no row too."""
+    z = scale * (_as_f64(hidden) @ _as_f64(table).T)
+    out, lse = np.zeros(n_segments), np.zeros(len(z))
+    for t, y, g in _labels(len(z), z.shape[1], n_segments, targets, segment_ids, fork_rows, fork_targets, fork_segments):
+        top = z[t].max()
+        lse[t] = top + np.log(np.exp(z[t] - top).sum())
+        out[g] += z[t, y] - lse[t]
+    return out, lse
+
+
+def linear_logp_grad(hidden, table, targets, segment_ids, coef, fork_rows=(), fork_targets=(), fork_segments=(), scale=1.0):
+    """(d_hidden, d_table, dz) of sum_g coef[g] * linear_logp(...)[0][g]; dz is the gradient of scale-free products
+    hidden @ table.T."""
+    h, w = _as_f64(hidden), _as_f64(table)
+    z = scale * (h @ w.T)
+    dz = np.zeros_like(z)
+    for t, y, g in _labels(len(z), z.shape[1], len(coef), targets, segment_ids, fork_rows, fork_targets, fork_segments):
+        p = np.exp(z[t] - z[t].max())
+        dz[t] -= coef[g] * scale * p / p.sum()
+        dz[t, y] += coef[g] * scale
+    return dz @ w, dz.T @ h, dz
+
+
+def _labels(n_rows, vocab, n_segments, targets, segment_ids, fork_rows, fork_targets, fork_segments):
+    every = [(t, targets[t], segment_ids[t]) for t in range(n_rows)] + list(zip(fork_rows, fork_targets, fork_segments))
+    return [(int(t), int(y), int(g)) for t, y, g in every if 0 <= t < n_rows and 0 <= y < vocab and 0 <= g < n_segments]

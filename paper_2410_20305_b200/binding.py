@@ -42,6 +42,7 @@ EXPORTED_SYMBOLS = (
     "psa_check_device_status", "psa_selftest_wait_expiry", "psa_logp_labels", "psa_pack_ffd_emit",
     "psa_selftest_bounds", "dpo_logp_f64sum", "psa_plan_launch", "psa_norm", "psa_norm_bwd", "psa_norm_bwd_workspace_bytes",
     "psa_embed", "psa_embed_bwd", "psa_embed_bwd_workspace_bytes", "psa_ffn", "psa_ffn_bwd", "psa_ffn_workspace_bytes",
+    "dpo_linear_logp", "dpo_linear_logp_bwd", "dpo_linear_logp_workspace_bytes",
 )
 
 
@@ -111,6 +112,9 @@ def load_library():
     lib.psa_ffn.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.psa_ffn_bwd.argtypes = [vp] * 7 + [i64, i32, i32] + [vp] * 7
     lib.psa_ffn_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    lib.dpo_linear_logp.argtypes = [vp, vp, i64, i64, i32, f32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    lib.dpo_linear_logp_bwd.argtypes = [vp, vp, vp, vp, i64, i64, i32, f32, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    lib.dpo_linear_logp_workspace_bytes.argtypes = [i64, i32, i32, i64, i32, i32]
     lib.psa_step_host_arena_bytes.argtypes = [vp]
     for name in EXPORTED_SYMBOLS:
         if name.endswith("_bytes"):
@@ -1049,3 +1053,83 @@ def psa_ffn_bwd(d_out, x, w_gate, w_up, w_down, saved, dx=None, dw_gate=None, dw
                                           T, D, F, _ptr(dx), _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down), _ptr(workspace),
                                           _ptr(status), _stream(stream)))
     return dx, dw_gate, dw_up, dw_down
+
+
+def _want_linear_logp(hidden, table, targets, segment_ids, forks):
+    """(n_rows, vocab, width, number of forks), the checked operands, and the fork arrays as they are handed over."""
+    import torch
+    if hidden.dim() != 2 or table.dim() != 2:
+        raise ValueError("hidden: [rows, width], table: [vocab, width]")
+    (n_rows, D), V = hidden.shape, table.shape[0]
+    given = [("hidden", hidden, (n_rows, D), torch.bfloat16), ("table", table, (V, D), torch.bfloat16),
+             ("targets", targets, (n_rows,), torch.int32), ("segment_ids", segment_ids, (n_rows,), torch.int32)]
+    missing = [t is None for t in forks]
+    if any(missing) and not all(missing):
+        raise ValueError("fork_rows, fork_targets and fork_segments go together")
+    n_forks = 0 if missing[0] else forks[0].numel()
+    if n_forks:
+        given += [(name, t, (n_forks,), torch.int32) for name, t in zip(("fork_rows", "fork_targets", "fork_segments"), forks)]
+    else:
+        forks = (None, None, None)
+    return n_rows, V, D, n_forks, given, forks
+
+
+def dpo_linear_logp(hidden, table, targets, segment_ids, n_segments, fork_rows=None, fork_targets=None, fork_segments=None,
+                    scale=1.0, out=None, lse=None, workspace=None, status=None, stream=None):
+    """dpo_logp of the logits scale * hidden @ table.T, which are never stored: hidden [n_rows, width] and table [vocab, width]
+    bf16 (width a multiple of 8), labels as dpo_logp takes them.  Returns (out fp32 [n_segments], lse fp32 [n_rows]); lse is
+    what dpo_linear_logp_bwd needs: log sum exp of the logits of every row that scores a label, 0 of the others."""
+    import torch
+    n_rows, V, D, n_forks, given, forks = _want_linear_logp(hidden, table, targets, segment_ids,
+                                                           (fork_rows, fork_targets, fork_segments))
+    n_segments = int(n_segments)
+    _want_given(given)
+    _want_status_here(status)
+    _want_widths("dpo_linear_logp", D, n_forks, n_segments)
+    if n_segments < 0:
+        raise ValueError("n_segments: %d" % n_segments)
+    new = lambda n: _result(hidden, stream, lambda: torch.empty(n, dtype=torch.float32, device=hidden.device))  # noqa: E731
+    out, lse = new(n_segments) if out is None else out, new(n_rows) if lse is None else lse
+    outputs = [("out", out, (n_segments,), torch.float32), ("lse", lse, (n_rows,), torch.float32)]
+    _want_given(outputs)
+    _want_apart([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given])
+    lib = load_library()
+    need = lib.dpo_linear_logp_workspace_bytes(n_rows, n_forks, n_segments, V, D, 0)
+    workspace = _scratch(workspace, need, hidden, stream)
+    _check("dpo_linear_logp", lib.dpo_linear_logp(_ptr(hidden), _ptr(table), n_rows, V, D, float(scale), _ptr(targets), _ptr(segment_ids),
+                                                  *map(_ptr, forks), n_forks, n_segments, _ptr(out), _ptr(lse), _ptr(workspace),
+                                                  _ptr(status), _stream(stream)))
+    return out, lse
+
+
+def dpo_linear_logp_bwd(coef, hidden, table, lse, targets, segment_ids, fork_rows=None, fork_targets=None, fork_segments=None,
+                        scale=1.0, with_table=True, d_hidden=None, d_table=None, workspace=None, status=None, stream=None):
+    """Gradient of sum_g coef[g] * dpo_linear_logp(...)[0][g] for coef fp32 [n_segments]; lse as dpo_linear_logp returned it.
+    Returns (d_hidden [n_rows, width], d_table [vocab, width]), bf16; with_table=False leaves d_table out (None), for a table
+    that is not trained."""
+    import torch
+    n_rows, V, D, n_forks, given, forks = _want_linear_logp(hidden, table, targets, segment_ids,
+                                                           (fork_rows, fork_targets, fork_segments))
+    if coef.dim() != 1:
+        raise ValueError("coef: [n_segments]")
+    n_segments = coef.shape[0]
+    given += [("coef", coef, (n_segments,), torch.float32), ("lse", lse, (n_rows,), torch.float32)]
+    _want_given(given)
+    _want_status_here(status)
+    _want_widths("dpo_linear_logp_bwd", D, n_forks, n_segments)
+    d_hidden = _result(hidden, stream) if d_hidden is None else d_hidden
+    outputs = [("d_hidden", d_hidden, (n_rows, D), torch.bfloat16)]
+    if with_table:
+        d_table = _result(table, stream) if d_table is None else d_table
+        outputs.append(("d_table", d_table, (V, D), torch.bfloat16))
+    elif d_table is not None:
+        raise ValueError("d_table: not written with with_table=False")
+    _want_given(outputs)
+    _want_apart([(n, t) for n, t, _, _ in outputs], [(n, t) for n, t, _, _ in given])
+    lib = load_library()
+    need = lib.dpo_linear_logp_workspace_bytes(n_rows, n_forks, n_segments, V, D, 1)
+    workspace = _scratch(workspace, need, hidden, stream)
+    _check("dpo_linear_logp_bwd", lib.dpo_linear_logp_bwd(
+        _ptr(coef), _ptr(hidden), _ptr(table), _ptr(lse), n_rows, V, D, float(scale), _ptr(targets), _ptr(segment_ids), *map(_ptr, forks),
+        n_forks, n_segments, _ptr(d_hidden), _ptr(d_table), _ptr(workspace), _ptr(status), _stream(stream)))
+    return d_hidden, d_table
