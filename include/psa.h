@@ -361,6 +361,53 @@ psa_status_t psa_rope(const void* x, void* y, const int32_t* position_ids, int64
                       int32_t n_heads, int32_t head_dim, float rope_theta, void* stream);
 
 /*
+ * psa_rotary_frequencies -- the table of frequencies that psa_rotary takes, with its scaling for contexts longer than the
+ * original one.  With r = rotary_dim and f_i = theta^(-2i / r), i = 0 .. r / 2 - 1, in radians per position:
+ *     PSA_ROTARY_PLAIN       f_i
+ *     PSA_ROTARY_LINEAR      f_i / factor  (positions divided by factor)
+ *     PSA_ROTARY_BASE        theta' = theta * factor^(r / (r - 2)): the lowest frequency is divided by factor, the highest kept
+ *     PSA_ROTARY_WAVELENGTH  by n_i = original_length * f_i / (2 pi), a pair's turns over the original length:
+ *                            f_i from `high` turns on, f_i / factor up to `low`, between them by (n_i - low) / (high - low)
+ *     PSA_ROTARY_RAMP        the same weights along the pairs' numbers: from 1 at the pair (rounded down) that turns `high`
+ *                            times over the original length to 0 at the one (rounded up) that turns `low` times; the rotated
+ *                            part is to be multiplied by 0.1 log(factor) + 1
+ *   rotary_dim   even, at most 1024          theta   greater than 1
+ *   factor       at least 1 (not PLAIN);  original_length >= 1, 0 < low < high (WAVELENGTH and RAMP)
+ *   turns        host int64 [rotary_dim / 2] (out): turns per position, in units of 2^-64 turns
+ *   magnitude    host fp32 (out): 1, or the factor of RAMP
+ * Host only.  Errors: INVALID_ARG.
+ */
+#define PSA_ROTARY_PLAIN 0
+#define PSA_ROTARY_LINEAR 1
+#define PSA_ROTARY_BASE 2
+#define PSA_ROTARY_WAVELENGTH 3
+#define PSA_ROTARY_RAMP 4
+psa_status_t psa_rotary_frequencies(int32_t rotary_dim, double theta, int32_t scaling, double factor,
+                                    double original_length, double low, double high, int64_t* turns,
+                                    float* magnitude);
+
+/*
+ * psa_rotary -- rotary position embedding of the queries and keys of a layer in one launch, where psa_rope's one form does not
+ * do: pairs of neighbours, a part of the head, scaled frequencies, fp32, strided views.  Pair i of a head is
+ * (a, b) = (x[2i], x[2i + 1]) if interleaved, else (x[i], x[i + rotary_dim / 2]); with s = sin and c = cos of
+ * position * 2 pi * turns[i] 2^-64, exact for every position,
+ *     a' = magnitude * (a c - b s),   b' = magnitude * (b c + a s);
+ * elements from rotary_dim on are copied.  inverse != 0 takes -s: the gradient of the call without it.
+ *   q, q_out     device [n_tokens, n_q_heads, head_dim] of `dtype` (PSA_DTYPE_F32 or PSA_DTYPE_BF16); q_out may be q
+ *   k, k_out     the same with n_k_heads, which may be 0
+ *   position_ids device int32 [n_tokens], of either sign      turns  device int64 [rotary_dim / 2]
+ *   head_dim     at most 1024;  rotary_dim even and at most head_dim
+ *   strides      host int64 [8] or NULL (all contiguous), in elements: token and head stride of q, of q_out, of k, of k_out;
+ *                elements of a head are neighbours.  An output is its input, with the same strides, or lies apart from all others.
+ * Views of 16-byte alignment (and parts of a head that are multiples of it) move 16 bytes at a time, others fewer.
+ * Errors: INVALID_ARG, UNSUPPORTED (sizes), ALIGNMENT (of an element, of a pair if interleaved), CUDA.
+ */
+psa_status_t psa_rotary(const void* q, const void* k, void* q_out, void* k_out, const int32_t* position_ids,
+                        const int64_t* turns, int32_t dtype, int64_t n_tokens, int32_t n_q_heads, int32_t n_k_heads,
+                        int32_t head_dim, int32_t rotary_dim, const int64_t* strides, int32_t interleaved,
+                        int32_t inverse, float magnitude, void* stream);
+
+/*
  * psa_pack_ffd -- first-fit-decreasing packing of prefix-shared units into rows of a fixed
  * packing length (Section 3.2: the packing unit is the shared prompt with both responses;
  * Section 4.3.2: a first-fit-decreasing sampler, packing length = batch size x max unit length).
@@ -581,6 +628,51 @@ psa_status_t psa_norm_bwd(const void* d_out, const void* x, const void* weight, 
                           const void* d_total, int32_t dtype, int32_t weight_dtype, int64_t n_tokens,
                           int32_t hidden, int32_t rms, void* dx, void* dweight, void* dbias,
                           void* workspace, int32_t* device_status, void* stream);
+
+/*
+ * psa_block_norm -- the step between two sublayers whose output is normalised before it joins the residual stream, or scaled by
+ * a gate, or both (psa_norm with a residual is the form without either).  Per row, in fp32:
+ *     y = norm(x) * post_weight + post_bias     (y = x where post_weight is NULL)
+ *     s = residual_scale * residual + gate * y, rounded to x's type     (gate = 1 where it is NULL)
+ *     out = norm(s) * weight + bias,            norm(v) = (v - m) * r, m and r as by psa_norm
+ *   x, residual  device [n_tokens, hidden] of `dtype`: the sublayer's output and the residual stream
+ *   weight, bias, post_weight, post_bias, gate   device [hidden] of `weight_dtype`; all but weight may be NULL; biases are
+ *                NULL if rms, and post_bias without post_weight
+ *   dtype, weight_dtype, hidden, rms             as for psa_norm
+ *   out          device [n_tokens, hidden] of `dtype` (out);  may be x or residual
+ *   total        device [n_tokens, hidden] of `dtype` (out): s;  may be x or residual, not out
+ *   stats        device fp32 [4, n_tokens] (out): m and r of every x (0 and 1 without post_weight), then of every s
+ * Rows that are not finite give what psa_norm gives for them; no other row changes.  n_tokens = 0 is a no-op.
+ * Errors: INVALID_ARG, UNSUPPORTED (hidden, n_tokens >= 2^31), ALIGNMENT (16 bytes), CUDA.
+ */
+psa_status_t psa_block_norm(const void* x, const void* residual, const void* weight, const void* bias,
+                            const void* post_weight, const void* post_bias, const void* gate, float residual_scale,
+                            int32_t dtype, int32_t weight_dtype, int64_t n_tokens, int32_t hidden, float eps,
+                            int32_t rms, void* out, void* total, float* stats, void* stream);
+
+/*
+ * psa_block_norm_bwd -- gradient of psa_block_norm.  With u1, u2 the normalised rows of x and s, and g = d_out * weight:
+ *     ds = r2 * (g - u2 * mean(g * u2) - mean(g)) + d_total,     d_residual = residual_scale * ds
+ *     q = ds * gate * post_weight,   dx = r1 * (q - u1 * mean(q * u1) - mean(q))     (dx = ds * gate without post_weight)
+ *     d_weight = sum d_out * u2,   d_bias = sum d_out,   d_post_weight = gate * sum ds * u1,   d_post_bias = gate * sum ds,
+ *     d_gate = sum ds * y   over the tokens;   the means of g and q are left out if rms
+ *   d_out, x, total, stats   as psa_block_norm took and wrote them;  d_total  device or NULL, as for psa_norm_bwd
+ *   dx, d_residual   device [n_tokens, hidden] of `dtype` (out); each may be d_out, total or d_total, dx may be x
+ *   d_weight, d_bias, d_post_weight, d_post_bias, d_gate   device [hidden] of `weight_dtype` (out); d_bias and d_post_bias may be
+ *                NULL; d_post_weight and d_gate are given where their parameter is
+ *   workspace    device scratch of psa_block_norm_bwd_workspace_bytes() bytes, 16-byte aligned
+ *   device_status  device int32 or NULL; PSA_DEVSTAT_WAIT_EXPIRED is ORed in as by psa_fwd
+ * The sums over tokens are taken in an order that depends on the sizes alone.  n_tokens = 0 writes zeros to the parameters' gradients.
+ * Errors: as psa_block_norm.
+ */
+size_t psa_block_norm_bwd_workspace_bytes(int64_t n_tokens, int32_t hidden);
+psa_status_t psa_block_norm_bwd(const void* d_out, const void* x, const void* total, const void* weight,
+                                const void* post_weight, const void* post_bias, const void* gate,
+                                float residual_scale, const float* stats, const void* d_total, int32_t dtype,
+                                int32_t weight_dtype, int64_t n_tokens, int32_t hidden, int32_t rms, void* dx,
+                                void* d_residual, void* d_weight, void* d_bias, void* d_post_weight,
+                                void* d_post_bias, void* d_gate, void* workspace, int32_t* device_status,
+                                void* stream);
 
 /*
  * psa_embed -- token embedding: out[t] = scale * table[token_ids[t]]  (the paper has no counterpart).

@@ -649,3 +649,80 @@ def linear_logp_grad(hidden, table, targets, segment_ids, coef, fork_rows=(), fo
 def _labels(n_rows, vocab, n_segments, targets, segment_ids, fork_rows, fork_targets, fork_segments):
     every = [(t, targets[t], segment_ids[t]) for t in range(n_rows)] + list(zip(fork_rows, fork_targets, fork_segments))
     return [(int(t), int(y), int(g)) for t, y, g in every if 0 <= t < n_rows and 0 <= y < vocab and 0 <= g < n_segments]
+
+
+# ------------------------------------------------------------------ rotary positions in their various forms
+def rotary_frequencies(rotary_dim, theta=10000.0, scaling=None, factor=1.0, original_length=0, low=1.0, high=None):
+    """(radians per position of every pair, magnitude of the rotated part) under a scaling for long contexts: positions divided
+    by factor ("linear"), the base raised so that the slowest pair is slowed by factor ("base"), or frequencies slowed by factor for
+    pairs that turn seldom over the original length, between `low` and `high` times: by that number ("wavelength"), or by the pair's
+    place between the pairs that turn so often ("ramp")."""
+    r, n = rotary_dim, rotary_dim // 2
+    high = (32.0 if scaling == "ramp" else 4.0) if high is None else high
+    freq, magnitude = [], 1.0
+    if scaling == "base":
+        theta = theta * factor ** (r / (r - 2))
+    if scaling == "ramp":
+        magnitude = 0.1 * np.log(factor) + 1
+        pair = lambda times: r * np.log(original_length / (times * 2 * np.pi)) / (2 * np.log(theta))  # noqa: E731
+        first, last = max(np.floor(pair(high)), 0), min(np.ceil(pair(low)), r - 1)
+    for i in range(n):
+        f = theta ** (-2 * i / r)
+        if scaling == "linear":
+            f = f / factor
+        elif scaling == "wavelength":
+            times = original_length / (2 * np.pi / f)
+            if times < low:
+                f = f / factor
+            elif times <= high:
+                share = (times - low) / (high - low)
+                f = share * f + (1 - share) * f / factor
+        elif scaling == "ramp":
+            share = 1 - min(max((i - first) / max(last - first, 0.001), 0), 1)
+            f = share * f + (1 - share) * f / factor
+        freq.append(f)
+    return np.array(freq), magnitude
+
+
+def rotary(x, pos, radians, magnitude=1.0, interleaved=False, inverse=False):
+    """x [T, H, d] with the first 2 * len(radians) elements of a head turned in pairs, written as a product of complex numbers."""
+    x, n = _as_f64(x).copy(), len(radians)
+    first, second = (slice(0, 2 * n, 2), slice(1, 2 * n, 2)) if interleaved else (slice(0, n), slice(n, 2 * n))
+    angle = np.asarray(pos, dtype=np.float64)[:, None] * radians
+    z = (x[..., first] + 1j * x[..., second]) * (magnitude * np.exp((-1j if inverse else 1j) * angle))[:, None, :]
+    x[..., first], x[..., second] = z.real, z.imag
+    return x
+
+
+# ------------------------------------------------------------------ norms before and after a block
+def block_norm_fwd(x, residual, weight, bias=None, post_weight=None, post_bias=None, gate=None, residual_scale=1.0, eps=1e-5,
+                   rms=False, rounded=lambda a: a):
+    """(out, total, stats [4, T]): a sublayer's output normalised, gated and added to the residual stream, and that normalised;
+    `rounded` is what the type of the stream makes of it."""
+    x = _as_f64(x)
+    y, m1, r1 = x, np.zeros(len(x)), np.ones(len(x))
+    if post_weight is not None:
+        y, m1, r1 = norm_fwd(x, post_weight, post_bias, eps, rms)
+    if gate is not None:
+        y = y * _as_f64(gate)
+    total = rounded(residual_scale * _as_f64(residual) + y)
+    out, m2, r2 = norm_fwd(total, weight, bias, eps, rms)
+    return out, total, np.stack([m1, r1, m2, r2])
+
+
+def block_norm_bwd(d_out, x, total, weight, post_weight=None, post_bias=None, gate=None, residual_scale=1.0, eps=1e-5, rms=False,
+                   d_total=None):
+    """Gradients of sum(out * d_out) + sum(total * d_total): a dict with x, residual, weight, bias, post_weight, post_bias, gate."""
+    g = {}
+    ds, g["weight"], g["bias"] = norm_bwd(d_out, total, weight, eps, rms)
+    ds = ds if d_total is None else ds + _as_f64(d_total)
+    g["residual"] = residual_scale * ds
+    dy = ds if gate is None else ds * _as_f64(gate)
+    y = _as_f64(x)
+    if post_weight is not None:
+        y = norm_fwd(x, post_weight, post_bias, eps, rms)[0]
+        g["x"], g["post_weight"], g["post_bias"] = norm_bwd(dy, x, post_weight, eps, rms)
+    else:
+        g["x"] = dy
+    g["gate"] = (ds * y).sum(0)
+    return g
