@@ -10,7 +10,9 @@ route that takes 4 to 9 us less of the host: psa_plan, psa_fwd and the losses
 without stream=, psa_bwd and psa_bwd_f32 without stream= and with workspace=,
 dpo_logp without stream=, out= and scratch=, dpo_logp_bwd without stream= and
 with dlogits=, psa_rope without stream= and with out=, the normalisation, the
-embedding and the feed-forward block without stream= and outputs of their own.
+embedding, the feed-forward block, psa_rotary, the norms around a block and
+the log-probabilities from hidden states without stream= and outputs of their
+own.
 Results and refusals are the same.
 
 A call with stream= runs on that stream, and what it allocates belongs to it;
@@ -140,7 +142,9 @@ _native_tried = False
 _NATIVE_ENTRIES = ("psa_fwd", "psa_bwd", "psa_bwd_f32", "dpo_logp_f64sum", "dpo_logp_bwd", "dpo_loss", "simpo_loss",
                    "orpo_loss", "psa_rope", "psa_plan", "psa_plan_stats", "psa_plan_destroy", "psa_norm", "psa_norm_bwd",
                    "psa_norm_bwd_workspace_bytes", "psa_embed", "psa_embed_bwd", "psa_embed_bwd_workspace_bytes", "psa_ffn",
-                   "psa_ffn_bwd", "psa_ffn_workspace_bytes")
+                   "psa_ffn_bwd", "psa_ffn_workspace_bytes", "psa_rotary", "psa_block_norm", "psa_block_norm_bwd",
+                   "psa_block_norm_bwd_workspace_bytes", "dpo_linear_logp", "dpo_linear_logp_bwd",
+                   "dpo_linear_logp_workspace_bytes")
 
 
 def _load_native():
@@ -1085,6 +1089,14 @@ def dpo_linear_logp(hidden, table, targets, segment_ids, n_segments, fork_rows=N
     """dpo_logp of the logits scale * hidden @ table.T, which are never stored: hidden [n_rows, width] and table [vocab, width]
     bf16 (width a multiple of 8), labels as dpo_logp takes them.  Returns (out fp32 [n_segments], lse fp32 [n_rows]); lse is
     what dpo_linear_logp_bwd needs: log sum exp of the logits of every row that scores a label, 0 of the others."""
+    fast = _fast(stream) if out is None and lse is None else None
+    if fast:
+        got = fast.linear_logp(hidden, table, targets, segment_ids, fork_rows, fork_targets, fork_segments, n_segments, float(scale),
+                               workspace, status)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            _check("dpo_linear_logp", got)
     import torch
     n_rows, V, D, n_forks, given, forks = _want_linear_logp(hidden, table, targets, segment_ids,
                                                            (fork_rows, fork_targets, fork_segments))
@@ -1113,6 +1125,14 @@ def dpo_linear_logp_bwd(coef, hidden, table, lse, targets, segment_ids, fork_row
     """Gradient of sum_g coef[g] * dpo_linear_logp(...)[0][g] for coef fp32 [n_segments]; lse as dpo_linear_logp returned it.
     Returns (d_hidden [n_rows, width], d_table [vocab, width]), bf16; with_table=False leaves d_table out (None), for a table
     that is not trained."""
+    fast = _fast(stream) if d_hidden is None and d_table is None else None
+    if fast:
+        got = fast.linear_logp_bwd(coef, hidden, table, lse, targets, segment_ids, fork_rows, fork_targets, fork_segments, float(scale),
+                                   with_table, workspace, status)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            _check("dpo_linear_logp_bwd", got)
     import torch
     n_rows, V, D, n_forks, given, forks = _want_linear_logp(hidden, table, targets, segment_ids,
                                                            (fork_rows, fork_targets, fork_segments))
@@ -1204,6 +1224,13 @@ def psa_rotary(q, k, position_ids, turns, magnitude=1.0, interleaved=False, inve
     stride.  turns, magnitude: as psa_rotary_frequencies gave them (turns on the device; its length says how much of a head
     is turned); position_ids int32 [T].  interleaved: pairs are neighbours, else halves of the rotated part.  inverse=True is the
     gradient of the call without it.  Returns (q_out, k_out), contiguous unless given; q_out may be q, k_out may be k."""
+    fast = _fast(stream) if q_out is None and k_out is None else None
+    if fast:
+        got = fast.rotary(q, k, position_ids, turns, float(magnitude), interleaved, inverse)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            _check("psa_rotary", got)
     import torch
     if q.dim() != 3 or (k is not None and k.dim() != 3) or turns.dim() != 1:
         raise ValueError("q, k: [tokens, heads, head_dim], turns: [rotary_dim / 2]")
@@ -1279,6 +1306,13 @@ def psa_block_norm(x, residual, weight, bias=None, post_weight=None, post_bias=N
     with what is None left out; layer norms, or with rms=True the root-mean-square form (without biases).  x in bf16 or fp32,
     parameters in x's type or fp32.  Returns (out, total, stats); stats, fp32 [4, T], is what psa_block_norm_bwd needs.  out and
     total may be x or residual."""
+    fast = _fast(stream) if out is None and total is None and stats is None else None
+    if fast:
+        got = fast.block_norm(x, residual, weight, bias, post_weight, post_bias, gate, float(residual_scale), float(eps), rms)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            _check("psa_block_norm", got)
     import torch
     T, D, dtype, wtype, params = _want_block(x, weight, bias, post_weight, post_bias, gate, rms)
     given = [("x", x, (T, D), x.dtype), ("residual", residual, (T, D), x.dtype)] + params
@@ -1302,6 +1336,14 @@ def psa_block_norm_bwd(d_out, x, total, weight, stats, post_weight=None, post_bi
     """Gradient of psa_block_norm for d_out and, if given, d_total, the gradient that reaches the sum by the residual stream.
     Returns (dx, d_residual, d_weight, d_bias, d_post_weight, d_post_bias, d_gate), None for parameters that the forward pass
     had not (d_bias: unless with_bias).  dx and d_residual may be d_out, total or d_total, dx may be x."""
+    fast = _fast(stream) if dx is None and d_residual is None else None
+    if fast:
+        got = fast.block_norm_bwd(d_out, x, total, weight, None, post_weight, post_bias, gate, stats, float(residual_scale), rms, d_total,
+                                  with_bias, workspace, status)
+        if type(got) is tuple:
+            return got
+        if got is not None:
+            _check("psa_block_norm_bwd", got)
     import torch
     T, D, dtype, wtype, params = _want_block(x, weight, None, post_weight, post_bias, gate, rms)
     if rms and with_bias:

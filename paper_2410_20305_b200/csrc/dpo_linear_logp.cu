@@ -150,10 +150,13 @@ logp_list_kernel(const int32_t* targets, const int32_t* segment_ids, const int32
 __host__ __device__ constexpr int64_t padded(int64_t n) { return (n + 255) / 256 * 256; }
 
 // The hidden rows of the labels side by side, zeros behind the last one to the next multiple of 256 (and in the first 256 where
-// there is no label), and for the backward pass what a label's row of dz takes: coef * scale and lse in units of log 2.
+// there is no label).  For the backward pass what a label's row of dz takes: coef * scale and lse in units of log 2.  For the
+// forward the label's own product, by fp32 additions that round: tcgen05's cut off, which makes a logit smaller by about width * 1e-9
+// of itself (4.2e-6 at 4096, the same for all), and a log-probability near 0 is the difference of two such numbers (1.5e-4 of it at
+// width 4096 where the logit of 6 was taken from TMEM).
 __global__ void __launch_bounds__(256)
-logp_gather_kernel(const uint4* hidden, Labels labels, int32_t vectors, uint4* rows, const float* coef, const float* lse, float scale,
-                   float2* of_label) {
+logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32_t vectors, uint4* rows, const float* coef, const float* lse,
+                   float scale, float2* of_label, float* label_logit) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t i = int64_t(blockIdx.x) * 8 + warp;
   behind_wait();
@@ -168,8 +171,28 @@ logp_gather_kernel(const uint4* hidden, Labels labels, int32_t vectors, uint4* r
   const int32_t t = labels.row[i];
   if (of_label && lane == 0) of_label[i] = make_float2(coef[labels.segment[i]] * scale, lse[t] * kLog2e);
   const uint4* from = hidden + int64_t(t) * vectors;
+  if (!label_logit) {
 #pragma unroll 4
-  for (int c = lane; c < vectors; c += 32) to[c] = from[c];
+    for (int c = lane; c < vectors; c += 32) to[c] = from[c];
+    return;
+  }
+  const uint4* weight = table + int64_t(labels.target[i]) * vectors;
+  float sum[8] = {};
+#pragma unroll 4
+  for (int c = lane; c < vectors; c += 32) {
+    const uint4 h = from[c], w = weight[c];
+    to[c] = h;
+    const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      sum[2 * j] = fmaf(__uint_as_float(hw[j] << 16), __uint_as_float(ww[j] << 16), sum[2 * j]);
+      sum[2 * j + 1] = fmaf(__uint_as_float(hw[j] & 0xffff0000u), __uint_as_float(ww[j] & 0xffff0000u), sum[2 * j + 1]);
+    }
+  }
+  float all = ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+#pragma unroll
+  for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+  if (lane == 0) label_logit[i] = all;
 }
 
 // ---------------------------------------------------------------- products
@@ -525,7 +548,7 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
 // sums and writes lse; the last CTA turns the sums into out.
 constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(32 * kJoinWarps)
-logp_join_kernel(const float2* stats, const float* picked, Labels labels, int64_t l_pad, int32_t v_tiles, int32_t n_rows,
+logp_join_kernel(const float2* stats, const float* picked, const float* label_logit, Labels labels, int64_t l_pad, int32_t v_tiles, int32_t n_rows,
                  int32_t n_segments, float scale_log2, Sum* sums, float* out, float* lse) {
   __shared__ float2 s_part[kJoinWarps][32];
   __shared__ bool s_last;
@@ -563,10 +586,13 @@ logp_join_kernel(const float2* stats, const float* picked, Labels labels, int64_
     if (warp == 0 && i < n) {
       for (int k = 1; k < kJoinWarps; ++k) merge(s_part[k][lane]);
       const int32_t t = labels.row[i];
-      // the maximum is taken off before anything is rounded to fp32: the term of a token that takes nearly all of the
-      // probability is near 0 itself, not the difference of two numbers like 50
-      const double log2s = log2f(s);
-      add_term(sums + labels.segment[i], (fma(double(picked[i]), double(scale_log2), -double(m)) - log2s) * kLn2);
+      // The label's logit as its own product in the place of the one from the tiles.  The maximum is taken off before anything is
+      // rounded to fp32: the term of a token that takes nearly all of the probability is near 0 itself, not the difference of two
+      // numbers like 50.
+      const double label = fma(double(label_logit[i]), double(scale_log2), -double(m));
+      const double summed = fma(double(picked[i]), double(scale_log2), -double(m));
+      const double corrected = double(s) + (exp2(label) - exp2(summed)), log2s = corrected < exp2(label) ? label : log2(corrected);
+      add_term(sums + labels.segment[i], (label - log2s) * kLn2);
       // a row that several labels score has it from its own one, or else from the first fork
       const int32_t state = labels.state[t];
       bool writes = (state >> 1) == i + 1;
@@ -630,7 +656,7 @@ struct Workspace {
   int64_t l_pad;
   int64_t piece;                 // columns of a piece of the vocabulary
   int32_t splits;
-  size_t row, target, segment, state, sums, rows, stats, picked, of_label, dz, parts, total;
+  size_t row, target, segment, state, sums, rows, stats, picked, label_logit, of_label, dz, parts, total;
   Workspace(int64_t n_rows, int64_t n_forks, int64_t n_segments, int64_t vocab, int64_t hidden, bool backward) {
     l_pad = std::max<int64_t>(256, padded(n_rows + n_forks));
     const int64_t most = std::max<int64_t>(256, kPieceBytes / (2 * l_pad) / 256 * 256), pieces = (vocab + most - 1) / most;
@@ -645,7 +671,7 @@ struct Workspace {
     segment = take(l_pad * 4);
     state = take(n_rows * 4);
     rows = take(l_pad * hidden * 2);
-    sums = stats = picked = of_label = dz = parts = 0;
+    sums = stats = picked = label_logit = of_label = dz = parts = 0;
     if (backward) {
       of_label = take(l_pad * sizeof(float2));
       dz = take(l_pad * piece * 2);
@@ -654,6 +680,7 @@ struct Workspace {
       sums = take(n_segments * sizeof(Sum));
       stats = take(size_t((vocab + kTile - 1) / kTile) * l_pad * sizeof(float2));
       picked = take(l_pad * 4);
+      label_logit = take(l_pad * 4);
     }
     total = at;
   }
@@ -702,9 +729,10 @@ bool launch_labels(const Call& c, const Workspace& w, bool backward, const float
                     c.fork_segments, int32_t(c.n_rows), c.n_forks, c.n_segments, int32_t(c.vocab), labels,
                     backward ? nullptr : reinterpret_cast<Sum*>(c.ws + w.sums), c.status) != cudaSuccess)
     return false;
-  return launch_behind(true, logp_gather_kernel, dim3(unsigned(w.l_pad / 8)), 256, 0, c.stream, static_cast<const uint4*>(c.hidden), labels,
-                       c.width / 8, reinterpret_cast<uint4*>(c.ws + w.rows), coef, lse, c.scale,
-                       backward ? reinterpret_cast<float2*>(c.ws + w.of_label) : nullptr) == cudaSuccess;
+  return launch_behind(true, logp_gather_kernel, dim3(unsigned(w.l_pad / 8)), 256, 0, c.stream, static_cast<const uint4*>(c.hidden),
+                       static_cast<const uint4*>(c.table), labels, c.width / 8, reinterpret_cast<uint4*>(c.ws + w.rows), coef, lse, c.scale,
+                       backward ? reinterpret_cast<float2*>(c.ws + w.of_label) : nullptr,
+                       backward ? nullptr : reinterpret_cast<float*>(c.ws + w.label_logit)) == cudaSuccess;
 }
 
 template <int EPI>
@@ -745,7 +773,8 @@ psa_status_t forward(const Call& c, float* out, float* lse) {
     return PSA_ERR_CUDA;
   const int64_t v_tiles = (c.vocab + kTile - 1) / kTile;
   if (!launch_product<kEpiStats>(a, w.l_pad / kTile * v_tiles, c.stream)) return failed_launch("dpo_linear_logp product");
-  launch_behind(true, logp_join_kernel, dim3(unsigned(w.l_pad / 32)), 32 * kJoinWarps, 0, c.stream, a.stats, a.picked, w.labels(c.ws), w.l_pad,
+  launch_behind(true, logp_join_kernel, dim3(unsigned(w.l_pad / 32)), 32 * kJoinWarps, 0, c.stream, a.stats, a.picked,
+                reinterpret_cast<const float*>(c.ws + w.label_logit), w.labels(c.ws), w.l_pad,
                 int32_t(v_tiles), int32_t(c.n_rows), c.n_segments, a.scale_log2, reinterpret_cast<Sum*>(c.ws + w.sums), out, lse);
   return check_last_cuda_error("dpo_linear_logp launch");
 }

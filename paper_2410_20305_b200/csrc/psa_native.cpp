@@ -34,6 +34,13 @@ struct Entry {   // in the order of binding.py's _NATIVE_ENTRIES
   decltype(&::psa_ffn) ffn;
   decltype(&::psa_ffn_bwd) ffn_bwd;
   decltype(&::psa_ffn_workspace_bytes) ffn_bytes;
+  decltype(&::psa_rotary) rotary;
+  decltype(&::psa_block_norm) block_norm;
+  decltype(&::psa_block_norm_bwd) block_norm_bwd;
+  decltype(&::psa_block_norm_bwd_workspace_bytes) block_norm_bwd_bytes;
+  decltype(&::dpo_linear_logp) linear_logp;
+  decltype(&::dpo_linear_logp_bwd) linear_logp_bwd;
+  decltype(&::dpo_linear_logp_workspace_bytes) linear_logp_bytes;
 } g_lib;
 bool g_ready = false;
 
@@ -605,10 +612,222 @@ PyObject* ffn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// A [tokens, heads, head_dim] view whose heads' elements are neighbours.
+const at::Tensor* take_heads(PyObject* o) {
+  const at::Tensor* t = plain(o);
+  return t && t->dim() == 3 && here(*t) && (t->stride(2) == 1 || t->size(2) <= 1) && t->size(1) <= INT32_MAX && t->size(2) <= INT32_MAX
+             ? t
+             : nullptr;
+}
+
+// rotary(q, k, position_ids, turns, magnitude, interleaved, inverse) -> (q_out, k_out), a status code (not 0), or None
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    float magnitude;
+    bool interleaved, inverse;
+    int32_t dtype;
+    if (n != 7 || !modes_off() || !take_float(a[4], &magnitude) || !take_bool(a[5], &interleaved) || !take_bool(a[6], &inverse)) return none();
+    const at::Tensor *q = take_heads(a[0]), *k = a[1] == Py_None ? nullptr : take_heads(a[1]), *turns = plain(a[3]);
+    if (!q || !take_dtype(*q, &dtype) || !turns || turns->dim() != 1 || turns->scalar_type() != at::kLong || !turns->is_contiguous() ||
+        !here(*turns))
+      return none();
+    const int64_t T = q->size(0), Hq = q->size(1), d = q->size(2), Hk = k ? k->size(1) : 0, r = 2 * turns->size(0);
+    const at::Tensor* pos = take_here(a[2], at::kInt, {T});
+    if (!pos || r > d || (a[1] != Py_None && (!k || k->scalar_type() != q->scalar_type() || k->size(0) != T || k->size(2) != d))) return none();
+    at::Tensor qo = make({T, Hq, d}, q->scalar_type(), *q), ko;
+    if (k) ko = make({T, Hk, d}, q->scalar_type(), *q);
+    const int64_t strides[8] = {q->stride(0), q->stride(1), Hq * d, d, k ? k->stride(0) : 0, k ? k->stride(1) : 0, Hk * d, d};
+    void *const from = q->data_ptr(), *const to = qo.data_ptr(), *const kf = k ? k->data_ptr() : nullptr,
+         *const kt = k ? ko.data_ptr() : nullptr, *const on = stream();
+    const int32_t* const at = static_cast<const int32_t*>(pos->data_ptr());
+    const int64_t* const table = static_cast<const int64_t*>(turns->data_ptr());
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.rotary(from, kf, to, kt, at, table, dtype, T, int32_t(Hq), int32_t(Hk), int32_t(d), int32_t(r), strides, interleaved,
+                          inverse, magnitude, on);
+    });
+    if (rc != PSA_OK) return PyLong_FromLong(rc);
+    return k ? tuple_of(qo, ko) : Py_BuildValue("(NO)", THPVariable_Wrap(qo), Py_None);
+  });
+}
+
+// The parameters of a block's norms: weight, bias, post_weight, post_bias, gate.
+struct BlockArgs {
+  NormArgs m;
+  void *weight, *p[4];
+  float scale;
+  bool rms;
+};
+bool take_block(PyObject* x, PyObject* const* params, PyObject* scale, PyObject* rms, BlockArgs* b) {
+  if (!take_norm(x, params[0], &b->m) || !take_float(scale, &b->scale) || !take_bool(rms, &b->rms)) return false;
+  b->weight = b->m.weight->data_ptr();
+  for (int i = 0; i < 4; ++i)
+    if (!take_optional(params[1 + i], b->m.weight->scalar_type(), {b->m.hidden}, &b->p[i])) return false;
+  const bool bias = params[1] != Py_None, post = params[2] != Py_None, post_bias = params[3] != Py_None;
+  return !(b->rms && (bias || post_bias)) && !(post_bias && !post) && !(b->m.dtype == PSA_DTYPE_F32 && b->m.wtype != PSA_DTYPE_F32);
+}
+
+// block_norm(x, residual, weight, bias, post_weight, post_bias, gate, residual_scale, eps, rms) -> (out, total, stats), a status code
+// (not 0), or None
+PyObject* block_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    BlockArgs b;
+    float eps;
+    void* res;
+    if (n != 10 || !modes_off() || !take_block(a[0], a + 2, a[7], a[9], &b) || !take_float(a[8], &eps) || a[1] == Py_None ||
+        !take_optional(a[1], b.m.x->scalar_type(), {b.m.T, b.m.hidden}, &res))
+      return none();
+    const NormArgs& m = b.m;
+    at::Tensor out = make({m.T, m.hidden}, m.x->scalar_type(), *m.x), total = make({m.T, m.hidden}, m.x->scalar_type(), *m.x),
+               stats = make({4, m.T}, at::kFloat, *m.x);
+    void *const x = m.x->data_ptr(), *const to = out.data_ptr(), *const sum = total.data_ptr(), *const on = stream();
+    float* const st = stats.data_ptr<float>();
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.block_norm(x, res, b.weight, b.p[0], b.p[1], b.p[2], b.p[3], b.scale, m.dtype, m.wtype, m.T, int32_t(m.hidden), eps, b.rms,
+                              to, sum, st, on);
+    });
+    return rc != PSA_OK ? PyLong_FromLong(rc) : tuple_of(out, total, stats);
+  });
+}
+
+// block_norm_bwd(d_out, x, total, weight, None, post_weight, post_bias, gate, stats, residual_scale, rms, d_total, with_bias, workspace,
+// status) -> (dx, d_residual, d_weight, d_bias, d_post_weight, d_post_bias, d_gate), None for those that there are not, a status
+// code (not 0), or None
+PyObject* block_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    BlockArgs b;
+    bool with_bias;
+    void *d_out, *total, *stats, *d_total, *word;
+    at::Tensor ws;
+    if (n != 15 || !modes_off() || !take_block(a[1], a + 3, a[9], a[10], &b) || !take_bool(a[12], &with_bias) || (b.rms && with_bias) ||
+        !take_status_here(a[14], &word))
+      return none();
+    const NormArgs& m = b.m;
+    const auto type = m.x->scalar_type();
+    for (int i : {0, 2, 8})
+      if (a[i] == Py_None) return none();
+    if (!take_optional(a[0], type, {m.T, m.hidden}, &d_out) || !take_optional(a[2], type, {m.T, m.hidden}, &total) ||
+        !take_optional(a[8], at::kFloat, {4, m.T}, &stats) || !take_optional(a[11], type, {m.T, m.hidden}, &d_total) ||
+        !take_workspace(a[13], g_lib.block_norm_bwd_bytes(m.T, int32_t(m.hidden)), *m.x, &ws))
+      return none();
+    at::Tensor dx = make({m.T, m.hidden}, type, *m.x), dr = make({m.T, m.hidden}, type, *m.x), grads[5];
+    const bool wanted[5] = {true, with_bias, a[5] != Py_None, a[6] != Py_None, a[7] != Py_None};
+    void* to[5];
+    for (int i = 0; i < 5; ++i) {
+      if (wanted[i]) grads[i] = make({m.hidden}, m.weight->scalar_type(), *m.x);
+      to[i] = wanted[i] ? grads[i].data_ptr() : nullptr;
+    }
+    void *const x = m.x->data_ptr(), *const tx = dx.data_ptr(), *const tr = dr.data_ptr(), *const scratch = ws.data_ptr(), *const on = stream();
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.block_norm_bwd(d_out, x, total, b.weight, b.p[1], b.p[2], b.p[3], b.scale, static_cast<float*>(stats), d_total, m.dtype,
+                                  m.wtype, m.T, int32_t(m.hidden), b.rms, tx, tr, to[0], to[1], to[2], to[3], to[4], scratch,
+                                  static_cast<int32_t*>(word), on);
+    });
+    if (rc != PSA_OK) return PyLong_FromLong(rc);
+    PyObject* all = PyTuple_New(7);
+    if (!all) return nullptr;
+    PyTuple_SET_ITEM(all, 0, THPVariable_Wrap(dx));
+    PyTuple_SET_ITEM(all, 1, THPVariable_Wrap(dr));
+    for (int i = 0; i < 5; ++i) PyTuple_SET_ITEM(all, 2 + i, wanted[i] ? THPVariable_Wrap(grads[i]) : none());
+    return all;
+  });
+}
+
+// hidden, table and the labels of log-probabilities from hidden states.
+struct LinearArgs {
+  const at::Tensor *hidden, *table;
+  int64_t rows, vocab, width, n_forks;
+  void *h, *w, *targets, *segments, *forks[3];
+};
+bool take_linear(PyObject* hidden, PyObject* table, PyObject* const* labels, LinearArgs* l) {
+  l->hidden = plain(hidden);
+  l->table = plain(table);
+  if (!l->hidden || !l->table || l->hidden->dim() != 2 || l->table->dim() != 2) return false;
+  l->rows = l->hidden->size(0);
+  l->width = l->hidden->size(1);
+  l->vocab = l->table->size(0);
+  l->n_forks = 0;
+  const auto b = at::kBFloat16;
+  if (!take_optional(hidden, b, {l->rows, l->width}, &l->h) || !take_optional(table, b, {l->vocab, l->width}, &l->w) ||
+      labels[0] == Py_None || labels[1] == Py_None || !take_optional(labels[0], at::kInt, {l->rows}, &l->targets) ||
+      !take_optional(labels[1], at::kInt, {l->rows}, &l->segments) || l->width > INT32_MAX)
+    return false;
+  if (labels[2] != Py_None) {
+    const at::Tensor* f = plain(labels[2]);
+    if (!f || f->dim() != 1 || f->size(0) > INT32_MAX || labels[3] == Py_None || labels[4] == Py_None) return false;
+    l->n_forks = f->size(0);
+  }
+  for (int i = 0; i < 3; ++i) {
+    if ((labels[2 + i] == Py_None) != (labels[2] == Py_None) || !take_optional(labels[2 + i], at::kInt, {l->n_forks}, &l->forks[i])) return false;
+    if (l->n_forks == 0) l->forks[i] = nullptr;
+  }
+  return true;
+}
+
+// linear_logp(hidden, table, targets, segment_ids, fork_rows, fork_targets, fork_segments, n_segments, scale, workspace, status) ->
+// (out, lse), a status code (not 0), or None
+PyObject* linear_logp(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    LinearArgs l;
+    int64_t segments;
+    float scale;
+    void* word;
+    at::Tensor ws;
+    if (n != 11 || !modes_off() || !take_linear(a[0], a[1], a + 2, &l) || !take_int(a[7], &segments) || segments < 0 || segments > INT32_MAX ||
+        !take_float(a[8], &scale) || !take_status_here(a[10], &word))
+      return none();
+    const size_t bytes = g_lib.linear_logp_bytes(l.rows, int32_t(l.n_forks), int32_t(segments), l.vocab, int32_t(l.width), 0);
+    if (bytes == 0 || !take_workspace(a[9], bytes, *l.hidden, &ws)) return none();
+    at::Tensor out = make({segments}, at::kFloat, *l.hidden), lse = make({l.rows}, at::kFloat, *l.hidden);
+    float *const to = out.data_ptr<float>(), *const tl = lse.data_ptr<float>();
+    void *const scratch = ws.data_ptr(), *const on = stream();
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.linear_logp(l.h, l.w, l.rows, l.vocab, int32_t(l.width), scale, static_cast<int32_t*>(l.targets),
+                               static_cast<int32_t*>(l.segments), static_cast<int32_t*>(l.forks[0]), static_cast<int32_t*>(l.forks[1]),
+                               static_cast<int32_t*>(l.forks[2]), int32_t(l.n_forks), int32_t(segments), to, tl, scratch,
+                               static_cast<int32_t*>(word), on);
+    });
+    return rc != PSA_OK ? PyLong_FromLong(rc) : tuple_of(out, lse);
+  });
+}
+
+// linear_logp_bwd(coef, hidden, table, lse, targets, segment_ids, fork_rows, fork_targets, fork_segments, scale, with_table, workspace,
+// status) -> (d_hidden, d_table or None), a status code (not 0), or None
+PyObject* linear_logp_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    LinearArgs l;
+    float scale;
+    bool with_table;
+    void *coef, *lse, *word;
+    at::Tensor ws;
+    if (n != 13 || !modes_off() || !take_linear(a[1], a[2], a + 4, &l) || !take_float(a[9], &scale) || !take_bool(a[10], &with_table) ||
+        !take_status_here(a[12], &word))
+      return none();
+    const at::Tensor* c = plain(a[0]);
+    if (!c || c->dim() != 1 || c->size(0) > INT32_MAX || !take_optional(a[0], at::kFloat, {c->size(0)}, &coef) || a[3] == Py_None ||
+        !take_optional(a[3], at::kFloat, {l.rows}, &lse))
+      return none();
+    const int32_t segments = int32_t(c->size(0));
+    const size_t bytes = g_lib.linear_logp_bytes(l.rows, int32_t(l.n_forks), segments, l.vocab, int32_t(l.width), 1);
+    if (bytes == 0 || !take_workspace(a[11], bytes, *l.hidden, &ws)) return none();
+    at::Tensor dh = make({l.rows, l.width}, at::kBFloat16, *l.hidden), dw;
+    if (with_table) dw = make({l.vocab, l.width}, at::kBFloat16, *l.hidden);
+    void *const to = dh.data_ptr(), *const tw = with_table ? dw.data_ptr() : nullptr, *const scratch = ws.data_ptr(), *const on = stream();
+    const psa_status_t rc = unlocked([&] {
+      return g_lib.linear_logp_bwd(static_cast<float*>(coef), l.h, l.w, static_cast<float*>(lse), l.rows, l.vocab, int32_t(l.width), scale,
+                                   static_cast<int32_t*>(l.targets), static_cast<int32_t*>(l.segments), static_cast<int32_t*>(l.forks[0]),
+                                   static_cast<int32_t*>(l.forks[1]), static_cast<int32_t*>(l.forks[2]), int32_t(l.n_forks), segments, to, tw,
+                                   scratch, static_cast<int32_t*>(word), on);
+    });
+    if (rc != PSA_OK) return PyLong_FromLong(rc);
+    return with_table ? tuple_of(dh, dw) : Py_BuildValue("(NO)", THPVariable_Wrap(dh), Py_None);
+  });
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {{"init", init, METH_O, nullptr}, FAST(fwd),  FAST(bwd),  FAST(logp), FAST(logp_bwd),
                            FAST(loss),                      FAST(rope), FAST(plan), {"destroy", destroy, METH_O, nullptr},
-                           FAST(norm), FAST(norm_bwd), FAST(embed), FAST(embed_bwd), FAST(ffn), FAST(ffn_bwd),
+                           FAST(norm), FAST(norm_bwd), FAST(embed), FAST(embed_bwd), FAST(ffn), FAST(ffn_bwd), FAST(rotary),
+                           FAST(block_norm), FAST(block_norm_bwd), FAST(linear_logp), FAST(linear_logp_bwd),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "psa_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
