@@ -41,21 +41,51 @@ struct Args {
   int32_t inverse;
 };
 
+// W elements as one load brings them.
 template <typename T, int W>
 struct alignas(W * sizeof(T)) Pack {
-  T v[W];
+  static constexpr int kWords = W * int(sizeof(T)) / 4;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void get(float (&v)[W]) const {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        v[i] = __uint_as_float(w[i]);
+      } else {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  }
+  __device__ __forceinline__ void set(const float (&v)[W]) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        w[i] = __float_as_uint(v[i]);
+      } else {
+        const __nv_bfloat162 pair = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&pair);
+      }
+    }
+  }
 };
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
+template <>
+struct Pack<__nv_bfloat16, 1> {
+  __nv_bfloat16 w;
+  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = __bfloat162float(w); }
+  __device__ __forceinline__ void set(const float (&v)[1]) { w = __float2bfloat16(v[0]); }
+};
 
 // W elements a load.  Half layout: a thread holds W pairs, one vector of each half; interleaved: W / 2 pairs in one vector.
+// All of a thread's heads are requested ahead of the sines; threads whose vector is only copied go the same way.
+template <bool kInterleaved>
+__host__ __device__ constexpr int most_heads() { return kInterleaved ? 8 : 4; }      // of a thread
+
 template <typename T, int W, bool kInterleaved>
 __global__ void __launch_bounds__(kThreads)
 rotary_kernel(const Args args) {
   using P = Pack<T, W>;
-  constexpr int kPairs = kInterleaved ? W / 2 : W;
+  constexpr int kPairs = kInterleaved ? W / 2 : W, kHeads = most_heads<kInterleaved>();
   const int turned = args.rotary_dim / 2 / kPairs, per_group = turned + args.copies;
   const int groups = args.side[0].groups + args.side[1].groups, per_token = groups * per_group;
   const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x, token = i / per_token;
@@ -63,50 +93,60 @@ rotary_kernel(const Args args) {
   behind_go();
   if (token >= args.n_tokens) return;
   const int at = int(i - token * per_token), group = at / per_group, v = at - group * per_group;
-  const bool second = group >= args.side[0].groups;
+  const bool second = group >= args.side[0].groups, turns = v < turned;
   const Side& side = args.side[second];
-  const int head0 = (second ? group - args.side[0].groups : group) * args.each, head1 = min(head0 + args.each, side.heads);
-  const T* x = static_cast<const T*>(side.x) + token * side.x_token + head0 * side.x_head;
-  T* y = static_cast<T*>(side.y) + token * side.y_token + head0 * side.y_head;
-  if (v >= turned) {
-    const int c = args.rotary_dim + (v - turned) * W;
-#pragma unroll 4
-    for (int h = head0; h < head1; ++h, x += side.x_head, y += side.y_head)
-      *reinterpret_cast<P*>(y + c) = *reinterpret_cast<const P*>(x + c);
-    return;
-  }
-  float cs[kPairs], sn[kPairs];
+  const int head0 = (second ? group - args.side[0].groups : group) * args.each, heads = min(args.each, side.heads - head0);
+  const int first = kInterleaved || turns ? v * W : args.rotary_dim + (v - turned) * W, half = args.rotary_dim / 2;
+  const T* x = static_cast<const T*>(side.x) + token * side.x_token + head0 * side.x_head + first;
+  T* y = static_cast<T*>(side.y) + token * side.y_token + head0 * side.y_head + first;
+  P p[kHeads], q[kInterleaved ? 1 : kHeads];
   const long long position = args.position_ids[token];
 #pragma unroll
-  for (int j = 0; j < kPairs; ++j) {
-    const unsigned long long angle = static_cast<unsigned long long>(position) * args.turns[v * kPairs + j];
-    // the signed top 32 bits: -1/2 to 1/2 of a turn
-    sincospif(float(int32_t(angle >> 32)) * 4.656612873077393e-10f, &sn[j], &cs[j]);
-    cs[j] *= args.magnitude;
-    sn[j] *= args.inverse ? -args.magnitude : args.magnitude;
+  for (int h = 0; h < kHeads; ++h)
+    if (h < heads) {
+      p[h] = *reinterpret_cast<const P*>(x + h * side.x_head);
+      if (!kInterleaved && turns) q[kInterleaved ? 0 : h] = *reinterpret_cast<const P*>(x + h * side.x_head + half);
+    }
+  float cs[kPairs], sn[kPairs];
+  if (turns) {
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) {
+      const unsigned long long angle = static_cast<unsigned long long>(position) * args.turns[v * kPairs + j];
+      // the signed top 32 bits: -1/2 to 1/2 of a turn
+      sincospif(float(int32_t(angle >> 32)) * 4.656612873077393e-10f, &sn[j], &cs[j]);
+      cs[j] *= args.magnitude;
+      sn[j] *= args.inverse ? -args.magnitude : args.magnitude;
+    }
   }
-  const int c = v * W, half = args.rotary_dim / 2;
-#pragma unroll 4
-  for (int h = head0; h < head1; ++h, x += side.x_head, y += side.y_head) {
+#pragma unroll
+  for (int h = 0; h < kHeads; ++h) {
+    if (h >= heads) break;
+    P* to = reinterpret_cast<P*>(y + h * side.y_head);
+    if (!turns) {
+      *to = p[h];
+      continue;
+    }
+    float a[W], b[W], r[W];
+    p[h].get(a);
     if (kInterleaved) {
-      P p = *reinterpret_cast<const P*>(x + c);
 #pragma unroll
-      for (int j = 0; j < kPairs; ++j) {
-        const float a = to_float(p.v[2 * j]), b = to_float(p.v[2 * j + 1]);
-        put(&p.v[2 * j], a * cs[j] - b * sn[j]);
-        put(&p.v[2 * j + 1], b * cs[j] + a * sn[j]);
+      for (int k = 0; k < kPairs; ++k) {
+        r[2 * k] = a[2 * k] * cs[k] - a[2 * k + 1] * sn[k];
+        r[2 * k + 1] = a[2 * k + 1] * cs[k] + a[2 * k] * sn[k];
       }
-      *reinterpret_cast<P*>(y + c) = p;
+      p[h].set(r);
+      *to = p[h];
     } else {
-      P p = *reinterpret_cast<const P*>(x + c), q = *reinterpret_cast<const P*>(x + c + half);
+      P& second_half = q[kInterleaved ? 0 : h];
+      second_half.get(b);
 #pragma unroll
-      for (int j = 0; j < kPairs; ++j) {
-        const float a = to_float(p.v[j]), b = to_float(q.v[j]);
-        put(&p.v[j], a * cs[j] - b * sn[j]);
-        put(&q.v[j], b * cs[j] + a * sn[j]);
-      }
-      *reinterpret_cast<P*>(y + c) = p;
-      *reinterpret_cast<P*>(y + c + half) = q;
+      for (int k = 0; k < kPairs; ++k) r[k] = a[k] * cs[k] - b[k] * sn[k];
+      p[h].set(r);
+      *to = p[h];
+#pragma unroll
+      for (int k = 0; k < kPairs; ++k) r[k] = b[k] * cs[k] + a[k] * sn[k];
+      second_half.set(r);
+      *reinterpret_cast<P*>(y + h * side.y_head + half) = second_half;
     }
   }
 }
@@ -133,8 +173,8 @@ psa_status_t launch(Args a, cudaStream_t stream) {
   } else {
     if (a.copies) a.copies = (a.head_dim - a.rotary_dim) / W;
     const int per_group = a.rotary_dim / 2 / (kInterleaved ? W / 2 : W) + a.copies;
-    // Heads a thread: as many as leave 1024 threads for each SM, 8 at most
-    a.each = 8;
+    // Heads a thread: as many as leave 1024 threads for each SM
+    a.each = most_heads<kInterleaved>();
     auto threads = [&] {
       int64_t groups = 0;
       for (Side& s : a.side) groups += s.groups = (s.heads + a.each - 1) / a.each;
