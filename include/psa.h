@@ -545,7 +545,8 @@ psa_status_t dpo_logp_bwd(const void* logits, int32_t logits_dtype, int64_t n_ro
  *   out[g] = sum over scored (row t, label y) with response id g of  z[t][y] - log sum_v exp(z[t][v])
  *   lse[t] = log sum_v exp(z[t][v]) of every row that scores a label, 0 of the others
  *   hidden        device bf16 [n_rows, width]      table  device bf16 [vocab, width] (as psa_embed's)
- *   width         a multiple of 8, at most 2^20;  n_rows, n_forks, n_segments and vocab at most 2^24
+ *   width         a multiple of 8, at most 2^20;  n_rows, n_forks, n_segments and vocab at most 2^24, and
+ *                 (n_rows + n_forks) * vocab at most 2^45
  *   scale         positive and finite
  *   targets, segment_ids, fork_rows, fork_targets, fork_segments, n_forks, n_segments   as for dpo_logp; a row may be
  *                 named by any number of forks

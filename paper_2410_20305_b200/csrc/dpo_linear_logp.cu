@@ -76,7 +76,7 @@ logp_list_kernel(const int32_t* targets, const int32_t* segment_ids, const int32
                  const int32_t* fork_segments, int32_t n_rows, int32_t n_forks, int32_t n_segments, int32_t vocab, Labels labels,
                  Sum* sums, int32_t* status) {
   constexpr int kWarps = kListThreads / 32, kCounts = kListEach * kWarps;
-  __shared__ int32_t s_count[kCounts], s_total;
+  __shared__ int32_t s_count[kCounts], s_warp[kCounts / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   behind_wait();
   behind_go();
@@ -111,20 +111,22 @@ logp_list_kernel(const int32_t* targets, const int32_t* segment_ids, const int32
         if (lane == 0) s_count[j * kWarps + warp] = __popc(mine[j]);
       }
       __syncthreads();
-      if (warp == 0) {     // counts become places
-        int32_t carry = base;
-        for (int c = 0; c < kCounts; c += 32) {
-          const int32_t v = s_count[c + lane];
-          int32_t up = v;
+      // counts become places: 32 of them by each of the first warps, then those of the warps in front are added
+      int32_t v = 0, up = 0;
+      if (warp < kCounts / 32) {
+        v = up = s_count[threadIdx.x];
 #pragma unroll
-          for (int o = 1; o < 32; o *= 2) {
-            const int32_t w = __shfl_up_sync(0xffffffffu, up, o);
-            if (lane >= o) up += w;
-          }
-          s_count[c + lane] = carry + up - v;
-          carry += __shfl_sync(0xffffffffu, up, 31);
+        for (int o = 1; o < 32; o *= 2) {
+          const int32_t w = __shfl_up_sync(0xffffffffu, up, o);
+          if (lane >= o) up += w;
         }
-        if (lane == 0) s_total = carry;
+        if (lane == 31) s_warp[warp] = up;
+      }
+      __syncthreads();
+      if (warp < kCounts / 32) {
+        int32_t in_front = base;
+        for (int w = 0; w < warp; ++w) in_front += s_warp[w];
+        s_count[threadIdx.x] = in_front + up - v;
       }
       __syncthreads();
 #pragma unroll
@@ -139,7 +141,8 @@ logp_list_kernel(const int32_t* targets, const int32_t* segment_ids, const int32
         if (!list && row[j] >= 0) labels.state[row[j]] = valid ? 2 * (place + 1) : 0;
         if (list && valid) atomicOr(labels.state + row[j], 1);
       }
-      base = s_total;
+#pragma unroll
+      for (int w = 0; w < kCounts / 32; ++w) base += s_warp[w];
       __syncthreads();
     }
     if (!list) n_own = base;
@@ -197,7 +200,9 @@ logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32
 
 // ---------------------------------------------------------------- products
 // A persistent kernel: 74 clusters of two CTAs take tiles of 256 x 256.  A tile's product is one UMMA stream of the pair: each
-// CTA loads its 128 rows of A and 128 of the tile's 256 columns of B.  The accumulator takes half of TMEM: while the end of one
+// CTA loads its 128 rows of A and 128 of the tile's 256 columns of B.  (Narrower tiles of the vocabulary, to fill the last round over
+// the clusters, took longer: the loads, 64 bytes a clock and SM, bind as soon as a tile is: 988 labels x 128256 x 4096 677 -> 689 us
+// with 240 columns, 1145 x 50257 x 1032 107 -> 128.)  The accumulator takes half of TMEM: while the end of one
 // tile drains it, the next tile's UMMAs fill the other half.
 // Warps: 0 TMA, 1 UMMA (in the CTA of rank 0), 2 TMEM, 4-7 the end of a tile, each for 32 rows of its CTA.
 enum Epilogue {
@@ -572,19 +577,28 @@ logp_join_kernel(const float2* stats, const float* picked, const float* label_lo
     };
     if (i < n) {
       int v = warp;
-      for (; v + 3 * kJoinWarps < v_tiles; v += 4 * kJoinWarps) {
-        float2 p[4];
+      for (; v + 7 * kJoinWarps < v_tiles; v += 8 * kJoinWarps) {
+        float2 p[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) p[k] = stats[int64_t(v + k * kJoinWarps) * l_pad + i];
+        for (int k = 0; k < 8; ++k) p[k] = stats[int64_t(v + k * kJoinWarps) * l_pad + i];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) merge(p[k]);
+        for (int k = 0; k < 8; ++k) merge(p[k]);
       }
+#pragma unroll 4
       for (; v < v_tiles; v += kJoinWarps) merge(stats[int64_t(v) * l_pad + i]);
     }
     s_part[warp][lane] = make_float2(m, s);
     __syncthreads();
     if (warp == 0 && i < n) {
-      for (int k = 1; k < kJoinWarps; ++k) merge(s_part[k][lane]);
+      float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int k = 0; k < kJoinWarps; ++k) top[k & 1] = fmaxf(top[k & 1], s_part[k][lane].x);
+      m = fmaxf(top[0], top[1]);
+      const float shift = m == -INFINITY ? 0.f : m;      // (nothing finite: all sums are 0, or NaN where a logit was)
+      float all[2] = {0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < kJoinWarps; ++k) all[k & 1] += s_part[k][lane].y * ex2_approx(s_part[k][lane].x - shift);
+      s = all[0] + all[1];
       const int32_t t = labels.row[i];
       // The label's logit as its own product in the place of the one from the tiles.  The maximum is taken off before anything is
       // rounded to fp32: the term of a token that takes nearly all of the probability is near 0 itself, not the difference of two
@@ -707,6 +721,7 @@ psa_status_t check_sizes(int64_t n_rows, int64_t n_forks, int64_t n_segments, in
   if (n_rows < 0 || n_forks < 0 || n_segments < 0 || vocab <= 0 || width <= 0) return PSA_ERR_INVALID_ARG;
   constexpr int64_t kMost = 1 << 24;
   if (width % 8 || width > (1 << 20) || n_rows > kMost || n_forks > kMost || n_segments > kMost || vocab > kMost) return PSA_ERR_UNSUPPORTED;
+  if ((n_rows + n_forks) * vocab > (int64_t(1) << 45)) return PSA_ERR_UNSUPPORTED;      // fewer than 2^30 tiles: they are counted in 32 bits
   return PSA_OK;
 }
 psa_status_t check(const Call& c, std::initializer_list<const void*> outputs) {
