@@ -11,6 +11,7 @@ import torch
 
 from oracle import psa_oracle as orc
 from paper_2410_20305_b200 import binding as B
+from paper_2410_20305_b200 import operators as O
 
 pytestmark = pytest.mark.gpu
 
@@ -60,10 +61,10 @@ def check(T, D, kind, rms, post, gate, scale=1.0, with_total=True, mean=0.0, see
     x, res = normal((T, D), seed, xt, mean), normal((T, D), seed + 6, xt, mean, 2.0)
     d_out, d_total = normal((T, D), seed + 7, xt), normal((T, D), seed + 8, xt) if with_total else None
     p = parameters(D, kind, rms, post, gate, seed)
-    out, total, stats = B.psa_block_norm(x, res, eps=1e-5, rms=rms, residual_scale=scale, **p)
+    out, total, stats = O.psa_block_norm(x, res, eps=1e-5, rms=rms, residual_scale=scale, **p)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     around = {k: v for k, v in p.items() if k != "bias"}
-    grads = B.psa_block_norm_bwd(d_out, x, total, stats=stats, rms=rms, residual_scale=scale, d_total=d_total, with_bias=not rms, status=status,
+    grads = O.psa_block_norm_bwd(d_out, x, total, stats=stats, rms=rms, residual_scale=scale, d_total=d_total, with_bias=not rms, status=status,
                                  **around)
     torch.cuda.synchronize()
     assert int(status.item()) == 0
@@ -146,9 +147,9 @@ def test_rows_far_from_zero(D):
 def test_no_tokens():
     p = parameters(40, "mixed", False, True, True, 0)
     x = torch.zeros((0, 40), dtype=torch.bfloat16, device="cuda")
-    out, total, stats = B.psa_block_norm(x, x, **p)
+    out, total, stats = O.psa_block_norm(x, x, **p)
     p.pop("bias")
-    dx, dr, *dp = B.psa_block_norm_bwd(x, x, x, stats=stats, with_bias=True, **p)
+    dx, dr, *dp = O.psa_block_norm_bwd(x, x, x, stats=stats, with_bias=True, **p)
     torch.cuda.synchronize()
     assert out.shape == total.shape == dx.shape == dr.shape == (0, 40) and stats.shape == (4, 0)
     assert len(dp) == 5 and not any(d.any() for d in dp)
@@ -159,17 +160,17 @@ def test_in_place_and_rows_beyond_the_last(D):
     T, more = 201, 240
     p = parameters(D, "bf16", False, True, True, 3)
     x, res, d_out, d_total = (normal((more, D), k, torch.bfloat16) for k in range(4))
-    want = B.psa_block_norm(x[:T].clone(), res[:T].clone(), **p)
+    want = O.psa_block_norm(x[:T].clone(), res[:T].clone(), **p)
     a, b = x.clone(), res.clone()
     a[T:], b[T:] = float("nan"), float("nan")
-    out, total, stats = B.psa_block_norm(a[:T], b[:T], out=a[:T], total=b[:T], **p)
+    out, total, stats = O.psa_block_norm(a[:T], b[:T], out=a[:T], total=b[:T], **p)
     assert all(torch.equal(u, v) for u, v in zip((out, total, stats), want))
     assert a[T:].isnan().all() and b[T:].isnan().all()
     p.pop("bias")
-    grads = B.psa_block_norm_bwd(d_out[:T].clone(), x[:T].clone(), total.clone(), stats=stats, d_total=d_total[:T].clone(), **p)
+    grads = O.psa_block_norm_bwd(d_out[:T].clone(), x[:T].clone(), total.clone(), stats=stats, d_total=d_total[:T].clone(), **p)
     for places in (("d_out", "total"), ("x", "d_total"), ("total", "d_out"), ("d_total", "total")):
         t = {"d_out": d_out[:T].clone(), "x": x[:T].clone(), "total": total.clone(), "d_total": d_total[:T].clone()}
-        again = B.psa_block_norm_bwd(**t, stats=stats, dx=t[places[0]], d_residual=t[places[1]], **p)
+        again = O.psa_block_norm_bwd(**t, stats=stats, dx=t[places[0]], d_residual=t[places[1]], **p)
         torch.cuda.synchronize()
         assert again[0] is t[places[0]] and all(u is v is None or torch.equal(u, v) for u, v in zip(again, grads)), places
 
@@ -177,12 +178,12 @@ def test_in_place_and_rows_beyond_the_last(D):
 def test_in_place_of_wide_rows():
     p = parameters(12000, "bf16", True, True, False, 3)
     x, res, d_out, d_total = (normal((7, 12000), k, torch.bfloat16) for k in range(4))
-    _, total, stats = B.psa_block_norm(x, res, rms=True, **p)
+    _, total, stats = O.psa_block_norm(x, res, rms=True, **p)
     p.pop("bias")
-    grads = B.psa_block_norm_bwd(d_out.clone(), x.clone(), total.clone(), stats=stats, d_total=d_total.clone(), rms=True, **p)
+    grads = O.psa_block_norm_bwd(d_out.clone(), x.clone(), total.clone(), stats=stats, d_total=d_total.clone(), rms=True, **p)
     for places in (("d_out", "total"), ("x", "d_total"), ("total", "d_out"), ("d_total", "total")):
         t = {"d_out": d_out.clone(), "x": x.clone(), "total": total.clone(), "d_total": d_total.clone()}
-        again = B.psa_block_norm_bwd(**t, stats=stats, rms=True, dx=t[places[0]], d_residual=t[places[1]], **p)
+        again = O.psa_block_norm_bwd(**t, stats=stats, rms=True, dx=t[places[0]], d_residual=t[places[1]], **p)
         assert all(u is v is None or torch.equal(u, v) for u, v in zip(again, grads)), places
 
 
@@ -191,15 +192,15 @@ def test_in_place_of_wide_rows():
 def test_rows_that_are_not_finite_stay_alone(D, bad):
     p = parameters(D, "bf16", False, True, True, 9)
     x, res = normal((60, D), 0, torch.bfloat16), normal((60, D), 1, torch.bfloat16)
-    clean = B.psa_block_norm(x, res, **p)
+    clean = O.psa_block_norm(x, res, **p)
     y = x.clone()
     y[31, D // 2] = bad
-    got = B.psa_block_norm(y, res, **p)
+    got = O.psa_block_norm(y, res, **p)
     rest = [i for i in range(60) if i != 31]
     assert all(torch.equal(a[rest], b[rest]) for a, b in zip(got[:2], clean[:2])) and got[0][31].isnan().all()
     p.pop("bias")
-    a = B.psa_block_norm_bwd(res, x, clean[1], stats=clean[2], **p)
-    b = B.psa_block_norm_bwd(res, y, got[1], stats=got[2], **p)
+    a = O.psa_block_norm_bwd(res, x, clean[1], stats=clean[2], **p)
+    b = O.psa_block_norm_bwd(res, y, got[1], stats=got[2], **p)
     assert all(torch.equal(u[rest], v[rest]) for u, v in zip(a[:2], b[:2])) and b[0][31].isnan().all()
 
 
@@ -207,21 +208,21 @@ def test_the_same_inputs_give_the_same_bits():
     for T, D in ((3000, 1237), (2000, 4096), (9000, 100)):
         p = parameters(D, "mixed", False, True, True, 9)
         x, res, g = (normal((T, D), k, torch.bfloat16) for k in range(3))
-        _, total, stats = B.psa_block_norm(x, res, **p)
+        _, total, stats = O.psa_block_norm(x, res, **p)
         q = {k: v for k, v in p.items() if k != "bias"}
-        first = B.psa_block_norm_bwd(g, x, total, stats=stats, d_total=res, with_bias=True, **q)
+        first = O.psa_block_norm_bwd(g, x, total, stats=stats, d_total=res, with_bias=True, **q)
         need = B.load_library().psa_block_norm_bwd_workspace_bytes(T, D)
         ws = torch.full((need + 256,), 255, dtype=torch.uint8, device="cuda")
-        again = B.psa_block_norm_bwd(g, x, total, stats=stats, d_total=res, with_bias=True, workspace=ws[:need], **q)
+        again = O.psa_block_norm_bwd(g, x, total, stats=stats, d_total=res, with_bias=True, workspace=ws[:need], **q)
         assert all(torch.equal(a, b) for a, b in zip(first, again)) and bool((ws[need:] == 255).all())
 
 
 def test_without_a_norm_or_a_gate_it_is_psa_norm():
     x, res, g, dt = (normal((130, 520), k, torch.bfloat16) for k in range(4))
     w, b = normal((520,), 5, torch.bfloat16, 1.0), normal((520,), 6, torch.bfloat16)
-    out, total, stats = B.psa_block_norm(x, res, w, bias=b)
+    out, total, stats = O.psa_block_norm(x, res, w, bias=b)
     want = B.psa_norm(x, w, b, residual=res)
     assert torch.equal(total, want[2]) and (out.float() - want[0].float()).abs().max() <= 2.0 ** -6
-    dx, dr, dw, db, *none = B.psa_block_norm_bwd(g, x, total, w, stats, d_total=dt, with_bias=True)
+    dx, dr, dw, db, *none = O.psa_block_norm_bwd(g, x, total, w, stats, d_total=dt, with_bias=True)
     wx, ww, wb = B.psa_norm_bwd(g, want[2], w, want[1], d_total=dt, with_bias=True)
     assert torch.equal(dx, dr) and (dx.float() - wx.float()).abs().max() <= 2.0 ** -5 and none == [None] * 3

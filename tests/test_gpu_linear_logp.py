@@ -13,6 +13,7 @@ import torch
 
 from oracle import psa_oracle as orc
 from paper_2410_20305_b200 import binding as B
+from paper_2410_20305_b200 import operators as O
 
 pytestmark = pytest.mark.gpu
 
@@ -41,8 +42,8 @@ def both(hidden, table, targets, seg, forks, coef, scale=1.0, **kw):
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     args = [i32(targets), i32(seg)]
     f = [i32(a) for a in forks]
-    out, lse = B.dpo_linear_logp(hidden.cuda(), table.cuda(), *args, len(coef), *f, scale=scale, status=status, **kw)
-    dh, dw = B.dpo_linear_logp_bwd(dev(coef), hidden.cuda(), table.cuda(), lse, *args, *f, scale=scale, status=status, **kw)
+    out, lse = O.dpo_linear_logp(hidden.cuda(), table.cuda(), *args, len(coef), *f, scale=scale, status=status, **kw)
+    dh, dw = O.dpo_linear_logp_bwd(dev(coef), hidden.cuda(), table.cuda(), lse, *args, *f, scale=scale, status=status, **kw)
     torch.cuda.synchronize()
     return out, lse, dh, dw, int(status.item())
 
@@ -193,7 +194,7 @@ def test_a_table_that_is_not_trained():
     args = inputs(200, 64, 900, 4)
     _, lse, dh, _, _ = both(*args)
     hidden, table, targets, seg, forks, coef = args
-    got, none = B.dpo_linear_logp_bwd(dev(coef), hidden.cuda(), table.cuda(), lse, i32(targets), i32(seg), *[i32(f) for f in forks],
+    got, none = O.dpo_linear_logp_bwd(dev(coef), hidden.cuda(), table.cuda(), lse, i32(targets), i32(seg), *[i32(f) for f in forks],
                                       with_table=False)
     assert none is None and torch.equal(got, dh)
 
