@@ -158,7 +158,7 @@ __host__ __device__ constexpr int64_t padded(int64_t n) { return (n + 255) / 256
 // of itself (4.2e-6 at 4096, the same for all), and a log-probability near 0 is the difference of two such numbers (1.5e-4 of it at
 // width 4096 where the logit of 6 was taken from TMEM).
 __global__ void __launch_bounds__(256)
-logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32_t vectors, uint4* rows, const float* coef, const float* lse,
+logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32_t vectors, int32_t pitch, uint4* rows, const float* coef, const float* lse,
                    float scale, float2* of_label, float* label_logit) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t i = int64_t(blockIdx.x) * 8 + warp;
@@ -166,7 +166,7 @@ logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32
   behind_go();
   const int32_t n = labels.shared->n_labels;
   if (i >= max(padded(n), int64_t(256))) return;
-  uint4* to = rows + i * vectors;
+  uint4* to = rows + i * pitch;
   if (i >= n) {
     for (int c = lane; c < vectors; c += 32) to[c] = make_uint4(0, 0, 0, 0);
     return;
@@ -669,6 +669,7 @@ size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
 struct Workspace {
   int64_t l_pad;
   int64_t piece;                 // columns of a piece of the vocabulary
+  int64_t pitch;                 // of the labels' rows: whole lines of 128 bytes
   int32_t splits;
   size_t row, target, segment, state, sums, rows, stats, picked, label_logit, of_label, dz, parts, total;
   Workspace(int64_t n_rows, int64_t n_forks, int64_t n_segments, int64_t vocab, int64_t hidden, bool backward) {
@@ -684,7 +685,8 @@ struct Workspace {
     target = take(l_pad * 4);
     segment = take(l_pad * 4);
     state = take(n_rows * 4);
-    rows = take(l_pad * hidden * 2);
+    pitch = (hidden + 63) / 64 * 64;
+    rows = take(l_pad * pitch * 2);
     sums = stats = picked = label_logit = of_label = dz = parts = 0;
     if (backward) {
       of_label = take(l_pad * sizeof(float2));
@@ -745,7 +747,7 @@ bool launch_labels(const Call& c, const Workspace& w, bool backward, const float
                     backward ? nullptr : reinterpret_cast<Sum*>(c.ws + w.sums), c.status) != cudaSuccess)
     return false;
   return launch_behind(true, logp_gather_kernel, dim3(unsigned(w.l_pad / 8)), 256, 0, c.stream, static_cast<const uint4*>(c.hidden),
-                       static_cast<const uint4*>(c.table), labels, c.width / 8, reinterpret_cast<uint4*>(c.ws + w.rows), coef, lse, c.scale,
+                       static_cast<const uint4*>(c.table), labels, c.width / 8, int32_t(w.pitch / 8), reinterpret_cast<uint4*>(c.ws + w.rows), coef, lse, c.scale,
                        backward ? reinterpret_cast<float2*>(c.ws + w.of_label) : nullptr,
                        backward ? nullptr : reinterpret_cast<float*>(c.ws + w.label_logit)) == cudaSuccess;
 }
@@ -783,7 +785,7 @@ psa_status_t forward(const Call& c, float* out, float* lse) {
   a.columns = int32_t(c.vocab);
   a.stats = reinterpret_cast<float2*>(c.ws + w.stats);
   a.picked = reinterpret_cast<float*>(c.ws + w.picked);
-  if (!operand_maps(&a.of[0].a, c.ws + w.rows, false, w.l_pad, c.width, 128) ||
+  if (!operand_maps(&a.of[0].a, c.ws + w.rows, false, w.l_pad, c.width, 128, w.pitch) ||
       !operand_maps(&a.of[0].b, c.table, false, c.vocab, c.width, 128))
     return PSA_ERR_CUDA;
   const int64_t v_tiles = (c.vocab + kTile - 1) / kTile;
@@ -806,7 +808,7 @@ psa_status_t backward(const Call& c, const float* coef, const float* lse, void* 
     a.columns = int32_t(columns);
     a.first_column = int32_t(first);
     a.of_label = reinterpret_cast<float2*>(c.ws + w.of_label);
-    if (!operand_maps(&a.of[0].a, c.ws + w.rows, false, w.l_pad, c.width, 128) ||
+    if (!operand_maps(&a.of[0].a, c.ws + w.rows, false, w.l_pad, c.width, 128, w.pitch) ||
         !operand_maps(&a.of[0].b, table, false, columns, c.width, 128) ||
         !matrix_map(&a.of[0].store, c.ws + w.dz, w.l_pad, columns, 32, 64, w.piece))
       return PSA_ERR_CUDA;
@@ -823,7 +825,7 @@ psa_status_t backward(const Call& c, const float* coef, const float* lse, void* 
       return PSA_ERR_CUDA;
     // dW = dz^T h: K runs along the labels
     if (d_table && (!operand_maps(&a.of[1].a, c.ws + w.dz, true, columns, w.l_pad, 128, w.piece) ||
-                    !operand_maps(&a.of[1].b, c.ws + w.rows, true, c.width, w.l_pad, 128) ||
+                    !operand_maps(&a.of[1].b, c.ws + w.rows, true, c.width, w.l_pad, 128, w.pitch) ||
                     !matrix_map(&a.of[1].store, static_cast<char*>(d_table) + first * c.width * 2, columns, c.width, 32)))
       return PSA_ERR_CUDA;
     if (!launch_product<kEpiOut>(a, (w.l_pad / kTile * w.splits + (d_table ? v_tiles : 0)) * d_tiles, c.stream))
