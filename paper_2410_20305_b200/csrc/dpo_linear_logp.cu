@@ -246,6 +246,11 @@ struct ProductArgs {
 struct Tile {
   int which, m0, n0, part, k0, k1;
 };
+// What a tile of dW costs beside its stages (0.37 us each): its end, 3.3 us with the tile's bytes on their way to memory, where there are
+// few stages, and a part of that where there are more.  (Counted by their stages alone, 1 to 64 labels of 128256 x 4096 took 1288 us
+// instead of 480, 256 took 784 instead of 577, 512 940 instead of 850: clusters without a heavy tile took too many of them.)
+constexpr int kEndStages = 9;
+
 // The tiles that a cluster takes.  Those of the first product (`heavy`) go round the clusters one by one; of the second, clusters
 // that have one heavy tile less take as many more as fit into its time, and the rest goes round again.
 struct Schedule {
@@ -321,7 +326,9 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
   const int v_tiles = (args.columns + kTile - 1) / kTile, d_tiles = (args.hidden + kTile - 1) / kTile;
   const int d_stages = (args.hidden + kBK - 1) / kBK, v_stages = (args.columns + kBK - 1) / kBK, l_stages = max(1, (n_labels + kBK - 1) / kBK);
   const int n_heavy = EPI == kEpiOut ? m_tiles * d_tiles * args.splits : 0, n_light = EPI == kEpiOut ? (args.with_table ? v_tiles * d_tiles : 0) : m_tiles * v_tiles;
-  const Schedule schedule(int(blockIdx.x) >> 1, int(gridDim.x) >> 1, n_heavy, n_light, v_stages / args.splits, l_stages);
+  // dW: as many rows of tiles as let the tiles in flight write whole rows of the table
+  const int dw_group = max(1, min(16, (int(gridDim.x) >> 1) / d_tiles));
+  const Schedule schedule(int(blockIdx.x) >> 1, int(gridDim.x) >> 1, n_heavy, n_light, v_stages / args.splits, max(kEndStages, l_stages + kEndStages / 2));
   auto tile_at = [&](int i, Tile* t) {
     int at = schedule.at(i);
     if (at < 0) return false;
@@ -336,7 +343,7 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
       t->k0 = int(int64_t(v_stages) * t->part / args.splits);
       t->k1 = int(int64_t(v_stages) * (t->part + 1) / args.splits);
     } else {
-      place(at - n_heavy, v_tiles, d_tiles, 16, t);
+      place(at - n_heavy, v_tiles, d_tiles, dw_group, t);
       t->which = 1;
       t->part = t->k0 = 0;
       t->k1 = l_stages;
