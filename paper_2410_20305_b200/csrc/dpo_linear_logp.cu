@@ -157,32 +157,37 @@ __host__ __device__ constexpr int64_t padded(int64_t n) { return (n + 255) / 256
 // forward the label's own product, by fp32 additions that round: tcgen05's cut off, which makes a logit smaller by about width * 1e-9
 // of itself (4.2e-6 at 4096, the same for all), and a log-probability near 0 is the difference of two such numbers (1.5e-4 of it at
 // width 4096 where the logit of 6 was taken from TMEM).
+// kWarps of a CTA's 8 take a row: all of them in a small call, where a row's trips to memory one after the other are what counts (one
+// row of 128256 x 4096: 223.6 -> 220.9 us in all).
+template <int kWarps>
 __global__ void __launch_bounds__(256)
 logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32_t vectors, int32_t pitch, uint4* rows, const float* coef, const float* lse,
                    float scale, float2* of_label, float* label_logit) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t i = int64_t(blockIdx.x) * 8 + warp;
+  constexpr int kThreads = 32 * kWarps;
+  __shared__ float s_sum[8];
+  const int tid = int(threadIdx.x) % kThreads, lane = threadIdx.x & 31;
+  const int64_t i = int64_t(blockIdx.x) * (8 / kWarps) + int(threadIdx.x) / kThreads;
   behind_wait();
   behind_go();
   const int32_t n = labels.shared->n_labels;
   if (i >= max(padded(n), int64_t(256))) return;
   uint4* to = rows + i * pitch;
   if (i >= n) {
-    for (int c = lane; c < vectors; c += 32) to[c] = make_uint4(0, 0, 0, 0);
+    for (int c = tid; c < vectors; c += kThreads) to[c] = make_uint4(0, 0, 0, 0);
     return;
   }
   const int32_t t = labels.row[i];
-  if (of_label && lane == 0) of_label[i] = make_float2(coef[labels.segment[i]] * scale, lse[t] * kLog2e);
+  if (of_label && tid == 0) of_label[i] = make_float2(coef[labels.segment[i]] * scale, lse[t] * kLog2e);
   const uint4* from = hidden + int64_t(t) * vectors;
   if (!label_logit) {
 #pragma unroll 4
-    for (int c = lane; c < vectors; c += 32) to[c] = from[c];
+    for (int c = tid; c < vectors; c += kThreads) to[c] = from[c];
     return;
   }
   const uint4* weight = table + int64_t(labels.target[i]) * vectors;
   float sum[8] = {};
 #pragma unroll 4
-  for (int c = lane; c < vectors; c += 32) {
+  for (int c = tid; c < vectors; c += kThreads) {
     const uint4 h = from[c], w = weight[c];
     to[c] = h;
     const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, ww[4] = {w.x, w.y, w.z, w.w};
@@ -195,7 +200,12 @@ logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32
   float all = ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
 #pragma unroll
   for (int o = 16; o; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
-  if (lane == 0) label_logit[i] = all;
+  if (kWarps > 1) {      // (a row a CTA: all threads are here)
+    if (lane == 0) s_sum[tid >> 5] = all;
+    __syncthreads();
+    all = ((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3])) + ((s_sum[4] + s_sum[5]) + (s_sum[6] + s_sum[7]));
+  }
+  if (tid == 0) label_logit[i] = all;
 }
 
 // ---------------------------------------------------------------- products
@@ -753,7 +763,8 @@ bool launch_labels(const Call& c, const Workspace& w, bool backward, const float
                     c.fork_segments, int32_t(c.n_rows), c.n_forks, c.n_segments, int32_t(c.vocab), labels,
                     backward ? nullptr : reinterpret_cast<Sum*>(c.ws + w.sums), c.status) != cudaSuccess)
     return false;
-  return launch_behind(true, logp_gather_kernel, dim3(unsigned(w.l_pad / 8)), 256, 0, c.stream, static_cast<const uint4*>(c.hidden),
+  const bool few = w.l_pad <= 2048;
+  return launch_behind(true, few ? logp_gather_kernel<8> : logp_gather_kernel<1>, dim3(unsigned(few ? w.l_pad : w.l_pad / 8)), 256, 0, c.stream, static_cast<const uint4*>(c.hidden),
                        static_cast<const uint4*>(c.table), labels, c.width / 8, int32_t(w.pitch / 8), reinterpret_cast<uint4*>(c.ws + w.rows), coef, lse, c.scale,
                        backward ? reinterpret_cast<float2*>(c.ws + w.of_label) : nullptr,
                        backward ? nullptr : reinterpret_cast<float*>(c.ws + w.label_logit)) == cudaSuccess;
