@@ -554,8 +554,9 @@ psa_status_t dpo_logp_bwd(const void* logits, int32_t logits_dtype, int64_t n_ro
  *   workspace     device scratch of dpo_linear_logp_workspace_bytes(.., backward = 0) bytes, 16-byte aligned
  *   device_status device int32 or NULL: BAD_TARGET and BAD_SEGMENT as by dpo_logp, WAIT_EXPIRED as by psa_fwd
  * The sums of the responses do not depend on the order of their terms: the same inputs give the same bits.  A term below
- * -2^38 counts as -2^38, one that rounding has put above 0 as 0.  A row whose logits are not all finite has no
- * log-probability: its term and lse are NaN.  Outputs must not overlap inputs or one another.
+ * -2^38 counts as -2^38, one that rounding has put above 0 as 0.  A logit of -inf is a probability of 0 (a label's term is then
+ * -inf); a row with another logit that is not finite has no log-probability: its term and lse are NaN.  Outputs must not
+ * overlap inputs or one another.
  * Errors: INVALID_ARG, UNSUPPORTED (sizes), ALIGNMENT (hidden, table, workspace: 16 bytes), CUDA.
  */
 size_t dpo_linear_logp_workspace_bytes(int64_t n_rows, int32_t n_forks, int32_t n_segments, int64_t vocab,

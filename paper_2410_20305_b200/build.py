@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -29,18 +31,25 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     if not force and not _stale(lib):
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-o", lib] + [os.path.join(CSRC, s) for s in SOURCES]
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    flags = ["-O3", "-std=c++17", *arch, "-lineinfo", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if debug:
-        cmd += ["-DPSA_DEBUG_BOUNDS"]
+        flags += ["-DPSA_DEBUG_BOUNDS"]
     if verbose:
-        cmd += ["-Xptxas", "-v"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed building " + os.path.basename(lib))
+        flags += ["-Xptxas", "-v"]
+
+    def run(cmd):
+        res = subprocess.run([nvcc, *cmd], capture_output=True, text=True)
+        if verbose or res.returncode != 0:
+            sys.stderr.write(res.stdout + res.stderr)
+        return res.returncode == 0
+
+    # the files side by side: the norms' many instances take a minute or more each
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        made = [os.path.join(objects, s + ".o") for s in SOURCES]
+        done = list(pool.map(lambda pair: run([*flags, "-c", "-o", pair[1], os.path.join(CSRC, pair[0])]), zip(SOURCES, made)))
+        if not all(done) or not run(["-shared", "-Xcompiler", "-fPIC", *arch, "-o", lib, *made]):
+            raise RuntimeError("nvcc failed building " + os.path.basename(lib))
     return lib
 
 

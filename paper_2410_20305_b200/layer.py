@@ -175,7 +175,7 @@ class PreferenceDecoder:
     """A decoder on one pack, from token ids to the summed log-probabilities of its responses, and back: token embedding, a
     BlockNormLayer for each weight of `layers`, the final norm, and dpo_linear_logp against the output table.  No logits are stored.
 
-    params: a dict with table [vocab, hidden], layers (a list of weights), final [hidden], and head [vocab, hidden] or None, where
+    params: a dict with table [vocab, hidden], layers (a list of weights, one at least), final [hidden], and head [vocab, hidden] or None, where
     the output table is the embedding's; all bf16.  labels: (targets, segment_ids, fork_rows, fork_targets, fork_segments) as
     logp_labels gives them, on the device."""
 
@@ -189,6 +189,8 @@ class PreferenceDecoder:
     def forward(self, params, token_ids, labels):
         """Returns (log-probabilities fp32 [2 n_samples], what backward needs)."""
         layers, head = params["layers"], params["table"] if params["head"] is None else params["head"]
+        if not layers:
+            raise ValueError("layers: one at least is needed")
         x, delta, saved, before = B.psa_embed(token_ids, params["table"], self.embed_scale, status=self.status), None, [], None
         for w in layers:
             x, delta, s = self.layer.forward(x, w, delta, before)
