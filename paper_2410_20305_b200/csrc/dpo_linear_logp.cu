@@ -11,6 +11,9 @@
 // (a relative 2^-9 of each element, independent of one another), and both gradients are products with it.  dh is summed over
 // pieces in fp32; a piece of dW is complete.
 // Bound by the tensor cores: 2 n V D operations forward and 6 n V D backward for n labels; with few labels by the table's bytes.
+// Measured: 8499 labels of 16215 rows, 128256 x 4096, forward and backward 26.5 to 27.3 ms (1.31 to 1.35 PFLOP/s under the power cap);
+// 988 of 15154, forward, 655 us alone (1.57 PFLOP/s) and 800 to 840 under repetition; one label 207 to 221 us (the table at 6 TB/s in the
+// product); 1145 labels, 50257 x 1032, both 570 us; 206 labels, 1024 x 256, both 51.7 us (nine launches).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>

@@ -9,6 +9,8 @@
 //     dpw = gate A,  dpb = gate C,  dgate = pw A + pb C           (dgate = A without a norm).
 // Bound by HBM: forward two rows are read and two written, backward four and two.  Both norms of a row are taken while it is in
 // registers.  Sums are fp32, the variance after the mean.
+// Measured: 16215 x 4096 bf16 RMS forward 94 us (5.7 TB/s), one token 7.6 to 8.2; 31041 x 4096 layer norm with gate backward 377 us (4.0 TB/s: two
+// barriers for two rows, with as many warps as registers allow), RMS 329; 5465 x 1237 forward and backward 60.
 // Rows of any width are moved 16 bytes at a time (psa_vector.cuh): a row that starts `a` elements behind an aligned one is
 // taken as windows, window k holding the columns [k V - a, (k + 1) V - a).
 #include <cuda_bf16.h>

@@ -224,3 +224,24 @@ def test_pieces_of_the_vocabulary():
     far = lambda a, b: ((a.double() - b).norm() / b.norm()).item()  # noqa: E731
     # (2-norms: a rounding to bf16 of dz and one of the result, 2^-8 / sqrt(3) each at most, with dz's error no larger than its share)
     assert far(out, ro) <= 1e-5 and far(lse, rl) <= 1e-6 and far(dh, rdh) <= 4.5e-3 and far(dw, rdw) <= 4.5e-3, (far(dh, rdh), far(dw, rdw))
+
+
+def test_logits_of_minus_infinity_are_probabilities_of_none():
+    """Table rows of -inf against hidden rows without a zero or a negative value: what the other tokens' probabilities are."""
+    rng = np.random.default_rng(2)
+    bf = lambda a: torch.as_tensor(a, dtype=torch.float32).to(torch.bfloat16)  # noqa: E731
+    hidden, table = bf(rng.uniform(0.5, 1, size=(70, 64))), bf(rng.normal(size=(600, 64)))
+    banned = [0, 5, 255, 256, 599] + list(range(300, 400))
+    full = table.clone()
+    full[banned] = float("-inf")
+    rest = [v for v in range(600) if v not in banned]
+    targets = np.array([rest[i % len(rest)] for i in range(70)], dtype=np.int32)
+    targets[69] = 5
+    seg = np.zeros(70, np.int32)
+    seg[69] = 1
+    out, lse = O.dpo_linear_logp(hidden.cuda(), full.cuda(), i32(targets), i32(seg), 2)
+    where = {v: i for i, v in enumerate(rest)}
+    ro, rl = orc.linear_logp(f64(hidden)[:69], f64(table)[rest], [where[v] for v in targets[:69]], np.zeros(69, int), 1)
+    e = 64 * 2.0 ** -23 * (np.abs(f64(hidden)) @ np.abs(f64(table)).T).max() + 2.0 ** -16 + 2.0 ** -23 * np.abs(rl).max()
+    assert np.abs(f64(lse)[:69] - rl).max() <= e and np.isfinite(f64(lse)).all()
+    assert abs(float(out[0]) - ro[0]) <= 69 * 2 * e + 2.0 ** -23 * abs(ro[0]) and float(out[1]) == float("-inf")
