@@ -578,7 +578,8 @@ psa_status_t dpo_linear_logp(const void* hidden, const void* table, int64_t n_ro
  *   d_hidden      device bf16 [n_rows, width] (out): zeros in rows that score nothing
  *   d_table       device bf16 [vocab, width] (out), or NULL where it is not wanted
  *   workspace     device scratch of dpo_linear_logp_workspace_bytes(.., backward = 1) bytes, 16-byte aligned
- * No atomics on floats: the same inputs give the same bits.
+ * No atomics on floats: the same inputs give the same bits.  A table entry that is not finite reaches d_hidden as a product, so
+ * that a probability of 0 times -inf is NaN there.
  * Errors and the rest: as dpo_linear_logp (d_hidden, d_table: 16 bytes).
  */
 psa_status_t dpo_linear_logp_bwd(const float* coef, const void* hidden, const void* table, const float* lse,
