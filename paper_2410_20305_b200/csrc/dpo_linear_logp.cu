@@ -6,7 +6,8 @@
 // Labels first: one kernel lists them (a row's own label, then the forks), so that each is a row of its own of the products, and
 // a second copies their hidden rows side by side.  Rows that score nothing (the prompts) take part in nothing behind that.
 // Forward: a tile of 256 labels x 256 tokens of the vocabulary is summed in TMEM and leaves as each row's maximum and sum of
-// exponentials, and as the label's own logit where the tile holds it; a last kernel joins the parts of a row.
+// exponentials, the label's own left out; a last kernel joins the parts of a row.  With z the label's logit, a product of its own, its
+// term is -log(1 + sum over the other tokens of exp(z[t, v] - z)): nothing near 1 is rounded and subtracted where the label is nearly certain.
 // Backward: the logits once more, in pieces of the vocabulary; their tile leaves as dz, rounded to bf16 as tcgen05.mma takes it
 // (a relative 2^-9 of each element, independent of one another), and both gradients are products with it.  dh is summed over
 // pieces in fp32; a piece of dW is complete.
@@ -158,8 +159,7 @@ __host__ __device__ constexpr int64_t padded(int64_t n) { return (n + 255) / 256
 // The hidden rows of the labels side by side, zeros behind the last one to the next multiple of 256 (and in the first 256 where
 // there is no label).  For the backward pass what a label's row of dz takes: coef * scale and lse in units of log 2.  For the
 // forward the label's own product, by fp32 additions that round: tcgen05's cut off, which makes a logit smaller by about width * 1e-9
-// of itself (4.2e-6 at 4096, the same for all), and a log-probability near 0 is the difference of two such numbers (1.5e-4 of it at
-// width 4096 where the logit of 6 was taken from TMEM).
+// of itself (4.2e-6 at 4096), and a term near 0 is off, relative to itself, by the errors of the logits that it is taken from.
 // kWarps of a CTA's 8 take a row: all of them in a small call, where a row's trips to memory one after the other are what counts (one
 // row of 128256 x 4096: 223.6 -> 220.9 us in all).
 template <int kWarps>
@@ -244,8 +244,7 @@ struct ProductArgs {
   const Shared* shared;
   const int32_t* target;
   const float2* of_label;
-  float2* stats;          // [tiles of the vocabulary][l_pad]
-  float* picked;          // [l_pad]: the label's logit, in units of log 2
+  float2* stats;          // [tiles of the vocabulary][l_pad]: maximum and sum of exponentials, in units of log 2, without the label's own
   int64_t l_pad;
   int32_t hidden, columns, first_column;     // columns of this piece of the vocabulary, and where it starts
   int32_t splits;         // parts of dh's K, each with rows of its own of the output
@@ -455,7 +454,7 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
       if (*abort_flag) break;
       if (EPI == kEpiStats) {
         const int n_columns = args.columns - t.n0;       // of the vocabulary, from this tile on
-        float m = -INFINITY, sum = 0.f, label = 0.f;
+        float m = -INFINITY, sum = 0.f;
 #pragma unroll 1
         for (int c = 0; c < kTile; c += 64) {
           uint32_t v[64];
@@ -465,6 +464,11 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
           if (c + 64 > n_columns)
 #pragma unroll
             for (int j = 0; j < 64; ++j) z[j] = c + j < n_columns ? z[j] : -INFINITY;
+          const int at = y - c;
+          if (__any_sync(0xffffffffu, at >= 0 && at < 64)) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j) z[j] = j == at ? -INFINITY : z[j];
+          }
           float top[4] = {z[0], z[1], z[2], z[3]};
 #pragma unroll
           for (int j = 4; j < 64; j += 8)
@@ -479,16 +483,8 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
           for (int j = 0; j < 64; ++j) s[j & 3] += ex2_approx(fmaf(z[j], args.scale_log2, -shift));
           sum = (s[0] + s[1]) + (s[2] + s[3]);
           m = mn;
-          const int at = y - c;
-          if (__any_sync(0xffffffffu, at >= 0 && at < 64)) {
-#pragma unroll
-            for (int j = 0; j < 64; ++j) label = j == at ? z[j] : label;
-          }
         }
-        if (live && PSA_IN_BOUNDS(row, args.l_pad, args.status)) {
-          args.stats[int64_t(t.n0 / kTile) * args.l_pad + row] = make_float2(m, sum);
-          if (y >= 0 && y < kTile) args.picked[row] = label;
-        }
+        if (live && PSA_IN_BOUNDS(row, args.l_pad, args.status)) args.stats[int64_t(t.n0 / kTile) * args.l_pad + row] = make_float2(m, sum);
       } else if (EPI == kEpiGrad) {
 #pragma unroll 1
         for (int c = 0; c < kTile; c += 64, ++use) {
@@ -573,8 +569,8 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
 // sums and writes lse; the last CTA turns the sums into out.
 constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(32 * kJoinWarps)
-logp_join_kernel(const float2* stats, const float* picked, const float* label_logit, Labels labels, int64_t l_pad, int32_t v_tiles, int32_t n_rows,
-                 int32_t n_segments, float scale_log2, Sum* sums, float* out, float* lse) {
+logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, int64_t l_pad, int32_t v_tiles, int32_t n_rows, int32_t n_segments,
+                 float scale_log2, Sum* sums, float* out, float* lse) {
   __shared__ float2 s_part[kJoinWarps][32];
   __shared__ bool s_last;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -620,13 +616,22 @@ logp_join_kernel(const float2* stats, const float* picked, const float* label_lo
       for (int k = 0; k < kJoinWarps; ++k) all[k & 1] += s_part[k][lane].y * ex2_approx(s_part[k][lane].x - shift);
       s = all[0] + all[1];
       const int32_t t = labels.row[i];
-      // The label's logit as its own product in the place of the one from the tiles.  The maximum is taken off before anything is
-      // rounded to fp32: the term of a token that takes nearly all of the probability is near 0 itself, not the difference of two
-      // numbers like 50.
-      const double label = fma(double(label_logit[i]), double(scale_log2), -double(m));
-      const double summed = fma(double(picked[i]), double(scale_log2), -double(m));
-      const double corrected = double(s) + (exp2(label) - exp2(summed)), log2s = corrected < exp2(label) ? label : log2(corrected);
-      add_term(sums + labels.segment[i], (label - log2s) * kLn2);
+      // The other tokens' sum, s 2^m, against the label's own exponential; where that is far below it, the label's share of the row's sum is
+      // lost in any case.
+      const double label = double(label_logit[i]) * double(scale_log2), apart = label - double(m);
+      double term, row_lse;
+      if (apart > -512.0) {
+        const double others = log1p(double(s) * exp2(-apart));
+        term = -others;
+        row_lse = label * kLn2 + others;
+      } else {
+        const double log2s = log2(double(s));
+        term = (apart - log2s) * kLn2;
+        row_lse = (double(m) + log2s) * kLn2;
+      }
+      // (a label of +inf is not finite, and beside others of -inf alone one of -inf has nothing to be compared with)
+      if (!(label < INFINITY) || apart != apart) term = row_lse = NAN;
+      add_term(sums + labels.segment[i], term);
       // a row that several labels score has it from its own one, or else from the first fork
       const int32_t state = labels.state[t];
       bool writes = (state >> 1) == i + 1;
@@ -634,7 +639,7 @@ logp_join_kernel(const float2* stats, const float* picked, const float* label_lo
         writes = true;
         for (int32_t k = labels.shared->n_own; k < i; ++k) writes &= labels.row[k] != t;
       }
-      if (writes) lse[t] = float((double(m) + log2s) * kLn2);
+      if (writes) lse[t] = float(row_lse);
     }
   }
   __threadfence();
@@ -691,7 +696,7 @@ struct Workspace {
   int64_t piece;                 // columns of a piece of the vocabulary
   int64_t pitch;                 // of the labels' rows: whole lines of 128 bytes
   int32_t splits;
-  size_t row, target, segment, state, sums, rows, stats, picked, label_logit, of_label, dz, parts, total;
+  size_t row, target, segment, state, sums, rows, stats, label_logit, of_label, dz, parts, total;
   Workspace(int64_t n_rows, int64_t n_forks, int64_t n_segments, int64_t vocab, int64_t hidden, bool backward) {
     l_pad = std::max<int64_t>(256, padded(n_rows + n_forks));
     const int64_t most = std::max<int64_t>(256, kPieceBytes / (2 * l_pad) / 256 * 256), pieces = (vocab + most - 1) / most;
@@ -707,7 +712,7 @@ struct Workspace {
     state = take(n_rows * 4);
     pitch = (hidden + 63) / 64 * 64;
     rows = take(l_pad * pitch * 2);
-    sums = stats = picked = label_logit = of_label = dz = parts = 0;
+    sums = stats = label_logit = of_label = dz = parts = 0;
     if (backward) {
       of_label = take(l_pad * sizeof(float2));
       dz = take(l_pad * piece * 2);
@@ -715,7 +720,6 @@ struct Workspace {
     } else {
       sums = take(n_segments * sizeof(Sum));
       stats = take(size_t((vocab + kTile - 1) / kTile) * l_pad * sizeof(float2));
-      picked = take(l_pad * 4);
       label_logit = take(l_pad * 4);
     }
     total = at;
@@ -805,13 +809,12 @@ psa_status_t forward(const Call& c, float* out, float* lse) {
   ProductArgs a = common_args(c, w);
   a.columns = int32_t(c.vocab);
   a.stats = reinterpret_cast<float2*>(c.ws + w.stats);
-  a.picked = reinterpret_cast<float*>(c.ws + w.picked);
   if (!operand_maps(&a.of[0].a, c.ws + w.rows, false, w.l_pad, c.width, 128, w.pitch) ||
       !operand_maps(&a.of[0].b, c.table, false, c.vocab, c.width, 128))
     return PSA_ERR_CUDA;
   const int64_t v_tiles = (c.vocab + kTile - 1) / kTile;
   if (!launch_product<kEpiStats>(a, w.l_pad / kTile * v_tiles, c.stream)) return failed_launch("dpo_linear_logp product");
-  launch_behind(true, logp_join_kernel, dim3(unsigned(w.l_pad / 32)), 32 * kJoinWarps, 0, c.stream, a.stats, a.picked,
+  launch_behind(true, logp_join_kernel, dim3(unsigned(w.l_pad / 32)), 32 * kJoinWarps, 0, c.stream, a.stats,
                 reinterpret_cast<const float*>(c.ws + w.label_logit), w.labels(c.ws), w.l_pad,
                 int32_t(v_tiles), int32_t(c.n_rows), c.n_segments, a.scale_log2, reinterpret_cast<Sum*>(c.ws + w.sums), out, lse);
   return check_last_cuda_error("dpo_linear_logp launch");

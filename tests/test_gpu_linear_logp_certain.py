@@ -1,0 +1,87 @@
+"""dpo_linear_logp where a token takes nearly all of a row's probability: the log-probability is then what is left for the others,
+1 - p, and is held relative to that.
+
+Bounds.  With z the label's logit and r = (1 - p) / p the sum of exp(z[v] - z) over the other tokens, a term is -log(1 + r).
+The label's own product is taken by fp32 additions, width / 256 of them in a row and 11 that join threads at most: off by
+(width / 256 + 11) 2^-24 of its sum of magnitudes.  Another token's logit comes from the tensor cores: off by width * 2^-23 of its own.  An
+exponent's argument is rounded to 2^-22 of itself, the scale's division by log 2 counted, and 2^-16 covers the exponential and the sums.
+r is off by the sum of these, relative to itself, the term by no more, and then by half a unit of 2^-40 and a rounding to fp32."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_linear_logp import both, f64, within
+
+pytestmark = pytest.mark.gpu
+
+NONE = [np.zeros(0, np.int32)] * 3
+
+
+def certain(n, width, vocab, low, high, seed):
+    """(hidden, table, targets): row t's token has the table's row along hidden[t], so long that 1 - p is about low .. high; the
+    other rows of the table are short."""
+    rng = np.random.default_rng(seed)
+    bf = lambda a: torch.as_tensor(a, dtype=torch.float32).to(torch.bfloat16)  # noqa: E731
+    hidden = bf(rng.normal(size=(n, width)))
+    h = hidden.double().numpy()
+    table = rng.normal(size=(vocab, width)) * 0.05 * width ** -0.5
+    targets = rng.permutation(vocab)[:n].astype(np.int32)
+    left = np.exp(np.linspace(np.log(low), np.log(high), n))
+    table[targets] = h / (h ** 2).sum(1, keepdims=True) * np.log(vocab / left)[:, None]
+    return hidden, bf(table), targets
+
+
+def terms(hidden, table, rows, targets, scale):
+    """Per label in 64 bits: z of every token, lse, 1 - p of the label, and the bounds of the label's product and of the others' logits."""
+    h, w = f64(hidden)[rows], f64(table)
+    z, size = scale * h @ w.T, scale * np.abs(h) @ np.abs(w).T
+    at = np.arange(len(rows))
+    own = z[at, targets]
+    apart = z - own[:, None]
+    apart[at, targets] = -np.inf
+    r = np.exp(apart).sum(1)
+    width = h.shape[1]
+    e_own = (width / 256 + 11) * 2.0 ** -24 * size[at, targets]
+    return z, own + np.log1p(r), r, e_own, width * 2.0 ** -23 * size
+
+
+def logp_bound(z, r, e_own, e, at, targets):
+    """Of a term -log1p(r)."""
+    own = z[at, targets]
+    rel = 2.0 ** -16 + e.max(1) + e_own + 2.0 ** -22 * (np.abs(z).max(1) + np.abs(own))
+    return np.log1p(r) * 1.01 * rel + 2.0 ** -41 + 2.0 ** -24 * np.log1p(r)
+
+
+@pytest.mark.parametrize("n,width,vocab,scale", [(200, 4096, 700, 1.0), (60, 64, 300, 1.0), (90, 1032, 2049, 0.5), (2500, 256, 3001, 1.0)])
+def test_log_probabilities_near_zero(n, width, vocab, scale):
+    hidden, table, targets = certain(n, width, vocab, 1e-8, 1e-1, n + width)
+    if scale != 1.0:
+        hidden = (hidden / scale).contiguous()
+    seg = np.arange(n, dtype=np.int32)
+    out, lse, _, _, status = both(hidden, table, targets, seg, NONE, np.ones(n, np.float32), scale=scale)
+    at = np.arange(n)
+    z, rl, r, e_own, e = terms(hidden, table, at, targets, scale)
+    assert status == 0 and r.min() < 1e-7 and r.max() > 1e-2
+    within("out", out, -np.log1p(r), logp_bound(z, r, e_own, e, at, targets))
+    within("lse", lse, rl, e_own + np.log1p(r) * (2.0 ** -16 + e.max(1)) + 2.0 ** -22 * np.abs(rl))
+
+
+def test_a_label_with_nothing_beside_it():
+    """A vocabulary of one token, other tokens of probability 0, and a label whose own logit is infinite."""
+    rng = np.random.default_rng(3)
+    bf = lambda a: torch.as_tensor(a, dtype=torch.float32).to(torch.bfloat16)  # noqa: E731
+    hidden, table = bf(rng.uniform(0.5, 1, size=(40, 72))), bf(rng.normal(size=(300, 72)))
+    seg = np.arange(40, dtype=np.int32)
+    bound = (72 / 256 + 11) * 2.0 ** -24 * (f64(hidden) @ np.abs(f64(table)).T).max() + 2.0 ** -22 * 88
+    out, lse, dh, dw, _ = both(hidden, table[:1].contiguous(), np.zeros(40, np.int32), seg, NONE, np.ones(40, np.float32))
+    z = f64(hidden) @ f64(table).T
+    assert not out.any() and np.abs(f64(lse) - z[:, 0]).max() <= bound
+    assert np.abs(f64(dh)).max() <= 2 * bound * np.abs(f64(table)).max() and np.abs(f64(dw)).max() <= 40 * 2 * bound
+    alone = torch.full_like(table, float("-inf"))
+    alone[257] = table[257]
+    out, lse, *_ = both(hidden, alone, np.full(40, 257, np.int32), seg, NONE, np.ones(40, np.float32))
+    assert not out.any() and np.abs(f64(lse) - z[:, 257]).max() <= bound
+    above = table.clone()
+    above[257] = float("inf")
+    out, lse, *_ = both(hidden, above, np.full(40, 257, np.int32), seg, NONE, np.ones(40, np.float32))
+    assert out.isnan().all() and lse.isnan().all()
