@@ -157,15 +157,17 @@ logp_list_kernel(const int32_t* targets, const int32_t* segment_ids, const int32
 __host__ __device__ constexpr int64_t padded(int64_t n) { return (n + 255) / 256 * 256; }
 
 // The hidden rows of the labels side by side, zeros behind the last one to the next multiple of 256 (and in the first 256 where
-// there is no label).  For the backward pass what a label's row of dz takes: coef * scale and lse in units of log 2.  For the
-// forward the label's own product, by fp32 additions that round: tcgen05's cut off, which makes a logit smaller by about width * 1e-9
-// of itself (4.2e-6 at 4096), and a term near 0 is off, relative to itself, by the errors of the logits that it is taken from.
+// there is no label), and the label's own product, by fp32 additions that round: tcgen05's cut off, which makes a logit smaller by about
+// width * 1e-9 of itself (4.2e-6 at 4096), and what is left of a nearly certain label's probability is off, relative to itself, by the errors
+// of the logits that it is taken from.  For the backward pass what a label's row of dz takes: coef * scale, lse in units of log 2, and
+// its element at the label, coef * scale * (1 - p) from the product that the forward took lse from (from tcgen05's, 1 - p was 84 % too large
+// at 1e-4 and a logit of 20).
 // kWarps of a CTA's 8 take a row: all of them in a small call, where a row's trips to memory one after the other are what counts (one
 // row of 128256 x 4096: 223.6 -> 220.9 us in all).
 template <int kWarps>
 __global__ void __launch_bounds__(256)
 logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32_t vectors, int32_t pitch, uint4* rows, const float* coef, const float* lse,
-                   float scale, float2* of_label, float* label_logit) {
+                   float scale, float2* of_label, float* label_value) {
   constexpr int kThreads = 32 * kWarps;
   __shared__ float s_sum[8];
   const int tid = int(threadIdx.x) % kThreads, lane = threadIdx.x & 31;
@@ -180,13 +182,7 @@ logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32
     return;
   }
   const int32_t t = labels.row[i];
-  if (of_label && tid == 0) of_label[i] = make_float2(coef[labels.segment[i]] * scale, lse[t] * kLog2e);
   const uint4* from = hidden + int64_t(t) * vectors;
-  if (!label_logit) {
-#pragma unroll 4
-    for (int c = tid; c < vectors; c += kThreads) to[c] = from[c];
-    return;
-  }
   const uint4* weight = table + int64_t(labels.target[i]) * vectors;
   float sum[8] = {};
 #pragma unroll 4
@@ -208,7 +204,17 @@ logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32
     __syncthreads();
     all = ((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3])) + ((s_sum[4] + s_sum[5]) + (s_sum[6] + s_sum[7]));
   }
-  if (tid == 0) label_logit[i] = all;
+  if (tid != 0) return;
+  if (!coef) {
+    label_value[i] = all;
+    return;
+  }
+  const float c = coef[labels.segment[i]] * scale, of_row = lse[t];
+  // (as the forward scales it; where fp32 does not tell it from lse, p is 1)
+  const double z = double(all) * double(scale * kLog2e) * kLn2;
+  const float logp = float(z) == of_row ? 0.f : float(z - double(of_row));
+  of_label[i] = make_float2(c, of_row * kLog2e);
+  label_value[i] = -c * expm1f(logp > 0.f ? 0.f : logp);      // (NaN stays)
 }
 
 // ---------------------------------------------------------------- products
@@ -244,6 +250,7 @@ struct ProductArgs {
   const Shared* shared;
   const int32_t* target;
   const float2* of_label;
+  const float* label_dz;
   float2* stats;          // [tiles of the vocabulary][l_pad]: maximum and sum of exponentials, in units of log 2, without the label's own
   int64_t l_pad;
   int32_t hidden, columns, first_column;     // columns of this piece of the vocabulary, and where it starts
@@ -445,9 +452,13 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
       const bool live = row < n_labels;
       int y = -1;
       float2 own = make_float2(0.f, 0.f);
+      float own_dz = 0.f;
       if (EPI != kEpiOut && live && PSA_IN_BOUNDS(row, args.l_pad, args.status)) {
         y = args.target[row] - args.first_column - t.n0;      // the label's column in the tile
-        if (EPI == kEpiGrad) own = args.of_label[row];
+        if (EPI == kEpiGrad) {
+          own = args.of_label[row];
+          own_dz = args.label_dz[row];
+        }
       }
       mbar_wait(acc_full(i & 1), (i >> 1) & 1, wctx);
       tc_fence_after();
@@ -497,7 +508,7 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
           const int at = y - c;
           if (__any_sync(0xffffffffu, at >= 0 && at < 64)) {
 #pragma unroll
-            for (int j = 0; j < 64; ++j) z[j] += j == at ? own.x : 0.f;
+            for (int j = 0; j < 64; ++j) z[j] = j == at ? own_dz : z[j];
           }
           if (!live)      // zeros, whatever the table holds
 #pragma unroll
@@ -696,7 +707,7 @@ struct Workspace {
   int64_t piece;                 // columns of a piece of the vocabulary
   int64_t pitch;                 // of the labels' rows: whole lines of 128 bytes
   int32_t splits;
-  size_t row, target, segment, state, sums, rows, stats, label_logit, of_label, dz, parts, total;
+  size_t row, target, segment, state, sums, rows, stats, label_value, of_label, dz, parts, total;
   Workspace(int64_t n_rows, int64_t n_forks, int64_t n_segments, int64_t vocab, int64_t hidden, bool backward) {
     l_pad = std::max<int64_t>(256, padded(n_rows + n_forks));
     const int64_t most = std::max<int64_t>(256, kPieceBytes / (2 * l_pad) / 256 * 256), pieces = (vocab + most - 1) / most;
@@ -712,7 +723,8 @@ struct Workspace {
     state = take(n_rows * 4);
     pitch = (hidden + 63) / 64 * 64;
     rows = take(l_pad * pitch * 2);
-    sums = stats = label_logit = of_label = dz = parts = 0;
+    label_value = take(l_pad * 4);
+    sums = stats = of_label = dz = parts = 0;
     if (backward) {
       of_label = take(l_pad * sizeof(float2));
       dz = take(l_pad * piece * 2);
@@ -720,7 +732,6 @@ struct Workspace {
     } else {
       sums = take(n_segments * sizeof(Sum));
       stats = take(size_t((vocab + kTile - 1) / kTile) * l_pad * sizeof(float2));
-      label_logit = take(l_pad * 4);
     }
     total = at;
   }
@@ -774,7 +785,7 @@ bool launch_labels(const Call& c, const Workspace& w, bool backward, const float
   return launch_behind(true, few ? logp_gather_kernel<8> : logp_gather_kernel<1>, dim3(unsigned(few ? w.l_pad : w.l_pad / 8)), 256, 0, c.stream, static_cast<const uint4*>(c.hidden),
                        static_cast<const uint4*>(c.table), labels, c.width / 8, int32_t(w.pitch / 8), reinterpret_cast<uint4*>(c.ws + w.rows), coef, lse, c.scale,
                        backward ? reinterpret_cast<float2*>(c.ws + w.of_label) : nullptr,
-                       backward ? nullptr : reinterpret_cast<float*>(c.ws + w.label_logit)) == cudaSuccess;
+                       reinterpret_cast<float*>(c.ws + w.label_value)) == cudaSuccess;
 }
 
 template <int EPI>
@@ -815,7 +826,7 @@ psa_status_t forward(const Call& c, float* out, float* lse) {
   const int64_t v_tiles = (c.vocab + kTile - 1) / kTile;
   if (!launch_product<kEpiStats>(a, w.l_pad / kTile * v_tiles, c.stream)) return failed_launch("dpo_linear_logp product");
   launch_behind(true, logp_join_kernel, dim3(unsigned(w.l_pad / 32)), 32 * kJoinWarps, 0, c.stream, a.stats,
-                reinterpret_cast<const float*>(c.ws + w.label_logit), w.labels(c.ws), w.l_pad,
+                reinterpret_cast<const float*>(c.ws + w.label_value), w.labels(c.ws), w.l_pad,
                 int32_t(v_tiles), int32_t(c.n_rows), c.n_segments, a.scale_log2, reinterpret_cast<Sum*>(c.ws + w.sums), out, lse);
   return check_last_cuda_error("dpo_linear_logp launch");
 }
@@ -832,6 +843,7 @@ psa_status_t backward(const Call& c, const float* coef, const float* lse, void* 
     a.columns = int32_t(columns);
     a.first_column = int32_t(first);
     a.of_label = reinterpret_cast<float2*>(c.ws + w.of_label);
+    a.label_dz = reinterpret_cast<float*>(c.ws + w.label_value);
     if (!operand_maps(&a.of[0].a, c.ws + w.rows, false, w.l_pad, c.width, 128, w.pitch) ||
         !operand_maps(&a.of[0].b, table, false, columns, c.width, 128) ||
         !matrix_map(&a.of[0].store, c.ws + w.dz, w.l_pad, columns, 32, 64, w.piece))

@@ -1,16 +1,18 @@
-"""dpo_linear_logp where a token takes nearly all of a row's probability: the log-probability is then what is left for the others,
-1 - p, and is held relative to that.
+"""dpo_linear_logp and dpo_linear_logp_bwd where a token takes nearly all of a row's probability: the log-probability and the gradient
+are then what is left for the others, 1 - p, and are held relative to that.
 
 Bounds.  With z the label's logit and r = (1 - p) / p the sum of exp(z[v] - z) over the other tokens, a term is -log(1 + r).
 The label's own product is taken by fp32 additions, width / 256 of them in a row and 11 that join threads at most: off by
 (width / 256 + 11) 2^-24 of its sum of magnitudes.  Another token's logit comes from the tensor cores: off by width * 2^-23 of its own.  An
 exponent's argument is rounded to 2^-22 of itself, the scale's division by log 2 counted, and 2^-16 covers the exponential and the sums.
-r is off by the sum of these, relative to itself, the term by no more, and then by half a unit of 2^-40 and a rounding to fp32."""
+r is off by the sum of these, relative to itself, the term by no more, and then by half a unit of 2^-40 and a rounding to fp32.
+In the gradient the label's element c (1 - p) is taken from its own product and lse as fp32 holds it: off by p times the product's error, the
+error of lse and 2^-23 of |z| and |lse|; the other elements as in test_gpu_linear_logp.py."""
 import numpy as np
 import pytest
 import torch
 
-from test_gpu_linear_logp import both, f64, within
+from test_gpu_linear_logp import H8, both, f64, within
 
 pytestmark = pytest.mark.gpu
 
@@ -64,6 +66,34 @@ def test_log_probabilities_near_zero(n, width, vocab, scale):
     assert status == 0 and r.min() < 1e-7 and r.max() > 1e-2
     within("out", out, -np.log1p(r), logp_bound(z, r, e_own, e, at, targets))
     within("lse", lse, rl, e_own + np.log1p(r) * (2.0 ** -16 + e.max(1)) + 2.0 ** -22 * np.abs(rl))
+
+
+def gradient(hidden, table, rows, targets, c, scale):
+    """Rows of d_hidden per label in 64 bits and their bounds."""
+    z, rl, r, e_own, e = terms(hidden, table, rows, targets, scale)
+    w, at = f64(table), np.arange(len(rows))
+    p = np.exp(z - rl[:, None])
+    e_lse = e_own + np.log1p(r) * (2.0 ** -16 + e.max(1)) + 2.0 ** -23 * np.abs(rl)
+    dz = -p
+    dz[at, targets] = r / (1 + r)
+    e_dz = 1.01 * p * (e + e_lse[:, None] + 2.0 ** -16) + 2.0 ** -22 * p
+    e_dz[at, targets] = 1.01 * p[at, targets] * (e_own + e_lse + 2.0 ** -23 * (np.abs(z[at, targets]) + np.abs(rl))) + 2.0 ** -22 * np.abs(dz[at, targets])
+    e_dz += H8 * np.abs(dz) + len(w) * 2.0 ** -23 * np.abs(dz)
+    c = scale * c[:, None]
+    ref = (c * dz) @ w
+    return ref, np.abs(c) * e_dz @ np.abs(w) + H8 * np.abs(ref) + 1e-30
+
+
+@pytest.mark.parametrize("n,width,vocab,scale", [(200, 4096, 700, 1.0), (60, 64, 300, 1.0), (90, 2056, 2049, 0.5)])
+def test_gradients_of_log_probabilities_near_zero(n, width, vocab, scale):
+    hidden, table, targets = certain(n, width, vocab, 1e-5, 1e-2, n + width)
+    if scale != 1.0:
+        hidden = (hidden / scale).contiguous()
+    coef = np.random.default_rng(1).uniform(0.5, 2, size=n).astype(np.float32)
+    _, _, dh, _, status = both(hidden, table, targets, np.arange(n, dtype=np.int32), NONE, coef, scale=scale)
+    ref, tol = gradient(hidden, table, np.arange(n), targets, coef.astype(float), scale)
+    assert status == 0
+    within("d_hidden", dh, ref, tol)
 
 
 def test_a_label_with_nothing_beside_it():
