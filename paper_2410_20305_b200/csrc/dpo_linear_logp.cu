@@ -48,7 +48,21 @@ struct Labels {
   Shared* shared;
   int32_t *row, *target, *segment;   // of each label: own labels in the rows' order, then the forks'
   int32_t* state;                    // of each row of hidden: twice (its own label + 1, 0 without one), + 1 where a fork names it
+  unsigned long long* best;          // forward, of each row that a fork names: the largest of its labels' ranked()
 };
+// A label's logit and the row's lse as it finds it, so that the largest is that of the likeliest label (or a NaN).  That label's logit is
+// a product of its own in its lse, the row's other labels' are not: theirs weigh least.
+__device__ __forceinline__ uint32_t rising(float v) {      // in the order of floats
+  const uint32_t bits = __float_as_uint(v);
+  return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+}
+__device__ __forceinline__ unsigned long long ranked(float logit, float lse) {
+  return static_cast<unsigned long long>(rising(logit)) << 32 | rising(lse);
+}
+__device__ __forceinline__ float lse_of(unsigned long long rank) {
+  const uint32_t bits = uint32_t(rank);
+  return __uint_as_float(bits & 0x80000000u ? bits & 0x7fffffffu : ~bits);
+}
 
 // The sum of a response's terms as whole numbers, which do not depend on their order: floor(term) and its rest in units of 2^-40,
 // a term taken as -2^38 where it is below (2^24 labels then stay within 64 bits).
@@ -143,7 +157,10 @@ logp_list_kernel(const int32_t* targets, const int32_t* segment_ids, const int32
           labels.segment[place] = g[j];
         }
         if (!list && row[j] >= 0) labels.state[row[j]] = valid ? 2 * (place + 1) : 0;
-        if (list && valid) atomicOr(labels.state + row[j], 1);
+        if (list && valid) {
+          atomicOr(labels.state + row[j], 1);
+          if (labels.best) labels.best[row[j]] = 0;
+        }
       }
 #pragma unroll
       for (int w = 0; w < kCounts / 32; ++w) base += s_warp[w];
@@ -577,7 +594,7 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
 
 // ---------------------------------------------------------------- ends
 // Joins the parts of 32 labels' rows (a lane each, the warps share the vocabulary's tiles), adds their terms to the responses'
-// sums and writes lse; the last CTA turns the sums into out.
+// sums and writes lse; the last CTA turns the sums into out, and writes lse of the rows that forks name.
 constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(32 * kJoinWarps)
 logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, int64_t l_pad, int32_t v_tiles, int32_t n_rows, int32_t n_segments,
@@ -626,7 +643,6 @@ logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, i
 #pragma unroll
       for (int k = 0; k < kJoinWarps; ++k) all[k & 1] += s_part[k][lane].y * ex2_approx(s_part[k][lane].x - shift);
       s = all[0] + all[1];
-      const int32_t t = labels.row[i];
       // The other tokens' sum, s 2^m, against the label's own exponential; where that is far below it, the label's share of the row's sum is
       // lost in any case.
       const double label = double(label_logit[i]) * double(scale_log2), apart = label - double(m);
@@ -643,14 +659,9 @@ logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, i
       // (a label of +inf is not finite, and beside others of -inf alone one of -inf has nothing to be compared with)
       if (!(label < INFINITY) || apart != apart) term = row_lse = NAN;
       add_term(sums + labels.segment[i], term);
-      // a row that several labels score has it from its own one, or else from the first fork
-      const int32_t state = labels.state[t];
-      bool writes = (state >> 1) == i + 1;
-      if (state == 1) {
-        writes = true;
-        for (int32_t k = labels.shared->n_own; k < i; ++k) writes &= labels.row[k] != t;
-      }
-      if (writes) lse[t] = float(row_lse);
+      const int32_t t = labels.row[i];
+      if (labels.state[t] & 1) atomicMax(labels.best + t, ranked(label_logit[i], float(row_lse)));      // (several labels may score it)
+      else lse[t] = float(row_lse);
     }
   }
   __threadfence();
@@ -662,6 +673,10 @@ logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, i
   for (int g = threadIdx.x; g < n_segments; g += blockDim.x) {
     const Sum s{__ldcg(&sums[g].whole), __ldcg(&sums[g].rest), __ldcg(&sums[g].odd), 0};
     out[g] = sum_of(s);
+  }
+  for (int32_t k = labels.shared->n_own + int32_t(threadIdx.x); k < n; k += blockDim.x) {
+    const int32_t t = labels.row[k];
+    lse[t] = lse_of(__ldcg(labels.best + t));
   }
 }
 
@@ -707,7 +722,7 @@ struct Workspace {
   int64_t piece;                 // columns of a piece of the vocabulary
   int64_t pitch;                 // of the labels' rows: whole lines of 128 bytes
   int32_t splits;
-  size_t row, target, segment, state, sums, rows, stats, label_value, of_label, dz, parts, total;
+  size_t row, target, segment, state, best, sums, rows, stats, label_value, of_label, dz, parts, total;
   Workspace(int64_t n_rows, int64_t n_forks, int64_t n_segments, int64_t vocab, int64_t hidden, bool backward) {
     l_pad = std::max<int64_t>(256, padded(n_rows + n_forks));
     const int64_t most = std::max<int64_t>(256, kPieceBytes / (2 * l_pad) / 256 * 256), pieces = (vocab + most - 1) / most;
@@ -724,12 +739,13 @@ struct Workspace {
     pitch = (hidden + 63) / 64 * 64;
     rows = take(l_pad * pitch * 2);
     label_value = take(l_pad * 4);
-    sums = stats = of_label = dz = parts = 0;
+    best = sums = stats = of_label = dz = parts = 0;
     if (backward) {
       of_label = take(l_pad * sizeof(float2));
       dz = take(l_pad * piece * 2);
       parts = take(size_t(splits) * l_pad * hidden * 4);
     } else {
+      best = take(n_rows * 8);
       sums = take(n_segments * sizeof(Sum));
       stats = take(size_t((vocab + kTile - 1) / kTile) * l_pad * sizeof(float2));
     }
@@ -737,7 +753,8 @@ struct Workspace {
   }
   Labels labels(char* ws) const {
     auto ints = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
-    return Labels{reinterpret_cast<Shared*>(ws), ints(row), ints(target), ints(segment), ints(state)};
+    return Labels{reinterpret_cast<Shared*>(ws), ints(row), ints(target), ints(segment), ints(state),
+                  best ? reinterpret_cast<unsigned long long*>(ws + best) : nullptr};
   }
 };
 

@@ -96,6 +96,30 @@ def test_gradients_of_log_probabilities_near_zero(n, width, vocab, scale):
     within("d_hidden", dh, ref, tol)
 
 
+@pytest.mark.parametrize("own", [True, False])
+def test_forks_that_are_nearly_certain(own):
+    """A row whose own label, or first fork, is improbable, and a later fork nearly certain: lse and the fork's gradient."""
+    n, width, vocab = 120, 4096, 700
+    hidden, table, sure = certain(n, width, vocab, 1e-5, 1e-2, 7)
+    rng = np.random.default_rng(2)
+    away = np.setdiff1d(np.arange(vocab), sure)[:n].astype(np.int32)
+    coef = rng.uniform(0.5, 2, size=n + 1).astype(np.float32)
+    coef[n] = 0      # of the improbable labels
+    rows, seg = np.arange(n, dtype=np.int32), np.arange(n, dtype=np.int32)
+    if own:
+        labels, forks = (away, np.full(n, n, np.int32)), [rows, sure, seg]
+    else:
+        labels = (away, np.full(n, -1, np.int32))
+        forks = [np.concatenate(a).astype(np.int32) for a in ((rows, rows), (away, sure), (np.full(n, n), seg))]
+    out, lse, dh, _, status = both(hidden, table, *labels, forks, coef)
+    z, rl, r, e_own, e = terms(hidden, table, rows, sure, 1.0)
+    assert status == 0
+    within("out", out[:n], -np.log1p(r), logp_bound(z, r, e_own, e, rows, sure))
+    within("lse", lse, rl, e_own + np.log1p(r) * (2.0 ** -16 + e.max(1)) + 2.0 ** -22 * np.abs(rl))
+    ref, tol = gradient(hidden, table, rows, sure, coef[:n].astype(float), 1.0)
+    within("d_hidden", dh, ref, tol)
+
+
 def test_a_label_with_nothing_beside_it():
     """A vocabulary of one token, other tokens of probability 0, and a label whose own logit is infinite."""
     rng = np.random.default_rng(3)
