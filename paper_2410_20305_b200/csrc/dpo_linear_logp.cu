@@ -47,7 +47,10 @@ struct Shared {
 struct Labels {
   Shared* shared;
   int32_t *row, *target, *segment;   // of each label: own labels in the rows' order, then the forks'
-  int32_t* state;                    // of each row of hidden: twice (its own label + 1, 0 without one), + 1 where a fork names it
+  // Of each row of hidden: its own label + 1 (0 without one), and the label of a fork that names it + 1 (0 without one), from which `next`
+  // (backward) leads to the others, in no order.
+  int2* state;
+  int32_t* next;
   unsigned long long* best;          // forward, of each row that a fork names: the largest of its labels' ranked()
 };
 // A label's logit and the row's lse as it finds it, so that the largest is that of the likeliest label (or a NaN).  That label's logit is
@@ -156,9 +159,10 @@ logp_list_kernel(const int32_t* targets, const int32_t* segment_ids, const int32
           labels.target[place] = y[j];
           labels.segment[place] = g[j];
         }
-        if (!list && row[j] >= 0) labels.state[row[j]] = valid ? 2 * (place + 1) : 0;
+        if (!list && row[j] >= 0) labels.state[row[j]] = make_int2(valid ? place + 1 : 0, 0);
         if (list && valid) {
-          atomicOr(labels.state + row[j], 1);
+          const int32_t other = atomicExch(&labels.state[row[j]].y, place + 1);
+          if (labels.next) labels.next[place] = other;
           if (labels.best) labels.best[row[j]] = 0;
         }
       }
@@ -607,7 +611,7 @@ logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, i
   const int32_t n = labels.shared->n_labels, i = int32_t(blockIdx.x) * 32 + lane;
   // rows that score nothing
   for (int64_t t = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; t < n_rows; t += int64_t(gridDim.x) * blockDim.x)
-    if (labels.state[t] == 0) lse[t] = 0.f;
+    if ((labels.state[t].x | labels.state[t].y) == 0) lse[t] = 0.f;
   if (int32_t(blockIdx.x) * 32 < n) {
     float m = -INFINITY, s = 0.f;
     auto merge = [&](float2 p) {
@@ -660,7 +664,7 @@ logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, i
       if (!(label < INFINITY) || apart != apart) term = row_lse = NAN;
       add_term(sums + labels.segment[i], term);
       const int32_t t = labels.row[i];
-      if (labels.state[t] & 1) atomicMax(labels.best + t, ranked(label_logit[i], float(row_lse)));      // (several labels may score it)
+      if (labels.state[t].y) atomicMax(labels.best + t, ranked(label_logit[i], float(row_lse)));      // (several labels may score it)
       else lse[t] = float(row_lse);
     }
   }
@@ -680,7 +684,9 @@ logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, i
   }
 }
 
-// dh of every row of hidden: the parts of its own label and of the forks that name it, in that order; zeros where it scores nothing.
+// dh of every row of hidden: the sum over its own label and the forks that name it, each the sum of its parts; zeros where it scores nothing.
+// Two labels are added as they come.  More, which are listed in no order, as whole numbers: the largest magnitude of a column gives a unit in which
+// all of them stay within 62 bits and lose what is 2^-35 of it at most, so that their sum depends on no order.
 __global__ void __launch_bounds__(256)
 logp_scatter_kernel(const float* parts, Labels labels, int32_t n_rows, int32_t hidden, int64_t l_pad,
                     int32_t splits, uint4* d_hidden) {
@@ -689,25 +695,66 @@ logp_scatter_kernel(const float* parts, Labels labels, int32_t n_rows, int32_t h
   behind_wait();
   behind_go();
   if (t >= n_rows) return;
-  const int32_t state = labels.state[t], n = labels.shared->n_labels, vectors = hidden / 8;
-  for (int first = 0; first < vectors; first += 32) {
-    const int c = first + lane;
+  const int2 state = labels.state[t];
+  const int c = int(blockIdx.y) * 32 + lane, vectors = hidden / 8;
+  if (c >= vectors) return;
+  auto part = [&](int32_t label, int p, int at) { return parts + (p * l_pad + label) * int64_t(hidden) + at; };
+  if (!state.y || !labels.next[state.y - 1]) {
     float sum[8] = {};
-    auto add = [&](int32_t i) {
-      for (int p = 0; c < vectors && p < splits; ++p) {
-        const float4* from = reinterpret_cast<const float4*>(parts + (p * l_pad + i) * int64_t(hidden) + 8 * c);
+    auto add = [&](int32_t label) {
+      float v[8] = {};
+      for (int p = 0; p < splits; ++p) {
+        const float4* from = reinterpret_cast<const float4*>(part(label, p, 8 * c));
         const float4 a = from[0], b = from[1];
-        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] += v[j];
+        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+        v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += v[j];
     };
-    if (state >> 1) add((state >> 1) - 1);
-    if (state & 1)
-      for (int32_t k = labels.shared->n_own; k < n; k += 32)
-        for (uint32_t found = __ballot_sync(0xffffffffu, k + lane < n && labels.row[min(k + lane, n - 1)] == t); found; found &= found - 1)
-          add(k + __ffs(found) - 1);
-    if (c < vectors) d_hidden[t * vectors + c] = pack8(sum);
+    if (state.x) add(state.x - 1);
+    if (state.y) add(state.y - 1);
+    d_hidden[t * vectors + c] = pack8(sum);
+    return;
+  }
+#pragma unroll 1
+  for (int at = 8 * c; at < 8 * c + 8; at += 2) {
+    auto all = [&](auto&& take) {      // calls take() with the two columns of each label; the number of labels
+      uint32_t n = 0;
+      for (int32_t i = state.x, k = state.y; i || k; ++n) {
+        const int32_t label = (i ? i : k) - 1;
+        if (i) i = 0;
+        else k = labels.next[label];
+        float v[2] = {};
+        for (int p = 0; p < splits; ++p) {
+          const float2 f = *reinterpret_cast<const float2*>(part(label, p, at));
+          v[0] += f.x;
+          v[1] += f.y;
+        }
+        take(v);
+      }
+      return n;
+    };
+    float top[2] = {}, sum[2] = {};      // sum: what is not finite
+    const uint32_t n = all([&](const float (&v)[2]) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (fabsf(v[j]) < INFINITY) top[j] = fmaxf(top[j], fabsf(v[j]));
+        else sum[j] += v[j];
+      }
+    });
+    int shift[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) shift[j] = top[j] > 0.f ? 61 - (32 - __clz(n)) - ilogbf(top[j]) : 0;
+    long long whole[2] = {};
+    all([&](const float (&v)[2]) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (fabsf(v[j]) < INFINITY) whole[j] += __double2ll_rn(scalbn(double(v[j]), shift[j]));
+    });
+#pragma unroll
+    for (int j = 0; j < 2; ++j) sum[j] += float(scalbn(double(whole[j]), -shift[j]));
+    reinterpret_cast<uint32_t*>(d_hidden + t * vectors + c)[(at >> 1) & 3] = pack_bf16x2(sum[0], sum[1]);
   }
 }
 
@@ -722,7 +769,7 @@ struct Workspace {
   int64_t piece;                 // columns of a piece of the vocabulary
   int64_t pitch;                 // of the labels' rows: whole lines of 128 bytes
   int32_t splits;
-  size_t row, target, segment, state, best, sums, rows, stats, label_value, of_label, dz, parts, total;
+  size_t row, target, segment, state, next, best, sums, rows, stats, label_value, of_label, dz, parts, total;
   Workspace(int64_t n_rows, int64_t n_forks, int64_t n_segments, int64_t vocab, int64_t hidden, bool backward) {
     l_pad = std::max<int64_t>(256, padded(n_rows + n_forks));
     const int64_t most = std::max<int64_t>(256, kPieceBytes / (2 * l_pad) / 256 * 256), pieces = (vocab + most - 1) / most;
@@ -735,12 +782,13 @@ struct Workspace {
     row = take(l_pad * 4);
     target = take(l_pad * 4);
     segment = take(l_pad * 4);
-    state = take(n_rows * 4);
+    state = take(n_rows * 8);
     pitch = (hidden + 63) / 64 * 64;
     rows = take(l_pad * pitch * 2);
     label_value = take(l_pad * 4);
-    best = sums = stats = of_label = dz = parts = 0;
+    next = best = sums = stats = of_label = dz = parts = 0;
     if (backward) {
+      next = take(l_pad * 4);
       of_label = take(l_pad * sizeof(float2));
       dz = take(l_pad * piece * 2);
       parts = take(size_t(splits) * l_pad * hidden * 4);
@@ -753,7 +801,7 @@ struct Workspace {
   }
   Labels labels(char* ws) const {
     auto ints = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
-    return Labels{reinterpret_cast<Shared*>(ws), ints(row), ints(target), ints(segment), ints(state),
+    return Labels{reinterpret_cast<Shared*>(ws), ints(row), ints(target), ints(segment), reinterpret_cast<int2*>(ws + state), next ? ints(next) : nullptr,
                   best ? reinterpret_cast<unsigned long long*>(ws + best) : nullptr};
   }
 };
@@ -885,7 +933,7 @@ psa_status_t backward(const Call& c, const float* coef, const float* lse, void* 
       return failed_launch("dpo_linear_logp_bwd products");
   }
   if (c.n_rows > 0)
-    launch_behind(true, logp_scatter_kernel, dim3(unsigned((c.n_rows + 7) / 8)), 256, 0, c.stream, parts, w.labels(c.ws),
+    launch_behind(true, logp_scatter_kernel, dim3(unsigned((c.n_rows + 7) / 8), unsigned((c.width + 255) / 256)), 256, 0, c.stream, parts, w.labels(c.ws),
                   int32_t(c.n_rows), c.width, w.l_pad, w.splits, static_cast<uint4*>(d_hidden));
   return check_last_cuda_error("dpo_linear_logp_bwd launch");
 }
