@@ -67,10 +67,12 @@ __device__ __forceinline__ float lse_of(unsigned long long rank) {
   return __uint_as_float(bits & 0x80000000u ? bits & 0x7fffffffu : ~bits);
 }
 
-// The sum of a response's terms as whole numbers, which do not depend on their order: floor(term) and its rest in units of 2^-40,
-// a term taken as -2^38 where it is below (2^24 labels then stay within 64 bits).
+// The sum of a response's terms as whole numbers, which do not depend on their order: floor(term), a term taken as -2^38 where it is below
+// (2^25 labels, the most that there may be, then stay within 64 bits), and its rest in units of 2^-40.  From 2^24 labels on the rests may pass
+// 2^64 units: who sees his addition do that adds 2^24 to the whole numbers.
 struct Sum {
-  long long whole, rest;
+  long long whole;
+  unsigned long long rest;
   uint32_t odd, pad;                 // 1: a NaN was added, 2: an infinity
 };
 __device__ __forceinline__ void add_term(Sum* sum, double term) {
@@ -79,10 +81,11 @@ __device__ __forceinline__ void add_term(Sum* sum, double term) {
     return;
   }
   term = fmin(fmax(term, -274877906944.0), 0.0);      // (a probability that rounding has put above 1 counts as 1)
-  const double whole = floor(term);
-  atomicAdd(reinterpret_cast<unsigned long long*>(&sum->whole), static_cast<unsigned long long>(static_cast<long long>(whole)));
-  atomicAdd(reinterpret_cast<unsigned long long*>(&sum->rest),
-            static_cast<unsigned long long>(static_cast<long long>((term - whole) * 1099511627776.0 + 0.5)));
+  const double floored = floor(term);
+  const unsigned long long rest = static_cast<unsigned long long>((term - floored) * 1099511627776.0 + 0.5);
+  const unsigned long long before = atomicAdd(&sum->rest, rest);
+  const long long whole = static_cast<long long>(floored) + (before + rest < before ? 1 << 24 : 0);
+  atomicAdd(reinterpret_cast<unsigned long long*>(&sum->whole), static_cast<unsigned long long>(whole));
 }
 __device__ __forceinline__ float sum_of(const Sum& s) {
   if (s.odd & 1) return __uint_as_float(0x7fc00000u);

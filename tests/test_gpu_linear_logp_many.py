@@ -11,6 +11,32 @@ pytestmark = pytest.mark.gpu
 i32s = lambda n, v: torch.full((n,), v, dtype=torch.int32, device="cuda")  # noqa: E731
 
 
+def test_a_response_of_more_than_2_23_tokens():
+    """Terms a little below 0: each is -1 and nearly a whole unit of the fixed-point rest."""
+    n = (1 << 23) + (1 << 22)
+    hidden = torch.ones((n, 8), dtype=torch.bfloat16, device="cuda")
+    table = torch.zeros((2, 8), dtype=torch.bfloat16, device="cuda")
+    table[1] = 1.0
+    out, lse = O.dpo_linear_logp(hidden, table, i32s(n, 1), i32s(n, 0), 1)
+    term = -np.log1p(np.exp(-8.0))
+    # a term: an exponential's 2^-16 as in test_gpu_linear_logp.py, half a unit of 2^-40; the sum rounded once
+    assert abs(float(out[0]) / (n * term) - 1) <= 2.0 ** -16 + 2.0 ** -41 / -term + 2.0 ** -24
+    assert bool(((lse - (8.0 - term)).abs() <= 2.0 ** -16).all())
+
+
+def test_a_response_of_as_many_tokens_as_there_may_be():
+    """2^24 rows and as many forks in one response."""
+    n = 1 << 24
+    hidden = torch.ones((n, 8), dtype=torch.bfloat16, device="cuda")
+    table = torch.zeros((2, 8), dtype=torch.bfloat16, device="cuda")
+    table[1] = 1.0
+    rows = torch.arange(n, dtype=torch.int32, device="cuda")
+    out, lse = O.dpo_linear_logp(hidden, table, i32s(n, 1), i32s(n, 0), 1, rows, i32s(n, 1), i32s(n, 0))
+    term = -np.log1p(np.exp(-8.0))
+    assert abs(float(out[0]) / (2 * n * term) - 1) <= 2.0 ** -16 + 2.0 ** -41 / -term + 2.0 ** -24
+    assert bool(((lse - (8.0 - term)).abs() <= 2.0 ** -16).all())
+
+
 @pytest.mark.parametrize("n_rows,n_forks,live", [(5, 700, 0.5), (300, 2000, 0.5), (1, 300, 0.0), (40, 90, 1.0)])
 def test_many_forks_on_a_row(n_rows, n_forks, live):
     hidden, table, targets, seg, forks, coef = inputs(n_rows, 264, 513, n_forks, live=live, n_segments=9, n_forks=n_forks)
