@@ -409,7 +409,8 @@ block_norm_bwd_kernel(const Args args, const Shape shape) {
     const int tiles_each = rows == 1 && pairs ? 2 : 1;
     const uint32_t step = uint32_t(stride) * rows;   // rows between two tiles of the group
     const uint32_t stage_bytes = n_tensors * shape.slot_bytes, weights_at = base + uint32_t(tid) * V * 4u;
-    // (Threads behind a row's last window take its first one, with weights of zero, and write nothing.)
+    // (Threads behind a row's last window write nothing and have weights of zero; from a ring they take the row's first window, from
+    // memory, where it may have been written over by then, nothing.)
     uint32_t in_row[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) in_row[i] = (i * width + tid) * V - a < hidden ? uint32_t(i * width + tid) * 16u : 0u;
@@ -454,6 +455,7 @@ block_norm_bwd_kernel(const Args args, const Shape shape) {
         const XT* const from = static_cast<const XT*>(p);
         const int64_t at = int64_t(x.row) * hidden + int64_t(in_row[i] / 16u) * V - a;
         const uint4 raw = kRing ? ld_shared_v4(x.slot + uint32_t(t) * shape.slot_bytes + in_row[i])
+                          : (i * width + tid) * V - a >= hidden ? make_uint4(0, 0, 0, 0)
                           : kRagged ? load_window(from, at, all) : *reinterpret_cast<const uint4*>(from + at);
         Vec<XT, V> w;
         memcpy(&w, &raw, 16);
