@@ -45,6 +45,20 @@ constexpr int bwd_threads() {
   return kWarp ? 32 * kRowsPerCta : NV * 16 / int(sizeof(XT)) < 32 ? 512 : 544;
 }
 
+// Sum over the threads that share a row: a warp (kWarp) or `n_warps`, for which sync() is a barrier.  `slot` alternates, so that one barrier is enough.
+template <bool kWarp, int N, typename Sync>
+__device__ __forceinline__ void row_sum(float (&v)[N], float (*s_part)[32], int slot, int tid, int n_warps, Sync&& sync) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
+  if (kWarp) return;
+  const int lane = tid & 31;
+  if (lane == 0)
+    for (int i = 0; i < N; ++i) s_part[slot * 2 + i][tid >> 5] = v[i];
+  sync();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < n_warps ? s_part[slot * 2 + i][lane] : 0.f);
+}
+
 // A thread's columns in a row that starts `a` elements behind an aligned one: window k holds the columns [k V - a, (k + 1) V - a).
 // `stride` rows lie between the rows that a warp or CTA takes, a multiple of V where it takes several: `a`, and with it every
 // column of a thread, is the same in all of them.  Where a thread has one or two windows (kHold) it keeps its weights in

@@ -151,19 +151,5 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Sum over the threads that share a row: a warp (kWarp) or `n_warps`, for which sync() is a barrier.  `slot` alternates, so that one barrier is enough.
-template <bool kWarp, int N, typename Sync>
-__device__ __forceinline__ void row_sum(float (&v)[N], float (*s_part)[32], int slot, int tid, int n_warps, Sync&& sync) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-  if (kWarp) return;
-  const int lane = tid & 31;
-  if (lane == 0)
-    for (int i = 0; i < N; ++i) s_part[slot * 2 + i][tid >> 5] = v[i];
-  sync();
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = warp_sum(lane < n_warps ? s_part[slot * 2 + i][lane] : 0.f);
-}
-
 }  // namespace dev
 }  // namespace psa
