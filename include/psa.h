@@ -553,10 +553,11 @@ psa_status_t dpo_logp_bwd(const void* logits, int32_t logits_dtype, int64_t n_ro
  *   out           device fp32 [n_segments] (out)   lse    device fp32 [n_rows] (out)
  *   workspace     device scratch of dpo_linear_logp_workspace_bytes(.., backward = 0) bytes, 16-byte aligned
  *   device_status device int32 or NULL: BAD_TARGET and BAD_SEGMENT as by dpo_logp, WAIT_EXPIRED as by psa_fwd
- * The sums of the responses do not depend on the order of their terms: the same inputs give the same bits.  A term below
- * -2^38 counts as -2^38, one that rounding has put above 0 as 0.  A logit of -inf is a probability of 0 (a label's term is then
- * -inf); a row with another logit that is not finite has no log-probability: its term and lse are NaN.  Outputs must not
- * overlap inputs or one another.
+ * The sums of the responses do not depend on the order of their terms: the same inputs give the same bits.  A term is taken from
+ * the sum over the other tokens against the label's own logit, and is right relative to itself where it is near 0 (to 2^-41).  lse of
+ * a row that several labels score is that of its likeliest one.  A term below -2^38 counts as -2^38.  A logit of -inf is a
+ * probability of 0 (a label's term is then -inf); a row with another logit that is not finite has no log-probability: its term
+ * and lse are NaN.  Outputs must not overlap inputs or one another.
  * Errors: INVALID_ARG, UNSUPPORTED (sizes), ALIGNMENT (hidden, table, workspace: 16 bytes), CUDA.
  */
 size_t dpo_linear_logp_workspace_bytes(int64_t n_rows, int32_t n_forks, int32_t n_segments, int64_t vocab,
@@ -578,7 +579,8 @@ psa_status_t dpo_linear_logp(const void* hidden, const void* table, int64_t n_ro
  *   d_hidden      device bf16 [n_rows, width] (out): zeros in rows that score nothing
  *   d_table       device bf16 [vocab, width] (out), or NULL where it is not wanted
  *   workspace     device scratch of dpo_linear_logp_workspace_bytes(.., backward = 1) bytes, 16-byte aligned
- * No atomics on floats: the same inputs give the same bits.  A table entry that is not finite reaches d_hidden as a product, so
+ * A label's own element is -coef * expm1(z - lse) with the logit that lse was taken from: 1 - p as nearly as lse in fp32 tells it, to
+ * 2^-24 of lse.  No atomics on floats: the same inputs give the same bits.  A table entry that is not finite reaches d_hidden as a product, so
  * that a probability of 0 times -inf is NaN there.
  * Errors and the rest: as dpo_linear_logp (d_hidden, d_table: 16 bytes).
  */

@@ -9,12 +9,12 @@
 // exponentials, the label's own left out; a last kernel joins the parts of a row.  With z the label's logit, a product of its own, its
 // term is -log(1 + sum over the other tokens of exp(z[t, v] - z)): nothing near 1 is rounded and subtracted where the label is nearly certain.
 // Backward: the logits once more, in pieces of the vocabulary; their tile leaves as dz, rounded to bf16 as tcgen05.mma takes it
-// (a relative 2^-9 of each element, independent of one another), and both gradients are products with it.  dh is summed over
+// (2^-8 of each element at most, independent of one another), and both gradients are products with it.  dh is summed over
 // pieces in fp32; a piece of dW is complete.
 // Bound by the tensor cores: 2 n V D operations forward and 6 n V D backward for n labels; with few labels by the table's bytes.
-// Measured: 8499 labels of 16215 rows, 128256 x 4096, forward and backward 26.5 to 27.3 ms (1.31 to 1.35 PFLOP/s under the power cap);
-// 988 of 15154, forward, 655 us alone (1.57 PFLOP/s) and 800 to 840 under repetition; one label 207 to 221 us (the table at 6 TB/s in the
-// product); 1145 labels, 50257 x 1032, both 570 us; 206 labels, 1024 x 256, both 51.7 us (nine launches).
+// Measured: 8499 labels of 16215 rows, 128256 x 4096, forward and backward 26.5 to 27.8 ms (1.28 to 1.35 PFLOP/s under the power cap);
+// 988 of 15154, forward, 655 to 667 us alone (1.57 PFLOP/s) and 800 to 848 under repetition; one label 207 to 228 us (the table at 6 TB/s in the
+// product); 1145 labels, 50257 x 1032, both 570 to 583 us; 206 labels, 1024 x 256, both 51.7 us (nine launches).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -186,8 +186,9 @@ __host__ __device__ constexpr int64_t padded(int64_t n) { return (n + 255) / 256
 // of the logits that it is taken from.  For the backward pass what a label's row of dz takes: coef * scale, lse in units of log 2, and
 // its element at the label, coef * scale * (1 - p) from the product that the forward took lse from (from tcgen05's, 1 - p was 84 % too large
 // at 1e-4 and a logit of 20).
-// kWarps of a CTA's 8 take a row: all of them in a small call, where a row's trips to memory one after the other are what counts (one
-// row of 128256 x 4096: 223.6 -> 220.9 us in all).
+// kWarps of a CTA's 8 take a row: all of them in a small call, where a row's trips to memory one after the other are what counts.  The
+// border lies at 2048 labels: forward at width 1024, vocabulary 8192, with one warp and with eight, 256 labels 32.7 and 30.7 us, 1024 38.5
+// and 36.5, 2048 50.8 and 50.8, 4096 70.7 and 71.7, 8192 117 and 122; at width 4096 57.3 and 49.2, 79.5 and 72.7, 122.5 and 118.4, 194.5 and 191, 372 and 367.
 template <int kWarps>
 __global__ void __launch_bounds__(256)
 logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32_t vectors, int32_t pitch, uint4* rows, const float* coef, const float* lse,
@@ -291,7 +292,9 @@ struct Tile {
 };
 // What a tile of dW costs beside its stages (0.37 us each): its end, 3.3 us with the tile's bytes on their way to memory, where there are
 // few stages, and a part of that where there are more.  (Counted by their stages alone, 1 to 64 labels of 128256 x 4096 took 1288 us
-// instead of 480, 256 took 784 instead of 577, 512 940 instead of 850: clusters without a heavy tile took too many of them.)
+// instead of 480, 256 took 784 instead of 577, 512 940 instead of 850: clusters without a heavy tile took too many of them.  The whole
+// backward with 3, 6, 9 and 14: 64 labels of that table 831, 659, 667 and 676 us, 256 of it 882, 832, 749 and 766, 64 of 50257 x 1032 139, 125, 120 and
+// 124, 300 of 50257 x 768 141, 131, 124 and 128, 2 of 32000 x 4096 273, 209, 202 and 209.)
 constexpr int kEndStages = 9;
 
 // The tiles that a cluster takes.  Those of the first product (`heavy`) go round the clusters one by one; of the second, clusters
@@ -320,7 +323,10 @@ struct Schedule {
     return k < light ? heavy + k : -1;
   }
 };
-// Tiles run down `group` rows of tiles before they move one column on, so that the tiles in flight share strips of A and of B in L2.
+// Tiles run down `group` rows of tiles before they move one column on, so that the tiles in flight share strips of A and of B in L2.  The logits'
+// 16: with 8, 8499 labels of 128256 x 4096 took 6.60 ms instead of 6.35, with 32 as long.  dh's 9: with 4, 5 and 16, backward passes of 1145 to 8499
+// labels and widths of 1024 to 4096 came out within what repetitions of the same differ by (up to 8 %, under
+// the power cap).
 __device__ __forceinline__ void place(int at, int m_tiles, int n_tiles, int group, Tile* t) {
   const int per_group = group * n_tiles, g = at / per_group, first = g * group, rows = min(group, m_tiles - first), in = at - g * per_group;
   t->m0 = (first + in % rows) * kTile;

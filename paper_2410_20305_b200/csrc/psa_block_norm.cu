@@ -9,7 +9,7 @@
 //     dpw = gate A,  dpb = gate C,  dgate = pw A + pb C           (dgate = A without a norm).
 // Bound by HBM: forward two rows are read and two written, backward four and two.  Both norms of a row are taken while it is in
 // registers.  Sums are fp32, the variance after the mean.
-// Measured: 16215 x 4096 bf16 RMS forward 93 us (5.7 TB/s), one token 7.6 to 8.2; 31041 x 4096 layer norm with gate backward 377 us (4.0 TB/s: two
+// Measured: 16215 x 4096 bf16 RMS forward 93 to 95 us (5.7 TB/s), one token 7.6 to 8.2; 31041 x 4096 layer norm with gate backward 377 us (4.0 TB/s: two
 // barriers for two rows, with as many warps as registers allow), RMS 329; 5465 x 1237 forward and backward 60.
 // Rows of any width are moved 16 bytes at a time (psa_vector.cuh): a row that starts `a` elements behind an aligned one is
 // taken as windows, window k holding the columns [k V - a, (k + 1) V - a).
@@ -259,7 +259,8 @@ block_norm_kernel(const Args args) {
 // ---------------------------------------------------------------- backward
 // A CTA's warps form groups that take rows one after the other, 8 columns a thread (16 beyond 4096), each from a ring of its own, which bulk copies
 // fill with the four tensors' rows, so that several rows are in flight whatever the arithmetic waits for.
-// (Beyond 8192 columns, where no ring of whole rows has room, 1024 threads take a row, 24 columns each, from where it lies.)
+// (Beyond 8192 columns, where no ring of whole rows has room, 1024 threads take a row, 24 columns each, from where it lies, and spill 1 to 2 KB
+// a thread.)
 // The two norms of a row need its sums one after the other; a group takes two rows at a time
 // (of up to 4096 columns), whose sums cross a barrier together.
 // All rows of a CTA start equally far behind an aligned element (where rows start anywhere, they lie a multiple of V rows
@@ -268,8 +269,8 @@ block_norm_kernel(const Args args) {
 constexpr int kRingThreads = 512, kWideThreads = 1024;
 constexpr int kMaxGroups = 16;                          // (15 of several warps: each needs a barrier)
 constexpr uint32_t kMaxStages = 8;
-// Shared memory of weights and rings.  (208 KB leave L1 no room for what the compiler spills, 16 to 80 bytes a thread in layer norms:
-// 385 us instead of 371 at 31041 x 4096.)
+// Shared memory of weights and rings.  (208 KB leave L1 no room for what the compiler spills, up to 276 bytes of stores a thread in layer
+// norms, stacks of 8 to 104: 385 us instead of 371 at 31041 x 4096.)
 constexpr uint32_t kRoom = 176 * 1024;
 constexpr int kRingColumns = 16, kWideColumns = 24;      // of a thread, at most
 __host__ __device__ constexpr int part_pitch(int hidden) { return (hidden + 3) / 4 * 4; }

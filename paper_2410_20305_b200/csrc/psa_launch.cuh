@@ -10,8 +10,8 @@
 //    `early`) is launched behind one that calls behind_wait() ahead of behind_go() and does not write it: all that came
 //    before is complete by then.  (An `early` product is never a call's first; the one before it is of the same call.)
 //    psa_bwd_kernel calls behind_go() first, so only kernels that wait before they read may follow it: psa_fwd_kernel,
-//    psa_bwd_delta_kernel, psa_bwd_convert_kernel, those of the loss, of the normalisation and of the embedding, and the
-//    first of the feed-forward block.
+//    psa_bwd_delta_kernel, psa_bwd_convert_kernel, those of the loss, of the normalisation, of the norms around a block, of the
+//    rotary positions, of the embedding and of the log-probabilities from hidden states, and the first of the feed-forward block.
 #pragma once
 #include <cuda_runtime.h>
 

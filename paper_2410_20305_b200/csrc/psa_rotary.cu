@@ -7,7 +7,7 @@
 // taken modulo 2^64, is the fraction of a turn exactly, for any position (an fp32 product p w is off by 0.06 rad at 10^6).
 // Bound by HBM.  A thread owns a few pairs of a token, computes their sines once and turns them in several heads, which it requests ahead
 // of the sines (with loads behind them 68.5 us instead of 54 in the first of these).  Measured: 16215 x 40 heads of 128 bf16, views of one
-// projection, 51.5 to 54 us (6.2 to 6.4 TB/s); 7965 x 15 heads of 80 fp32, 36 of them turned, 13.2 us (5.8 TB/s); one token 5.6 us.
+// projection, 51.5 to 55 us (6.0 to 6.4 TB/s); 7965 x 15 heads of 80 fp32, 36 of them turned, 13.2 to 13.5 us (5.7 TB/s); one token 5.6 us.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
