@@ -541,7 +541,8 @@ psa_status_t dpo_logp_bwd(const void* logits, int32_t logits_dtype, int64_t n_ro
 /*
  * dpo_linear_logp -- dpo_logp straight from the hidden states and the output table: the logits
  *     z[t][v] = scale * sum_c hidden[t][c] * table[v][c]
- * are formed tile by tile, in fp32, and not kept.
+ * are formed tile by tile, in fp32, and not kept.  (Tensor cores cut off where an fp32 addition rounds: the mean of what that
+ * takes, width * 2^-30 of a logit, is given back.  A label's own logit is a product of its own.)
  *   out[g] = sum over scored (row t, label y) with response id g of  z[t][y] - log sum_v exp(z[t][v])
  *   lse[t] = log sum_v exp(z[t][v]) of every row that scores a label, 0 of the others
  *   hidden        device bf16 [n_rows, width]      table  device bf16 [vocab, width] (as psa_embed's)
@@ -638,7 +639,7 @@ psa_status_t psa_norm_bwd(const void* d_out, const void* x, const void* weight, 
  * psa_block_norm -- the step between two sublayers whose output is normalised before it joins the residual stream, or scaled by
  * a gate, or both (psa_norm with a residual is the form without either).  Per row, in fp32:
  *     y = norm(x) * post_weight + post_bias     (y = x where post_weight is NULL)
- *     s = residual_scale * residual + gate * y, rounded to x's type     (gate = 1 where it is NULL)
+ *     s = residual_scale * residual + gate * y, rounded to x's type     (gate = 1 where it is NULL; the first product is rounded to fp32)
  *     out = norm(s) * weight + bias,            norm(v) = (v - m) * r, m and r as by psa_norm
  *   x, residual  device [n_tokens, hidden] of `dtype`: the sublayer's output and the residual stream
  *   weight, bias, post_weight, post_bias, gate   device [hidden] of `weight_dtype`; all but weight may be NULL; biases are

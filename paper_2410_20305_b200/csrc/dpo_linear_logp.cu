@@ -14,7 +14,7 @@
 // Bound by the tensor cores: 2 n V D operations forward and 6 n V D backward for n labels; with few labels by the table's bytes.
 // Measured: 8499 labels of 16215 rows, 128256 x 4096, forward and backward 26.5 to 27.8 ms (1.28 to 1.35 PFLOP/s under the power cap);
 // 988 of 15154, forward, 655 to 667 us alone (1.57 PFLOP/s) and 800 to 848 under repetition; one label 207 to 228 us (the table at 6 TB/s in the
-// product); 1145 labels, 50257 x 1032, both 570 to 583 us; 206 labels, 1024 x 256, both 51.7 us (nine launches).
+// product); 1145 labels, 50257 x 1032, both 570 to 583 us; 206 labels, 1024 x 256, both 51.7 to 53.6 us (nine launches).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -37,6 +37,12 @@ using namespace dev;
 constexpr int kSmCount = 148;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
+
+// tcgen05 cuts off what an addition of fp32 rounds.  Of a logit, a sum of terms of both signs, that takes 2^-30 of itself for each of its terms in the
+// mean (2^-30 is 0.93e-9; measured 0.94e-9 at 1024 and 2048 columns, 0.98, 1.02 and 1.03e-9 at 4096, 8192 and 16384; sums of one sign lose 1.7 to 5 times as
+// much), which the scale gives back: a log-probability of 128256 x 4096 was off by 1.2e-6 of itself and is by 2e-8 to 8e-8.
+// A label's own product, by fp32 additions, takes the scale without it.
+constexpr double cut_off(int32_t width) { return 1.0 + width * 0x1p-30; }
 
 // ---------------------------------------------------------------- labels
 // What the kernels of a call share, at the head of its workspace.
@@ -181,18 +187,17 @@ logp_list_kernel(const int32_t* targets, const int32_t* segment_ids, const int32
 __host__ __device__ constexpr int64_t padded(int64_t n) { return (n + 255) / 256 * 256; }
 
 // The hidden rows of the labels side by side, zeros behind the last one to the next multiple of 256 (and in the first 256 where
-// there is no label), and the label's own product, by fp32 additions that round: tcgen05's cut off, which makes a logit smaller by about
-// width * 1e-9 of itself (4.2e-6 at 4096), and what is left of a nearly certain label's probability is off, relative to itself, by the errors
-// of the logits that it is taken from.  For the backward pass what a label's row of dz takes: coef * scale, lse in units of log 2, and
-// its element at the label, coef * scale * (1 - p) from the product that the forward took lse from (from tcgen05's, 1 - p was 84 % too large
-// at 1e-4 and a logit of 20).
+// there is no label), and the label's own product, by fp32 additions that round: what is left of a nearly certain label's
+// probability is off, relative to itself, by the errors of the logits that it is taken from, and its own is the largest.  For the backward
+// pass what a label's row of dz takes: coef * scale, lse in units of log 2, and its element at the label, coef * scale * (1 - p) from the
+// product that the forward took lse from (from tcgen05's, d_hidden was off by 1.8 of its norm at 1 - p = 1e-4 and a logit of 16).
 // kWarps of a CTA's 8 take a row: all of them in a small call, where a row's trips to memory one after the other are what counts.  The
 // border lies at 2048 labels: forward at width 1024, vocabulary 8192, with one warp and with eight, 256 labels 32.7 and 30.7 us, 1024 38.5
 // and 36.5, 2048 50.8 and 50.8, 4096 70.7 and 71.7, 8192 117 and 122; at width 4096 57.3 and 49.2, 79.5 and 72.7, 122.5 and 118.4, 194.5 and 191, 372 and 367.
 template <int kWarps>
 __global__ void __launch_bounds__(256)
 logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32_t vectors, int32_t pitch, uint4* rows, const float* coef, const float* lse,
-                   float scale, float2* of_label, float* label_value) {
+                   float scale, double label_scale, float2* of_label, float* label_value) {
   constexpr int kThreads = 32 * kWarps;
   __shared__ float s_sum[8];
   const int tid = int(threadIdx.x) % kThreads, lane = threadIdx.x & 31;
@@ -207,6 +212,8 @@ logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32
     return;
   }
   const int32_t t = labels.row[i];
+  const bool ends = tid == 0 && coef;      // (what it needs then, requested now)
+  const float factor = ends ? coef[labels.segment[i]] * scale : 0.f, of_row = ends ? lse[t] : 0.f;
   const uint4* from = hidden + int64_t(t) * vectors;
   const uint4* weight = table + int64_t(labels.target[i]) * vectors;
   float sum[8] = {};
@@ -229,17 +236,13 @@ logp_gather_kernel(const uint4* hidden, const uint4* table, Labels labels, int32
     __syncthreads();
     all = ((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3])) + ((s_sum[4] + s_sum[5]) + (s_sum[6] + s_sum[7]));
   }
-  if (tid != 0) return;
-  if (!coef) {
-    label_value[i] = all;
-    return;
-  }
-  const float c = coef[labels.segment[i]] * scale, of_row = lse[t];
+  if (tid == 0 && !coef) label_value[i] = all;
+  if (!ends) return;
   // (as the forward scales it; where fp32 does not tell it from lse, p is 1)
-  const double z = double(all) * double(scale * kLog2e) * kLn2;
+  const double z = double(all) * label_scale * kLn2;
   const float logp = float(z) == of_row ? 0.f : float(z - double(of_row));
-  of_label[i] = make_float2(c, of_row * kLog2e);
-  label_value[i] = -c * expm1f(logp > 0.f ? 0.f : logp);      // (NaN stays)
+  of_label[i] = make_float2(factor, of_row * kLog2e);
+  label_value[i] = -factor * expm1f(logp > 0.f ? 0.f : logp);      // (NaN stays)
 }
 
 // ---------------------------------------------------------------- products
@@ -282,7 +285,7 @@ struct ProductArgs {
   int32_t splits;         // parts of dh's K, each with rows of its own of the output
   int32_t add;            // dh is added to what is there
   int32_t with_table;     // dW is wanted
-  float scale_log2;       // scale / log 2
+  float scale_log2;       // scale / log 2, with what the sums have lost
   int32_t* status;
 };
 
@@ -611,7 +614,7 @@ logp_product_kernel(const __grid_constant__ ProductArgs args) {
 constexpr int kJoinWarps = 32;
 __global__ void __launch_bounds__(32 * kJoinWarps)
 logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, int64_t l_pad, int32_t v_tiles, int32_t n_rows, int32_t n_segments,
-                 float scale_log2, Sum* sums, float* out, float* lse) {
+                 double label_scale, Sum* sums, float* out, float* lse) {
   __shared__ float2 s_part[kJoinWarps][32];
   __shared__ bool s_last;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -658,7 +661,7 @@ logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, i
       s = all[0] + all[1];
       // The other tokens' sum, s 2^m, against the label's own exponential; where that is far below it, the label's share of the row's sum is
       // lost in any case.
-      const double label = double(label_logit[i]) * double(scale_log2), apart = label - double(m);
+      const double label = double(label_logit[i]) * label_scale, apart = label - double(m);
       double term, row_lse;
       if (apart > -512.0) {
         const double others = log1p(double(s) * exp2(-apart));
@@ -848,6 +851,10 @@ psa_status_t check(const Call& c, std::initializer_list<const void*> outputs) {
   return PSA_OK;
 }
 
+// In units of log 2, of the logits from the tiles and of the labels' own: the same rounding in both.
+float tile_scale(const Call& c) { return float(double(c.scale) / kLn2 * cut_off(c.width)); }
+double label_scale(const Call& c) { return double(tile_scale(c)) / cut_off(c.width); }
+
 // Lists the labels and copies their rows.
 bool launch_labels(const Call& c, const Workspace& w, bool backward, const float* coef, const float* lse) {
   const Labels labels = w.labels(c.ws);
@@ -857,7 +864,7 @@ bool launch_labels(const Call& c, const Workspace& w, bool backward, const float
     return false;
   const bool few = w.l_pad <= 2048;
   return launch_behind(true, few ? logp_gather_kernel<8> : logp_gather_kernel<1>, dim3(unsigned(few ? w.l_pad : w.l_pad / 8)), 256, 0, c.stream, static_cast<const uint4*>(c.hidden),
-                       static_cast<const uint4*>(c.table), labels, c.width / 8, int32_t(w.pitch / 8), reinterpret_cast<uint4*>(c.ws + w.rows), coef, lse, c.scale,
+                       static_cast<const uint4*>(c.table), labels, c.width / 8, int32_t(w.pitch / 8), reinterpret_cast<uint4*>(c.ws + w.rows), coef, lse, c.scale, label_scale(c),
                        backward ? reinterpret_cast<float2*>(c.ws + w.of_label) : nullptr,
                        reinterpret_cast<float*>(c.ws + w.label_value)) == cudaSuccess;
 }
@@ -883,7 +890,7 @@ ProductArgs common_args(const Call& c, const Workspace& w) {
   a.l_pad = w.l_pad;
   a.hidden = c.width;
   a.splits = 1;
-  a.scale_log2 = c.scale * kLog2e;
+  a.scale_log2 = tile_scale(c);
   a.status = c.status;
   return a;
 }
@@ -901,7 +908,7 @@ psa_status_t forward(const Call& c, float* out, float* lse) {
   if (!launch_product<kEpiStats>(a, w.l_pad / kTile * v_tiles, c.stream)) return failed_launch("dpo_linear_logp product");
   launch_behind(true, logp_join_kernel, dim3(unsigned(w.l_pad / 32)), 32 * kJoinWarps, 0, c.stream, a.stats,
                 reinterpret_cast<const float*>(c.ws + w.label_value), w.labels(c.ws), w.l_pad,
-                int32_t(v_tiles), int32_t(c.n_rows), c.n_segments, a.scale_log2, reinterpret_cast<Sum*>(c.ws + w.sums), out, lse);
+                int32_t(v_tiles), int32_t(c.n_rows), c.n_segments, label_scale(c), reinterpret_cast<Sum*>(c.ws + w.sums), out, lse);
   return check_last_cuda_error("dpo_linear_logp launch");
 }
 
