@@ -222,8 +222,18 @@ block_norm_kernel(const Args args) {
     }
     pairs_of(rr[i], p);
     float f[V];
+    // The product is rounded before the sum: of a scale that fp32 does not hold, like 0.7, what was added to it goes with that.  (One fma kept it, and
+    // 6e-4 of all sums, which lie on a tie of bf16 as written, went the other way.  Products of pairs are made one fma with the sum, too.)
+    if (args.residual_scale != 1.f) {
 #pragma unroll
-    for (int j = 0; j < H; ++j) s[i][j] = fma_f32x2(p[j], both(args.residual_scale), s[i][j]);
+      for (int j = 0; j < H; ++j) {
+        float lo, hi;
+        unpack_f32x2(p[j], lo, hi);
+        p[j] = pack_f32x2(__fmul_rn(lo, args.residual_scale), __fmul_rn(hi, args.residual_scale));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < H; ++j) s[i][j] = add_f32x2(p[j], s[i][j]);
     to_floats<V>(s[i], f);
     put(args.total, col, f);
     Vec<XT, V> v;     // what is normalised is what the residual stream holds

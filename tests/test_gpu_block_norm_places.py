@@ -1,4 +1,5 @@
-"""psa_block_norm_bwd in place, where what is written over an input is not finite: the results are those of outputs that lie apart."""
+"""psa_block_norm_bwd in place, where what is written over an input is not finite: the results are those of outputs that lie apart; and
+how psa_block_norm rounds the scaled residual."""
 import pytest
 import torch
 
@@ -29,3 +30,15 @@ def test_a_gradient_of_the_residual_that_overflows_over_an_input(T, D, dtype):
         torch.cuda.synchronize()
         same = [a is b is None or bool(((a == b) | (a.isnan() & b.isnan())).all()) for a, b in zip(got, want)]
         assert all(same), (place, same)
+
+
+@pytest.mark.parametrize("D", [100, 1237, 4096])
+@pytest.mark.parametrize("scale", [0.7, 0.3, 1.0])
+def test_the_scaled_residual_is_rounded_before_the_block_joins_it(scale, D):
+    """Of a scale that fp32 does not hold, what was added to it goes with the rounding of the product, so that sums of few digits which
+    lie half way between two values of bf16 go the way that they go as written: the sum is that of products and a sum rounded to fp32 each."""
+    T = 700
+    x, res, w = normal((T, D), 1, torch.bfloat16), (2 * normal((T, D), 2, torch.float32)).to(torch.bfloat16), normal((D,), 3, torch.bfloat16, 1.0)
+    gate = (0.5 * normal((D,), 4, torch.float32)).to(torch.bfloat16)
+    _, total, _ = O.psa_block_norm(x, res, w, gate=gate, residual_scale=scale)
+    assert torch.equal(total, (res.float() * scale + x.float() * gate.float()).to(torch.bfloat16))
