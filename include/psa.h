@@ -574,7 +574,7 @@ psa_status_t dpo_linear_logp(const void* hidden, const void* table, int64_t n_ro
  *     dz[t][v] = scale * sum over the labels (t, y, g) of coef[g] * (1[v == y] - exp(z[t][v] - lse[t])),
  *     d_hidden = dz table,   d_table = dz^T hidden,
  * with fp32 sums; the logits are formed again, in pieces of the vocabulary, and dz of a piece, rounded to bf16 for the two
- * products, takes 1 GiB of the workspace at most (or 256 columns of the vocabulary, where those are more).
+ * products (d_hidden gets back what that takes from a label's own element), takes 1 GiB of the workspace at most (or 256 columns of the vocabulary, where those are more).
  *   coef          device fp32 [n_segments], e.g. from dpo_loss
  *   lse           device fp32 [n_rows] as written by dpo_linear_logp
  *   d_hidden      device bf16 [n_rows, width] (out): zeros in rows that score nothing

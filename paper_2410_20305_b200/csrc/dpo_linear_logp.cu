@@ -10,11 +10,11 @@
 // term is -log(1 + sum over the other tokens of exp(z[t, v] - z)): nothing near 1 is rounded and subtracted where the label is nearly certain.
 // Backward: the logits once more, in pieces of the vocabulary; their tile leaves as dz, rounded to bf16 as tcgen05.mma takes it
 // (2^-8 of each element at most, independent of one another), and both gradients are products with it.  dh is summed over
-// pieces in fp32; a piece of dW is complete.
+// pieces in fp32, and gets back what the label's element has lost; a piece of dW is complete.
 // Bound by the tensor cores: 2 n V D operations forward and 6 n V D backward for n labels; with few labels by the table's bytes.
 // Measured: 8499 labels of 16215 rows, 128256 x 4096, forward and backward 26.5 to 27.8 ms (1.28 to 1.35 PFLOP/s under the power cap);
 // 988 of 15154, forward, 655 to 667 us alone (1.57 PFLOP/s) and 800 to 848 under repetition; one label 207 to 228 us (the table at 6 TB/s in the
-// product); 1145 labels, 50257 x 1032, both 570 to 583 us; 206 labels, 1024 x 256, both 51.7 to 53.6 us (nine launches).
+// product); 1145 labels, 50257 x 1032, both 570 to 583 us; 206 labels, 1024 x 256, both 51.7 to 54 us (nine launches).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -697,10 +697,12 @@ logp_join_kernel(const float2* stats, const float* label_logit, Labels labels, i
 }
 
 // dh of every row of hidden: the sum over its own label and the forks that name it, each the sum of its parts; zeros where it scores nothing.
+// The label's element is most of a row of dz: what its rounding to bf16 has taken joins here, times its row of the table (dh's error in the 2-norm,
+// the result's own rounding of 0.0017 with it, 0.0024 to 0.0026 -> 0.0017).
 // Two labels are added as they come.  More, which are listed in no order, as whole numbers: the largest magnitude of a column gives a unit in which
 // all of them stay within 62 bits and lose what is 2^-35 of it at most, so that their sum depends on no order.
 __global__ void __launch_bounds__(256)
-logp_scatter_kernel(const float* parts, Labels labels, int32_t n_rows, int32_t hidden, int64_t l_pad,
+logp_scatter_kernel(const float* parts, const float* label_dz, const uint32_t* table, Labels labels, int32_t n_rows, int32_t hidden, int64_t l_pad,
                     int32_t splits, uint4* d_hidden) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t t = int64_t(blockIdx.x) * 8 + warp;
@@ -711,6 +713,13 @@ logp_scatter_kernel(const float* parts, Labels labels, int32_t n_rows, int32_t h
   const int c = int(blockIdx.y) * 32 + lane, vectors = hidden / 8;
   if (c >= vectors) return;
   auto part = [&](int32_t label, int p, int at) { return parts + (p * l_pad + label) * int64_t(hidden) + at; };
+  auto row_of_table = [&](int32_t label, int at) { return table + (int64_t(labels.target[label]) * hidden + at) / 2; };
+  auto taken = [&](int32_t label) {
+    const float dz = label_dz[label];
+    return dz - __bfloat162float(__float2bfloat16(dz));
+  };
+  // (a table entry that is not finite has reached the product)
+  auto give = [](float& to, float e, float w) { to += fabsf(w) < INFINITY ? e * w : 0.f; };
   if (!state.y || !labels.next[state.y - 1]) {
     float sum[8] = {};
     auto add = [&](int32_t label) {
@@ -720,6 +729,14 @@ logp_scatter_kernel(const float* parts, Labels labels, int32_t n_rows, int32_t h
         const float4 a = from[0], b = from[1];
         v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
         v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+      }
+      const float e = taken(label);
+      const uint4 w = *reinterpret_cast<const uint4*>(row_of_table(label, 8 * c));
+      const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        give(v[2 * j], e, __uint_as_float(words[j] << 16));
+        give(v[2 * j + 1], e, __uint_as_float(words[j] & 0xffff0000u));
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) sum[j] += v[j];
@@ -743,6 +760,9 @@ logp_scatter_kernel(const float* parts, Labels labels, int32_t n_rows, int32_t h
           v[0] += f.x;
           v[1] += f.y;
         }
+        const uint32_t w = *row_of_table(label, at);
+        give(v[0], taken(label), __uint_as_float(w << 16));
+        give(v[1], taken(label), __uint_as_float(w & 0xffff0000u));
         take(v);
       }
       return n;
@@ -949,7 +969,8 @@ psa_status_t backward(const Call& c, const float* coef, const float* lse, void* 
       return failed_launch("dpo_linear_logp_bwd products");
   }
   if (c.n_rows > 0)
-    launch_behind(true, logp_scatter_kernel, dim3(unsigned((c.n_rows + 7) / 8), unsigned((c.width + 255) / 256)), 256, 0, c.stream, parts, w.labels(c.ws),
+    launch_behind(true, logp_scatter_kernel, dim3(unsigned((c.n_rows + 7) / 8), unsigned((c.width + 255) / 256)), 256, 0, c.stream, parts,
+                  reinterpret_cast<const float*>(c.ws + w.label_value), static_cast<const uint32_t*>(c.table), w.labels(c.ws),
                   int32_t(c.n_rows), c.width, w.l_pad, w.splits, static_cast<uint4*>(d_hidden));
   return check_last_cuda_error("dpo_linear_logp_bwd launch");
 }

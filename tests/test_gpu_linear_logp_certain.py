@@ -161,3 +161,31 @@ def test_log_probabilities_are_not_high_in_the_mean(width, vocab):
     error = (f64(out) - ro).mean(), (f64(lse) - rl).mean()
     print("mean error of the terms %.2e, of lse %.2e, bound %.2e" % (*error, bound))
     assert likely > 5 and abs(error[0]) <= bound and abs(error[1]) <= bound
+
+
+@pytest.mark.parametrize("n,width,vocab,forked", [(300, 512, 2000, False), (40, 1032, 700, True), (2500, 64, 1500, False)])
+def test_the_rounding_of_a_label_s_element_is_given_back_to_d_hidden(n, width, vocab, forked):
+    """Responses' coefficients at which a label's element of dz, nearly all of its row, lies half way between two values of bf16: d_hidden has
+    the error of its own rounding, uniform within 2^-8 of a value at most, and of the roundings of the other elements."""
+    rng = np.random.default_rng(n)
+    bf = lambda a: torch.as_tensor(a, dtype=torch.float32).to(torch.bfloat16)  # noqa: E731
+    hidden, table = bf(rng.normal(size=(n, width))), bf(rng.normal(size=(vocab, width)) * 0.5 * width ** -0.5)
+    targets, rows = rng.integers(0, vocab, size=n).astype(np.int32), np.arange(n, dtype=np.int32)
+    coef = ((1 + 2.0 ** -8) * (1 + 1.0 / vocab) * rng.uniform(0.9995, 1.0005, size=n)).astype(np.float32)
+    forks = NONE
+    if forked:      # three more labels for each row, of the same responses
+        forks = [np.tile(rows, 3), rng.integers(0, vocab, size=3 * n).astype(np.int32), np.tile(rows, 3)]
+    _, _, dh, _, status = both(hidden, table, targets, rows, forks, coef)
+    h, w = f64(hidden), f64(table)
+    z = h @ w.T
+    p = np.exp(z) / np.exp(z).sum(1, keepdims=True)
+    ref, others = np.zeros_like(h), np.zeros_like(h)
+    for t, y in zip(np.concatenate([rows, forks[0]]), np.concatenate([targets, forks[1]])):
+        dz = -float(coef[t]) * p[t]
+        others[t] += dz ** 2 @ w ** 2
+        dz[y] += float(coef[t])
+        ref[t] += dz @ w
+    err = np.linalg.norm(f64(dh) - ref)
+    bound = H8 / 3 ** 0.5 * np.sqrt((ref ** 2).sum() + others.sum()) + 2.0 ** -16 * np.linalg.norm(ref)
+    print("%.3f of the bound" % (err / bound))
+    assert status == 0 and err <= bound
