@@ -574,15 +574,16 @@ psa_status_t dpo_linear_logp(const void* hidden, const void* table, int64_t n_ro
  *     dz[t][v] = scale * sum over the labels (t, y, g) of coef[g] * (1[v == y] - exp(z[t][v] - lse[t])),
  *     d_hidden = dz table,   d_table = dz^T hidden,
  * with fp32 sums; the logits are formed again, in pieces of the vocabulary, and dz of a piece, rounded to bf16 for the two
- * products (d_hidden gets back what that takes from a label's own element), takes 1 GiB of the workspace at most (or 256 columns of the vocabulary, where those are more).
+ * products (d_hidden gets back what that takes from a label's own element), takes 1 GiB of the workspace at most (or 256
+ * columns of the vocabulary, where those are more).
  *   coef          device fp32 [n_segments], e.g. from dpo_loss
  *   lse           device fp32 [n_rows] as written by dpo_linear_logp
  *   d_hidden      device bf16 [n_rows, width] (out): zeros in rows that score nothing
  *   d_table       device bf16 [vocab, width] (out), or NULL where it is not wanted
  *   workspace     device scratch of dpo_linear_logp_workspace_bytes(.., backward = 1) bytes, 16-byte aligned
- * A label's own element is -coef * expm1(z - lse) with the logit that lse was taken from: 1 - p as nearly as lse in fp32 tells it, to
- * 2^-24 of lse.  No atomics on floats: the same inputs give the same bits.  A table entry that is not finite reaches d_hidden as a product, so
- * that a probability of 0 times -inf is NaN there.
+ * A label's own element is -scale * coef * expm1(z - lse) with the logit that lse was taken from: 1 - p as nearly as lse in fp32
+ * tells it, to 2^-24 of lse.  No atomics on floats: the same inputs give the same bits.  A table entry that is not finite reaches
+ * d_hidden as a product, so that a probability of 0 times -inf is NaN there.
  * Errors and the rest: as dpo_linear_logp (d_hidden, d_table: 16 bytes).
  */
 psa_status_t dpo_linear_logp_bwd(const float* coef, const void* hidden, const void* table, const float* lse,
