@@ -75,7 +75,7 @@ __device__ __forceinline__ float lse_of(unsigned long long rank) {
 
 // The sum of a response's terms as whole numbers, which do not depend on their order: floor(term), a term taken as -2^38 where it is below
 // (2^25 labels, the most that there may be, then stay within 64 bits), and its rest in units of 2^-40.  From 2^24 labels on the rests may pass
-// 2^64 units: who sees his addition do that adds 2^24 to the whole numbers.
+// 2^64 units: the addition that sees them do so adds 2^24 to the whole numbers.
 struct Sum {
   long long whole;
   unsigned long long rest;
@@ -716,7 +716,8 @@ logp_scatter_kernel(const float* parts, const float* label_dz, const uint32_t* t
   auto row_of_table = [&](int32_t label, int at) { return table + (int64_t(labels.target[label]) * hidden + at) / 2; };
   auto taken = [&](int32_t label) {
     const float dz = label_dz[label];
-    return dz - __bfloat162float(__float2bfloat16(dz));
+    const float e = dz - __bfloat162float(__float2bfloat16(dz));
+    return fabsf(e) < INFINITY ? e : 0.f;      // (beyond bf16's range the product has an infinity)
   };
   // (a table entry that is not finite has reached the product)
   auto give = [](float& to, float e, float w) { to += fabsf(w) < INFINITY ? e * w : 0.f; };

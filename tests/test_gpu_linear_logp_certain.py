@@ -189,3 +189,18 @@ def test_the_rounding_of_a_label_s_element_is_given_back_to_d_hidden(n, width, v
     bound = H8 / 3 ** 0.5 * np.sqrt((ref ** 2).sum() + others.sum()) + 2.0 ** -16 * np.linalg.norm(ref)
     print("%.3f of the bound" % (err / bound))
     assert status == 0 and err <= bound
+
+
+@pytest.mark.parametrize("forked", [False, True])
+def test_a_label_s_element_beyond_the_range_of_bf16(forked):
+    """A coefficient that fp32 holds and bf16 does not: what reaches d_hidden is the label's infinity times its row of the table."""
+    rng = np.random.default_rng(4)
+    bf = lambda a: torch.as_tensor(a, dtype=torch.float32).to(torch.bfloat16)  # noqa: E731
+    n, width, vocab = 20, 64, 3000
+    hidden, table = bf(rng.normal(size=(n, width)) * 0.1), bf(rng.normal(size=(vocab, width)))
+    targets, rows = rng.integers(0, vocab, size=n).astype(np.int32), np.arange(n, dtype=np.int32)
+    coef = np.full(n, 3.401e38, np.float32)      # (1 - 1 / 3000 of it is nearer to the infinity of bf16 than to its largest number, 3.39e38)
+    forks = [np.tile(rows, 2), np.tile(targets, 2), np.tile(rows, 2)] if forked else NONE
+    _, _, dh, _, _ = both(hidden, table, targets, rows, forks, coef)
+    w = f64(table)[targets]
+    assert np.array_equal(f64(dh), np.sign(w) * np.inf)
