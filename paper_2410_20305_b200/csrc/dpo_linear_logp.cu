@@ -14,7 +14,7 @@
 // Bound by the tensor cores: 2 n V D operations forward and 6 n V D backward for n labels; with few labels by the table's bytes.
 // Measured: 8499 labels of 16215 rows, 128256 x 4096, forward and backward 26.5 to 27.8 ms (1.28 to 1.35 PFLOP/s under the power cap);
 // 988 of 15154, forward, 655 to 667 us alone (1.57 PFLOP/s) and 800 to 848 under repetition; one label 207 to 228 us (the table at 6 TB/s in the
-// product); 1145 labels, 50257 x 1032, both 570 to 583 us; 206 labels, 1024 x 256, both 51.7 to 54 us (nine launches).
+// product); 1145 labels, 50257 x 1032, both 570 to 583 us; 206 labels, 1024 x 256, both 52 to 55 us (nine launches).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
